@@ -73,7 +73,8 @@ typedef enum gmlp_status {
     GMLP_ERR_TIMEOUT = -8,    /* a bounded device-side wait ran out (see gmlp_device_status) */
     GMLP_ERR_UNSUPPORTED = -9,/* the forced variant cannot run this shape (SKINNY: M <= 128, or <= 256 on layers whose
                                  two GEMMs both have its cluster form) */
-    GMLP_ERR_STATIC_LIMIT = -10 /* gmlp_forward_static: the shape needs more than its fixed built-in scratch */
+    GMLP_ERR_STATIC_LIMIT = -10,/* gmlp_forward_static: the shape needs more than its fixed built-in scratch */
+    GMLP_ERR_INDEX = -11      /* with GMLP_FLAG_CHECKED: a cache slot, page or length on the device was out of range */
 } gmlp_status;
 
 enum {
@@ -283,6 +284,165 @@ typedef struct gmlp_gqa_args {
     void* stream;             /* cudaStream_t */
 } gmlp_gqa_args;
 int gmlp_gqa_attention(const gmlp_gqa_args* args);
+
+/*
+ * Products with 4-bit weights, for a few tokens (decode).  A matrix W [K, N] is held as codes q in 0..15 with one scale s (bf16)
+ * and, optionally, one zero point z (0..15; 8 without) per group of `group` = 32, 64 or 128 input rows and output column:
+ *     W[k, n] = (q[k, n] - z[k / group, n]) * s[k / group, n].
+ * The buffers of a gmlp_w4_matrix are filled once by one of
+ *     gmlp_w4_quantize  from a bf16 matrix: without zero points s = bf16(max|w| / 7), q = clamp(rint(w / s) + 8, 0, 15); with them
+ *                       s = bf16((hi - lo) / 15), lo = min(0, min w), hi = max(0, max w), z = clamp(rint(-lo / s), 0, 15),
+ *                       q = clamp(rint(w / s) + z, 0, 15).  A scale of 0 makes the group 0; a group with an infinity or a NaN
+ *                       (or a range past float's) becomes NaN throughout.
+ *     gmlp_w4_pack      from codes (one byte each, low four bits), scales and zero points that some other tool made.
+ * Their order is the library's own (tiles of 16 columns by 128 rows); gmlp_w4_dequantize writes the bf16 matrix back, e.g. for a
+ * prompt's gmlp_forward (rounded once; pass GMLP_FLAG_WEIGHTS_IN_STREAM_ORDER to a gmlp_forward that follows on the stream).
+ * K must be a multiple of `group`; N is any positive number; both at most 2^20.
+ */
+typedef struct gmlp_w4_matrix {
+    const void* codes;        /* device, gmlp_w4_code_bytes(K, N) bytes */
+    const void* scales;       /* device, gmlp_w4_scale_count(K, N, group) bf16 */
+    const void* zeros;        /* device, gmlp_w4_scale_count(K, N, group) bytes, or NULL: every zero point is 8 */
+    int64_t K, N;             /* input rows, output columns */
+    int32_t group;
+    int32_t reserved;         /* must be 0 */
+} gmlp_w4_matrix;
+uint64_t gmlp_w4_code_bytes(int64_t K, int64_t N);                       /* 0 for invalid sizes */
+uint64_t gmlp_w4_scale_count(int64_t K, int64_t N, int32_t group);
+
+typedef struct gmlp_w4_layout_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_w4_layout_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED | GMLP_FLAG_WEIGHTS_OUT_IN: W is [N, K], scales and zeros [N, K / group] */
+    void* W;                  /* device; quantize: bf16 [K, N], read; pack: bytes [K, N], read; dequantize: bf16 [K, N], written */
+    const void* scales;       /* pack only: device, bf16 [K / group, N] */
+    const void* zeros;        /* pack only: device, bytes [K / group, N], given exactly if m.zeros is */
+    gmlp_w4_matrix m;         /* written by quantize (zero points if m.zeros is given) and pack, read by dequantize */
+    void* stream;             /* cudaStream_t */
+} gmlp_w4_layout_args;
+int gmlp_w4_quantize(const gmlp_w4_layout_args* args);
+int gmlp_w4_pack(const gmlp_w4_layout_args* args);
+int gmlp_w4_dequantize(const gmlp_w4_layout_args* args);
+
+/*
+ * Y = X W for a 4-bit W: X [M, K], Y [M, N] row-major bf16, M at most GMLP_W4_MAX_M.  Codes are used exactly, group sums and their
+ * scaling are fp32, Y is rounded once.  Beyond GMLP_W4_MAX_M tokens the product is no longer bound by the weights' bytes:
+ * dequantise and use the bf16 operators (GMLP_ERR_SHAPE).  Everything is read in stream order (the weights too).
+ */
+#define GMLP_W4_MAX_M 64
+typedef struct gmlp_w4_matmul_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_w4_matmul_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED */
+    const void* X;            /* device, [M, K] bf16 */
+    void* Y;                  /* device, [M, N] bf16, written; must not overlap an input */
+    int64_t M;
+    gmlp_w4_matrix W;
+    void* stream;             /* cudaStream_t */
+} gmlp_w4_matmul_args;
+int gmlp_w4_matmul(const gmlp_w4_matmul_args* args);
+/* How a product of M tokens (terms = 1 for bf16 input, 2 for the two-term inputs inside gmlp_w4_forward) with a [K, N] matrix (gated:
+ * with two of them) is launched on a device with `sm_count` SMs (0: the current device, 148 if there is none): plan[0] = columns of
+ * eight tokens, [1] = column groups per CTA (32 columns each; gated: 16), [2] = CTAs per cluster (K is split over them), [3] = steps of
+ * K per chunk of X in shared memory, [4] = steps in all, [5] = bytes of shared memory, [6] = CTAs.  Pure host arithmetic. */
+int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t sm_count, int32_t plan[7]);
+
+/*
+ * The Gated MLP on 4-bit weights: Y = (act(Xn Wg) (.) (Xn Wu)) Wd with Wg, Wu [d_model, d_ff] and Wd [d_ff, d_model] as
+ * gmlp_w4_matrix, M at most GMLP_W4_MAX_M; the prologue and the gate activation are those of gmlp_forward_ex.  The normed input and
+ * the gated product are kept to 16 bits of significand (two bf16 terms), not rounded to bf16; Y is rounded once.
+ * Wg and Wu must agree in group and in having zero points.  d_model is Wg.K, d_ff is Wg.N (both multiples of a group).
+ * workspace: gmlp_w4_workspace_bytes(), 256-byte aligned, required; no state is kept in it between calls.
+ */
+typedef struct gmlp_w4_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_w4_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED | GMLP_FLAG_RMSNORM | GMLP_FLAG_ACT_* */
+    const void* X;            /* device, [M, d_model] bf16 */
+    void* Y;                  /* device, [M, d_model] bf16, written */
+    int64_t M;
+    gmlp_w4_matrix Wg, Wu, Wd;
+    const void* rms_gain;     /* device, [d_model] bf16, or NULL */
+    float rms_eps;
+    float act_beta;           /* GMLP_FLAG_ACT_SWISH */
+    void* stream;             /* cudaStream_t */
+    void* workspace;
+    uint64_t workspace_bytes;
+    uint64_t reserved;        /* must be 0 */
+} gmlp_w4_args;
+int gmlp_w4_forward(const gmlp_w4_args* args);
+uint64_t gmlp_w4_workspace_bytes(int64_t M, int64_t d_model, int64_t d_ff, uint32_t flags);
+
+/*
+ * A paged key/value cache held in 4 bits.  A page holds page_size tokens (a multiple of 16) of every key/value head; a token lives
+ * in slot  page * page_size + place.  Per token and head the head_dim (64 or 128) channels are cut into groups of `group` (32, 64
+ * or 128, at most head_dim), quantised as gmlp_w4_quantize does with zero points:
+ *     codes   [n_pages][n_kv_heads][page_size][head_dim / 2] bytes: 32 units of head_dim / 32 nibbles, channel c in nibble c / 32
+ *             (the lowest bits are nibble 0) of unit c % 32,
+ *     params  [n_pages][n_kv_heads][page_size][head_dim / group][2] bf16: scale, zero point,
+ * one such pair for K and one for V.  n_pages * page_size must fit 31 bits; byte offsets may pass 32.
+ */
+typedef struct gmlp_kv4_cache {
+    void* k_codes;            /* device; written by gmlp_kv4_append */
+    void* k_params;
+    void* v_codes;
+    void* v_params;
+    int64_t n_pages;
+    int32_t n_kv_heads, page_size, head_dim, group;
+    int64_t reserved;         /* must be 0 */
+} gmlp_kv4_cache;
+
+/*
+ * gmlp_kv4_append: rows of K and V [T, n_kv_heads * head_dim] bf16 (the layout of gmlp_qkv_proj) go to the cache at slots[i]
+ * (int64, device); a negative slot skips its row (padding).  The slots of one call must differ: of two rows with the same slot
+ * either may win, channel group by channel group.  No other row of the cache is touched.
+ * gmlp_kv4_gather: the reverse; the rows of slots[i] become bf16 rows of K and V (rounded once), for gmlp_gqa_attention over a
+ * prompt's earlier chunks.  A slot may occur more than once; a negative one gives a row of zeros.
+ * A slot past the cache is skipped (gather: zeros) and reported: GMLP_ERR_INDEX with GMLP_FLAG_CHECKED, else through
+ * gmlp_device_status().  T at most 2^24.
+ */
+typedef struct gmlp_kv4_rows_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_kv4_rows_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED */
+    void* K;                  /* device, [T, n_kv_heads * head_dim] bf16; append: read, gather: written */
+    void* V;
+    const void* slots;        /* device, [T] int64 */
+    int64_t T;
+    gmlp_kv4_cache cache;
+    void* stream;             /* cudaStream_t */
+} gmlp_kv4_rows_args;
+int gmlp_kv4_append(const gmlp_kv4_rows_args* args);
+int gmlp_kv4_gather(const gmlp_kv4_rows_args* args);
+
+/*
+ * Grouped-query attention over the cache, for the newest q_len (1..GMLP_KV4_MAX_QUERIES) positions of each of B requests:
+ *     O = softmax(scale * Q K^T) V,   position i of a request with length L sees keys 0 .. L - q_len + i  (its own included),
+ * Q, O [B * q_len, n_q_heads * head_dim] bf16, position by position; request b's key j is in slot
+ * block_table[b][j / page_size] * page_size + j % page_size.  lengths[b] counts the keys, the new positions' included (append them
+ * first).  A position that sees no key (L = 0, or L < q_len) gets zeros.  What the pages hold past a request's end, and table entries
+ * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value is rounded to bf16 for the
+ * second product; O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table are reported as above;
+ * their keys are left out.
+ * workspace: gmlp_kv4_workspace_bytes(); may be NULL where that is 0; no state is kept in it between calls.
+ */
+#define GMLP_KV4_MAX_QUERIES 16
+typedef struct gmlp_kv4_attention_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_kv4_attention_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED */
+    const void* Q;            /* device, [B * q_len, n_q_heads * head_dim] bf16 */
+    void* O;                  /* device, the same shape, written */
+    gmlp_kv4_cache cache;
+    const void* block_table;  /* device, [B, table_width] int32 */
+    const void* lengths;      /* device, [B] int32 */
+    int64_t B, table_width;
+    int32_t n_q_heads, q_len;
+    float scale;              /* e.g. 1 / sqrt(head_dim); any finite number */
+    int32_t reserved;         /* must be 0 */
+    void* stream;             /* cudaStream_t */
+    void* workspace;          /* 256-byte aligned */
+    uint64_t workspace_bytes;
+} gmlp_kv4_attention_args;
+int gmlp_kv4_attention(const gmlp_kv4_attention_args* args);
+/* On a device with `sm_count` SMs (0: the current device, 148 if there is none); 0 bytes too for invalid sizes. */
+uint64_t gmlp_kv4_workspace_bytes(int64_t B, int32_t q_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                  int64_t table_width, int32_t page_size, int32_t sm_count);
 
 /*
  * The same call for a caller whose activations live in HOST memory: copies X_host

@@ -25,6 +25,8 @@
 #include "umma_skinny_cluster.cuh"
 #include "umma_skinny_fused.cuh"
 #include "gqa_attention.cuh"
+#include "w4_matmul.cuh"
+#include "kv4.cuh"
 
 namespace {
 
@@ -33,6 +35,7 @@ using gmlp::bf16;
 constexpr int kVersion = 101;            // 101: one-kernel small-M form, tuned small-M forms in the tune file, GMLP_FLAG_WEIGHTS_IN_STREAM_ORDER
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxDim = (int64_t)1 << 30;      // per-dimension limit (TMA coordinates are int32)
+constexpr int64_t kW4MaxDim = (int64_t)1 << 20;    // rows and columns of a 4-bit matrix
 constexpr uint32_t kKnownFlags = GMLP_FLAG_RMSNORM | GMLP_FLAG_CHECKED | GMLP_FLAG_ACT_SWISH | GMLP_FLAG_ACT_GLU |
                                  GMLP_FLAG_ACT_GELU | GMLP_FLAG_WEIGHTS_OUT_IN | GMLP_FLAG_Y_FP32 | GMLP_FLAG_WEIGHTS_IN_STREAM_ORDER;
 constexpr gmlp::GateAct kSilu = {1.0f, 0};
@@ -141,6 +144,7 @@ struct DeviceState {
     bool skinny_attr_set = false;
     bool skinny_cluster_attr_set = false;
     bool skinny_fused_attr_set = false;
+    bool w4_attr_set[48] = {};                   // (token tiles - 1) * 6 + gated * 3 + group
     int fused_capacity[9] = {};                  // the same for the fused small-M kernel
     int cluster_capacity[2][9] = {};             // clusters of C CTAs of the cluster-form kernels resident at once (0 = not asked yet)
     // arrival-counter regions zeroed by the library (the kernels leave them zero after every call); a few are
@@ -1948,6 +1952,9 @@ int gqa_attention_impl(const gmlp_gqa_args* a) {
     return GMLP_OK;
 }
 
+#include "w4_host.cuh"
+#include "kv4_host.cuh"
+
 // Empirical schedule selection for one shape: time every tensor-core schedule that can run it, keep the fastest.
 int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* best_us) {
     if (a == nullptr) return GMLP_ERR_NULL;
@@ -2174,6 +2181,53 @@ int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* b
 }  // namespace
 
 extern "C" {
+
+#define GMLP_GUARDED(call)          \
+    do {                            \
+        try {                       \
+            return call;            \
+        } catch (...) {             \
+            return GMLP_ERR_LAUNCH; \
+        }                           \
+    } while (0)
+int gmlp_w4_quantize(const gmlp_w4_layout_args* args) { GMLP_GUARDED(w4_layout_impl(args, gmlp::kW4FromBf16)); }
+int gmlp_w4_pack(const gmlp_w4_layout_args* args) { GMLP_GUARDED(w4_layout_impl(args, gmlp::kW4FromCodes)); }
+int gmlp_w4_dequantize(const gmlp_w4_layout_args* args) { GMLP_GUARDED(w4_layout_impl(args, -1)); }
+int gmlp_w4_matmul(const gmlp_w4_matmul_args* args) { GMLP_GUARDED(w4_matmul_impl(args)); }
+int gmlp_w4_forward(const gmlp_w4_args* args) { GMLP_GUARDED(w4_forward_impl(args)); }
+int gmlp_kv4_append(const gmlp_kv4_rows_args* args) { GMLP_GUARDED(kv4_rows_impl(args, true)); }
+int gmlp_kv4_gather(const gmlp_kv4_rows_args* args) { GMLP_GUARDED(kv4_rows_impl(args, false)); }
+int gmlp_kv4_attention(const gmlp_kv4_attention_args* args) { GMLP_GUARDED(kv4_attention_impl(args)); }
+
+uint64_t gmlp_w4_code_bytes(int64_t K, int64_t N) {
+    if (K <= 0 || N <= 0 || K > kW4MaxDim || N > kW4MaxDim) return 0;
+    return (uint64_t)((K + 127) / 128) * (uint64_t)((N + 15) / 16) * 1024u;
+}
+uint64_t gmlp_w4_scale_count(int64_t K, int64_t N, int32_t group) {
+    if (group != 32 && group != 64 && group != 128) return 0;
+    return gmlp_w4_code_bytes(K, N) / 1024u * 16u * (uint64_t)(128 / group);
+}
+int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t sm_count, int32_t plan[7]) {
+    if (plan == nullptr) return GMLP_ERR_NULL;
+    if (M < 1 || M > gmlp::kW4MaxM || terms < 1 || terms > 2 || K <= 0 || N <= 0 || K > kW4MaxDim || N > kW4MaxDim) return GMLP_ERR_SHAPE;
+    const int KB = (int)((K + 127) / 128), n16 = (int)((N + 15) / 16);
+    const W4Plan p = w4_plan((int)M, terms, KB, gated ? n16 : (n16 + 1) / 2, sm_count > 0 ? sm_count : current_sm_count());
+    const int wk = 8 >> p.wr_log2, kb_cta = (KB + p.cluster - 1) / p.cluster;
+    const int32_t out[7] = {p.nt, 1 << p.wr_log2, p.cluster, p.chunk, (kb_cta + wk - 1) / wk, (int32_t)p.smem, p.groups * p.cluster};
+    for (int i = 0; i < 7; ++i) plan[i] = out[i];
+    return GMLP_OK;
+}
+uint64_t gmlp_w4_workspace_bytes(int64_t M, int64_t d_model, int64_t d_ff, uint32_t flags) {
+    return w4_forward_workspace(M, d_model, d_ff, flags);
+}
+uint64_t gmlp_kv4_workspace_bytes(int64_t B, int32_t q_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                  int64_t table_width, int32_t page_size, int32_t sm_count) {
+    if (page_size < 16 || page_size > 65536 || page_size % 16 != 0 || (head_dim != 64 && head_dim != 128) || B == 0 ||
+        check_kv4_attention(B, q_len, n_q_heads, n_kv_heads, table_width, page_size) != GMLP_OK)
+        return 0;
+    return kv4_plan(B, q_len, n_q_heads / n_kv_heads, n_kv_heads, head_dim, table_width * page_size,
+                    sm_count > 0 ? sm_count : current_sm_count()).workspace;
+}
 
 int gmlp_gqa_attention(const gmlp_gqa_args* args) {
     try {
@@ -2493,6 +2547,7 @@ const char* gmlp_status_string(int status) {
         case GMLP_ERR_UNSUPPORTED: return "the forced variant cannot run this shape";
         case GMLP_ERR_STATIC_LIMIT:
             return "gmlp_forward_static: shape exceeds its fixed scratch (M <= 16, no RMSNorm, scratch <= 12 MiB)";
+        case GMLP_ERR_INDEX: return "a cache slot, page or length on the device is out of range";
         default: return "unknown status";
     }
 }

@@ -15,6 +15,11 @@ __device__ __forceinline__ void report_timeout(int kernel_id, int site) {
     atomicCAS(&g_device_status, 0, (kernel_id << 16) | (site & 0xFFFF));
 }
 
+// The same word for an index that a caller's array holds and that no buffer has (a cache slot, a page, a length): the access is
+// skipped and (kIndexStatus << 16 | site) is left behind.
+constexpr int kIndexStatus = 200;
+__device__ __forceinline__ void report_index(int site) { atomicCAS(&g_device_status, 0, (kIndexStatus << 16) | site); }
+
 // Optional timeline of the small-M kernels (builds with -DGMLP_TRACE only; nothing of it exists in the normal
 // library): one thread per site stores the global nanosecond timer, the last launch of each kernel wins.
 #ifdef GMLP_TRACE

@@ -1,0 +1,620 @@
+// A paged key/value cache held in 4 bits, and attention over it.
+//
+// Cache: codes [n_pages][n_kv_heads][page_size][D / 2] bytes and parameters [n_pages][n_kv_heads][page_size][D / G] pairs of
+// bf16 (scale s, zero point z, an integer 0..15), one such pair of arrays for K and one for V; a value is (q - z) * s.  A token
+// lives in slot page * page_size + place.  The D codes of a row lie in 32 units of D / 32 nibbles, channel c in nibble c / 32 of
+// unit c % 32 (16-bit units for D = 128, bytes for D = 64): a lane that reads 8 neighbouring units of a key gets, with one shift
+// and one and-or per pair, the A operands of the score product, a lane that reads 4 units of a value those of the output product,
+// and each nibble position holds channels of one block of 32, so that every mma stays inside one group of G >= 32 channels.
+#pragma once
+#include "common.cuh"
+#include "ptx.cuh"
+#include "w4_matmul.cuh"
+
+namespace gmlp {
+
+struct Kv4Cache {
+    uint8_t* codes[2];         // K, V
+    uint32_t* params[2];       // bf16 pairs: scale in the low half, zero point in the high half
+    int n_pages, n_kv_heads, page_size, head_dim, group;
+};
+
+// ------------------------------------------------------------------------------------------------ append and gather
+__device__ __forceinline__ float redux_min_nan(float v) {
+    float r;
+    asm("redux.sync.min.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float redux_max_nan(float v) {
+    float r;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// One warp per token, head and K or V.  Lane r holds unit r, channels r + 32 j; minimum and maximum of a group are warp
+// reductions.  Bound by HBM (256 bytes in, 68 to 80 out per row of 128 channels) and, for a few tokens, by the launch.
+template <int D, int G>
+__global__ void __launch_bounds__(256)
+kv4_append_kernel(const bf16* K, const bf16* V, const Kv4Cache c, const int64_t* slots, int64_t items, int64_t total_slots)
+{
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    constexpr int NJ = D / 32, NG = D / G, PER = G / 32;
+    const int lane = threadIdx.x & 31;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);       // (token * 2 + which) * heads + head
+    if (item >= items) return;
+    const int64_t tw = item / c.n_kv_heads;
+    const int head = (int)(item - tw * c.n_kv_heads), which = (int)(tw & 1);
+    const int64_t token = tw >> 1;
+    const int64_t slot = slots[token];
+    if (slot < 0) return;                            // padding: nothing is written
+    if (slot >= total_slots) {
+        if (lane == 0) report_index(1);
+        return;
+    }
+    const bf16* x = (which ? V : K) + (token * c.n_kv_heads + head) * D;
+    float v[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) v[j] = __bfloat162float(x[j * 32 + lane]);
+    const uint32_t page = (uint32_t)slot / (uint32_t)c.page_size;
+    const int64_t row = ((int64_t)page * c.n_kv_heads + head) * c.page_size + ((uint32_t)slot - page * (uint32_t)c.page_size);
+    uint32_t unit = 0, par[NG];
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+        float lo = v[gi * PER], hi = lo;
+        bool finite = lo - lo == 0.0f;
+#pragma unroll
+        for (int j = 1; j < PER; ++j) {
+            const float a = v[gi * PER + j];
+            lo = fminf(lo, a);
+            hi = fmaxf(hi, a);
+            finite = finite && a - a == 0.0f;
+        }
+        if (!finite) lo = hi = __int_as_float(0x7FC00000);
+        lo = redux_min_nan(lo);
+        hi = redux_max_nan(hi);
+        finite = lo - lo == 0.0f;                    // a NaN of any lane is in both
+        lo = fminf(lo, 0.0f);
+        hi = fmaxf(hi, 0.0f);
+        float s = __bfloat162float(__float2bfloat16_rn((hi - lo) / 15.0f));
+        if (!finite || s - s != 0.0f) s = __int_as_float(0x7FC00000);
+        const bool some = s > 0.0f;
+        const float z = some ? fminf(fmaxf(rintf(-lo / s), 0.0f), 15.0f) : 0.0f;
+        par[gi] = pack_bf16x2(s, z);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const float q = some ? fminf(fmaxf(rintf(v[gi * PER + j] / s) + z, 0.0f), 15.0f) : 0.0f;
+            unit |= (uint32_t)q << (4 * (gi * PER + j));
+        }
+    }
+    uint8_t* codes = c.codes[which] + row * (D / 2);
+    if constexpr (D == 128) reinterpret_cast<uint16_t*>(codes)[lane] = (uint16_t)unit;
+    else codes[lane] = (uint8_t)unit;
+    if (lane < NG) {
+        uint32_t mine = par[0];
+#pragma unroll
+        for (int gi = 1; gi < NG; ++gi)
+            if (lane == gi) mine = par[gi];
+        c.params[which][row * NG + lane] = mine;
+    }
+}
+
+// Slots back to bf16 rows [T][n_kv_heads * D].  Four lanes per token, head and K or V: a lane reads 8 units and writes 8
+// neighbouring channels of each block of 32.  Bound by the bf16 rows it writes.
+template <int D, int G>
+__global__ void __launch_bounds__(256)
+kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int64_t items, int64_t total_slots)
+{
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    constexpr int NJ = D / 32, NG = D / G;
+    const int t = threadIdx.x & 3;
+    const int64_t item = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2);
+    if (item >= items) return;
+    const int64_t tw = item / c.n_kv_heads;
+    const int head = (int)(item - tw * c.n_kv_heads), which = (int)(tw & 1);
+    const int64_t token = tw >> 1;
+    const int64_t slot = slots[token];
+    bf16* out = (which ? V : K) + (token * c.n_kv_heads + head) * D + 8 * t;
+    if (slot < 0 || slot >= total_slots) {           // padding: a row of zeros; a slot past the cache is reported, too
+        if (slot >= 0 && t == 0) report_index(2);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) *reinterpret_cast<uint4*>(out + 32 * j) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const uint32_t page = (uint32_t)slot / (uint32_t)c.page_size;
+    const int64_t row = ((int64_t)page * c.n_kv_heads + head) * c.page_size + ((uint32_t)slot - page * (uint32_t)c.page_size);
+    uint32_t w[D / 32], par[NG];
+    const uint8_t* codes = c.codes[which] + row * (D / 2) + t * (D / 8);
+    if constexpr (D == 128) {
+        const uint4 u = *reinterpret_cast<const uint4*>(codes);
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(codes);
+        w[0] = u.x; w[1] = u.y;
+    }
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) par[gi] = c.params[which][row * NG + gi];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const float s = bf16_lo(par[j * 32 / G]), z = bf16_hi(par[j * 32 / G]);
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                // units 2 i and 2 i + 1
+            uint32_t a, b;
+            if constexpr (D == 128) {
+                a = (w[i] >> (4 * j)) & 15u;
+                b = (w[i] >> (16 + 4 * j)) & 15u;
+            } else {
+                a = (w[i >> 1] >> (16 * (i & 1) + 4 * j)) & 15u;
+                b = (w[i >> 1] >> (16 * (i & 1) + 8 + 4 * j)) & 15u;
+            }
+            o[i] = pack_bf16x2(((float)a - z) * s, ((float)b - z) * s);
+        }
+        *reinterpret_cast<uint4*>(out + 32 * j) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+// T new positions per request (the last T of its sequence), O = softmax(scale * Q K^T) V over the keys up to each position's
+// own.  A CTA takes one request, one key/value head, up to 8 NT of its T * (query heads per key/value head) query rows and a range
+// of the keys; its four warps take 16-token tiles in turn.  Per tile and warp (flash-style, running maximum and sum in fp32):
+//   S^T = K Q^T   tokens are the 16 mma rows, query rows the 8 columns, (q - z) exact in bf16; the token's scale is a row
+//                 factor in fp32, per group of channels;
+//   P'  = exp2(S - m) * s_v, rounded to bf16 once as the operand of the second product; transposed in registers (movmatrix);
+//   O^T += V^T P'^T   with 8 instead of z subtracted from the codes (one constant); the rest, sum of P' (z - 8), is a scalar per
+//                 query row and group, summed in fp32 from the same rounded P' and taken off at the end.
+// Bound by HBM and by the issue slots of the unpacking (about two instructions per value); the tensor pipe idles.
+// The next tile's codes and parameters are loaded while the current one is computed, the page-table entry one tile earlier.
+constexpr int kKv4Warps = 4;
+constexpr int kKv4Threads = 32 * kKv4Warps;
+constexpr int kKv4Tile = 16;
+
+struct Kv4AttnArgs {
+    const bf16* Q;             // [B * T][Hq * D]
+    bf16* O;
+    Kv4Cache c;
+    const int32_t* table;      // [B][width]
+    const int32_t* lengths;    // [B]
+    float* part;               // [B * Hkv * col_tiles][splits][8 NT][D + 2]: O, then maximum and sum; unused for one split
+    int B, T, Hq, ratio, width, splits, col_tiles;
+    float scale_log2;
+};
+
+// Keys per split of a request with `len` keys: the same formula in both kernels.
+__device__ __forceinline__ int kv4_split_keys(int len, int splits) {
+    const int per = (len + splits - 1) / splits;
+    const int rounded = (per + kKv4Warps * kKv4Tile - 1) / (kKv4Warps * kKv4Tile) * (kKv4Warps * kKv4Tile);
+    return rounded < 2 * kKv4Warps * kKv4Tile ? 2 * kKv4Warps * kKv4Tile : rounded;
+}
+// A request's keys: its length, or what its row of the page table can hold.
+__device__ __forceinline__ int kv4_length(const Kv4AttnArgs& p, int b) {
+    const int64_t most = (int64_t)p.width * p.c.page_size;
+    const int len = p.lengths[b];
+    return len < 0 ? 0 : ((int64_t)len > most ? (int)most : len);
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+template <int D, int G>
+struct Kv4Tile {
+    uint32_t k[2][D / 32];     // rows (tokens) g and g + 8: units 8 t .. 8 t + 7
+    uint32_t v[4][D / 64];     // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9: units 4 g .. 4 g + 3
+    uint32_t kp[2][D / G], vp[2][D / G];
+};
+
+template <int NG>
+__device__ __forceinline__ void kv4_load_params(uint32_t (&d)[NG], const uint32_t* p) {
+    if constexpr (NG == 1) {
+        d[0] = ld_4B(p);
+    } else if constexpr (NG == 2) {
+        const uint2 v = ld_8B(p);
+        d[0] = v.x; d[1] = v.y;
+    } else {
+        const uint4 v = ld_16B(p);
+        d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
+    }
+}
+
+template <int D, int G, int NT>
+__global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_kernel(const Kv4AttnArgs p)
+{
+    constexpr int NJ = D / 32, NG = D / G, PER = G / 32, MT = D / 16;        // blocks of 32, groups, output tiles
+    constexpr int COLS = 8 * NT;
+    __shared__ float s_o[kKv4Warps][COLS][D + 4];
+    __shared__ float s_m[kKv4Warps][COLS], s_l[kKv4Warps][COLS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int split = blockIdx.x, head = (int)blockIdx.y / p.col_tiles, ct = (int)blockIdx.y % p.col_tiles, b = blockIdx.z;
+    const int cols_all = p.T * p.ratio, col0 = ct * COLS;
+
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int len = kv4_length(p, b);
+    const int keys = kv4_split_keys(len, p.splits);
+    const int first = split * keys, last = min(first + keys, len);
+    if (split > 0 && first >= len) return;           // the joining kernel uses the same formula and does not look here
+    if (split == 0 && ct == 0 && head == 0 && threadIdx.x == 0 && (p.lengths[b] < 0 || p.lengths[b] > len)) report_index(3);
+
+    // query operands: column n = query row col0 + n of this head, channels 32 j + 8 t + 0..7
+    uint32_t q[NT][NJ][4];
+    int limit[NT][2];                                // keys that the lane's two columns of a tile may see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int col = col0 + n * 8 + g;
+        const int i = col / p.ratio, r = col - i * p.ratio;
+        const bf16* row = p.Q + ((int64_t)(b * (int64_t)p.T + i) * p.Hq + head * p.ratio + r) * D + 8 * t;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (col < cols_all) x = *reinterpret_cast<const uint4*>(row + 32 * j);
+            if constexpr (D == 128) {
+                q[n][j][0] = x.x; q[n][j][1] = x.y; q[n][j][2] = x.z; q[n][j][3] = x.w;
+            } else {                                 // bytes come apart as units (0, 2), (1, 3), (4, 6), (5, 7)
+                q[n][j][0] = __byte_perm(x.x, x.y, 0x5410);
+                q[n][j][1] = __byte_perm(x.x, x.y, 0x7632);
+                q[n][j][2] = __byte_perm(x.z, x.w, 0x5410);
+                q[n][j][3] = __byte_perm(x.z, x.w, 0x7632);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = col0 + n * 8 + 2 * t + e;
+            limit[n][e] = c < cols_all ? min(last, len - p.T + 1 + c / p.ratio) : 0;
+        }
+    }
+
+    float o[MT][NT][4], m[NT][2], l[NT][2], zsum[NG][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            m[n][e] = -INFINITY;
+            l[n][e] = 0.0f;
+#pragma unroll
+            for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][n][e] = 0.0f;
+    }
+
+    const int32_t* table = p.table + (int64_t)b * p.width;
+    // Places of this warp's tiles, stepped without divisions: page-table entry `entry`, token `place` of its page.
+    const int stride = kKv4Warps * kKv4Tile, page_step = stride / p.c.page_size, place_step = stride % p.c.page_size;
+    auto advance = [&](int& entry, int& place) {
+        entry += page_step;
+        place += place_step;
+        if (place >= p.c.page_size) {
+            place -= p.c.page_size;
+            ++entry;
+        }
+    };
+    // A tile's loads; a page outside of the cache is not read.  Tokens past the end of a request may hold anything.
+    auto fetch = [&](Kv4Tile<D, G>& d, int page, int place) {
+        if ((uint32_t)page >= (uint32_t)p.c.n_pages) return;
+        const int64_t row = ((int64_t)page * p.c.n_kv_heads + head) * p.c.page_size + place;
+        const uint8_t* k = p.c.codes[0] + (row + g) * (D / 2) + t * (D / 8);
+        const uint8_t* v = p.c.codes[1] + (row + 2 * t) * (D / 2) + g * (D / 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (D == 128) {
+                const uint4 x = ld_once_16B(k + h * 8 * (D / 2));
+                d.k[h][0] = x.x; d.k[h][1] = x.y; d.k[h][2] = x.z; d.k[h][3] = x.w;
+            } else {
+                const uint2 x = ld_8B(k + h * 8 * (D / 2));
+                d.k[h][0] = x.x; d.k[h][1] = x.y;
+            }
+            kv4_load_params<NG>(d.kp[h], p.c.params[0] + (row + g + 8 * h) * NG);
+            kv4_load_params<NG>(d.vp[h], p.c.params[1] + (row + g + 8 * h) * NG);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint8_t* a = v + ((i >> 1) * 8 + (i & 1)) * (D / 2);
+            if constexpr (D == 128) {
+                const uint2 x = ld_8B(a);
+                d.v[i][0] = x.x; d.v[i][1] = x.y;
+            } else {
+                d.v[i][0] = ld_4B(a);
+            }
+        }
+    };
+
+    int token = first + warp * kKv4Tile;
+    int entry = token / p.c.page_size, place = token - entry * p.c.page_size;        // of the tile whose entry is read next
+    int page = token < last ? (int)ld_4B(table + entry) : -1, cur_place = place;
+    advance(entry, place);
+    int next_page = token + stride < last ? (int)ld_4B(table + entry) : -1, next_place = place;
+    advance(entry, place);
+    Kv4Tile<D, G> cur, nxt;
+    {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&cur);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(cur) / 4); ++i) w[i] = 0;
+        nxt = cur;
+    }
+    if (token < last) fetch(cur, page, cur_place);
+
+    for (; token < last; token += stride) {
+        const int page_ahead = token + 2 * stride < last ? (int)ld_4B(table + entry) : -1;
+        if (token + stride < last) fetch(nxt, next_page, next_place);
+        next_place = place;
+        advance(entry, place);
+        const bool page_ok = (uint32_t)page < (uint32_t)p.c.n_pages;
+        if (!page_ok && lane == 0) report_index(4);
+
+        // scores of tokens (rows) g and g + 8, columns 2 t and 2 t + 1
+        float s[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+            float acc[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
+            uint32_t zc[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {            // 128 + z in both halves (z <= 15: exact)
+                const uint32_t z2 = __byte_perm(cur.kp[h][gi], 0, 0x3232);
+                asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(zc[h]) : "r"(z2), "r"(0x43004300u));
+            }
+#pragma unroll
+            for (int jj = 0; jj < PER; ++jj) {
+                const int j = gi * PER + jj;
+                uint32_t a[8];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int at = (u >> 1) * 4 + (u & 1) * 2;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t w = D == 128 ? cur.k[h][u] >> (4 * j) : cur.k[h][u >> 1] >> (8 * (u & 1) + 4 * j);
+                        a[at + h] = bf16x2_sub((w & 0x000F000Fu) | 0x43004300u, zc[h]);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma_bf16_16816(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
+                    mma_bf16_16816(acc[n], a[4], a[5], a[6], a[7], q[n][j][2], q[n][j][3]);
+                }
+            }
+            const float s0 = bf16_lo(cur.kp[0][gi]), s1 = bf16_lo(cur.kp[1][gi]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][0] = fmaf(acc[n][0], s0, s[n][0]);
+                s[n][1] = fmaf(acc[n][1], s0, s[n][1]);
+                s[n][2] = fmaf(acc[n][2], s1, s[n][2]);
+                s[n][3] = fmaf(acc[n][3], s1, s[n][3]);
+            }
+        }
+        // mask, running maximum; a masked score is -inf whatever its token holds
+        const int t0 = page_ok ? token + g : INT_MAX - 16;
+        bool moved = false;
+        float alpha[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                s[n][e] = t0 < limit[n][e] ? s[n][e] * p.scale_log2 : -INFINITY;
+                s[n][2 + e] = t0 + 8 < limit[n][e] ? s[n][2 + e] * p.scale_log2 : -INFINITY;
+                float top = fmaxf(s[n][e], s[n][2 + e]);
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                alpha[n][e] = 1.0f;
+                if (top > m[n][e]) {
+                    alpha[n][e] = fast_exp2(m[n][e] - top);                  // 0 from -inf
+                    m[n][e] = top;
+                    moved = true;
+                }
+            }
+        if (__any_sync(0xFFFFFFFFu, moved)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    l[n][e] *= alpha[n][e];
+#pragma unroll
+                    for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] *= alpha[n][e];
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    o[i][n][0] *= alpha[n][0];
+                    o[i][n][1] *= alpha[n][1];
+                    o[i][n][2] *= alpha[n][0];
+                    o[i][n][3] *= alpha[n][1];
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float base = m[n][e] == -INFINITY ? 0.0f : m[n][e];
+                s[n][e] = fast_exp2(s[n][e] - base);
+                s[n][2 + e] = fast_exp2(s[n][2 + e] - base);
+                l[n][e] += s[n][e] + s[n][2 + e];
+            }
+        // second product, group by group
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float sv = bf16_lo(cur.vp[h][gi]);
+                    // a masked token adds nothing, not even 0 * NaN
+                    const float a = t0 + 8 * h < limit[n][0] ? s[n][2 * h] * sv : 0.0f;
+                    const float c = t0 + 8 * h < limit[n][1] ? s[n][2 * h + 1] * sv : 0.0f;
+                    const uint32_t w = pack_bf16x2(a, c);
+                    const float z = t0 + 8 * h < last ? bf16_hi(cur.vp[h][gi]) - 8.0f : 0.0f;
+                    zsum[gi][n][0] = fmaf(bf16_lo(w), z, zsum[gi][n][0]);
+                    zsum[gi][n][1] = fmaf(bf16_hi(w), z, zsum[gi][n][1]);
+                    pb[n][h] = movmatrix_trans(w);
+                }
+#pragma unroll
+            for (int hw = 0; hw < 2; ++hw) {
+                // the two tokens of a pair side by side: units 4 g + 2 hw and 4 g + 2 hw + 1
+                uint32_t lo01, hi01, lo89, hi89;
+                if constexpr (D == 128) {
+                    lo01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x5410);
+                    hi01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x7632);
+                    lo89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x5410);
+                    hi89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x7632);
+                } else {
+                    lo01 = __byte_perm(cur.v[0][0], cur.v[1][0], hw ? 0x7632 : 0x5410);
+                    lo89 = __byte_perm(cur.v[2][0], cur.v[3][0], hw ? 0x7632 : 0x5410);
+                    hi01 = lo01 >> 8;
+                    hi89 = lo89 >> 8;
+                }
+#pragma unroll
+                for (int jj = 0; jj < PER; ++jj) {
+                    const int j = gi * PER + jj;
+                    const uint32_t eight = 0x43084308u;                      // 128 + 8
+                    const uint32_t a0 = bf16x2_sub(((lo01 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
+                    const uint32_t a1 = bf16x2_sub(((hi01 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
+                    const uint32_t a2 = bf16x2_sub(((lo89 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
+                    const uint32_t a3 = bf16x2_sub(((hi89 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                }
+            }
+        }
+        cur = nxt;
+        page = next_page;
+        next_page = page_ahead;
+    }
+
+    // sums over the lanes that share a column, then the warps' results side by side
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) {
+                l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], x);
+#pragma unroll
+                for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] += __shfl_xor_sync(0xFFFFFFFFu, zsum[gi][n][e], x);
+            }
+            const int c = n * 8 + 2 * t + e;
+            if (g == 0) {
+                s_m[warp][c] = m[n][e];
+                s_l[warp][c] = l[n][e];
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int hw = 0; hw < 2; ++hw) {
+                    const float z = zsum[j / PER][n][e];
+                    float* at = &s_o[warp][c][32 * j + 4 * g + 2 * hw];
+                    at[0] = o[j * 2 + hw][n][e] - z;
+                    at[1] = o[j * 2 + hw][n][2 + e] - z;
+                }
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < COLS * (D / 4); i += kKv4Threads) {
+        const int c = i / (D / 4), d = (i % (D / 4)) * 4, col = col0 + c;
+        if (col >= cols_all) continue;
+        float top = s_m[0][c];
+#pragma unroll
+        for (int w = 1; w < kKv4Warps; ++w) top = fmaxf(top, s_m[w][c]);
+        float sum = 0.0f;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kKv4Warps; ++w) {
+            const float f = s_m[w][c] == -INFINITY ? (s_l[w][c] != s_l[w][c] ? s_l[w][c] : 0.0f) : fast_exp2(s_m[w][c] - top);
+            sum = fmaf(f, s_l[w][c], sum);
+            const float4 x = *reinterpret_cast<const float4*>(&s_o[w][c][d]);
+            v.x = fmaf(f, x.x, v.x);
+            v.y = fmaf(f, x.y, v.y);
+            v.z = fmaf(f, x.z, v.z);
+            v.w = fmaf(f, x.w, v.w);
+        }
+        if (p.splits == 1) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;               // a row that sees no key is 0
+            const int i_pos = col / p.ratio, r = col - i_pos * p.ratio;
+            bf16* out = p.O + ((int64_t)(b * (int64_t)p.T + i_pos) * p.Hq + head * p.ratio + r) * D + d;
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+        } else {
+            float* out = p.part + ((((int64_t)b * gridDim.y + blockIdx.y) * p.splits + split) * COLS + c) * (D + 4);
+            *reinterpret_cast<float4*>(out + d) = v;
+            if (d == 0) *reinterpret_cast<float2*>(out + D) = make_float2(top, sum);
+        }
+    }
+}
+
+// Joins the splits of one query row: every warp a share of them, in a fixed order.
+template <int D, int NT>
+__global__ void __launch_bounds__(128) kv4_join_kernel(const Kv4AttnArgs p)
+{
+    constexpr int COLS = 8 * NT, V = D / 32;         // channels per lane
+    __shared__ float s_o[4][D];
+    __shared__ float s_m[4], s_l[4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row = blockIdx.x, b = row / (p.T * p.Hq), rest = row % (p.T * p.Hq), i = rest / p.Hq, h = rest % p.Hq;
+    const int head = h / p.ratio, col = i * p.ratio + h % p.ratio, ct = col / COLS, c = col % COLS;
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int len = kv4_length(p, b), keys = kv4_split_keys(len, p.splits);
+    const int used = len == 0 ? 1 : (len + keys - 1) / keys;
+    const float* base = p.part + ((((int64_t)b * p.c.n_kv_heads + head) * p.col_tiles + ct) * p.splits * COLS + c) * (D + 4);
+    const int64_t step = (int64_t)COLS * (D + 4);
+    float m = -INFINITY, l = 0.0f, v[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = 0.0f;
+#pragma unroll 4
+    for (int s = warp; s < used; s += 4) {
+        const float* x = base + s * step;
+        const float2 ml = *reinterpret_cast<const float2*>(x + D);
+        float w[V];
+        if constexpr (V == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(x + lane * 4);
+            w[0] = f.x; w[1] = f.y; w[2] = f.z; w[3] = f.w;
+        } else {
+            const float2 f = *reinterpret_cast<const float2*>(x + lane * 2);
+            w[0] = f.x; w[1] = f.y;
+        }
+        const float top = fmaxf(m, ml.x);
+        if (top == -INFINITY) {                      // nothing seen so far: 0, or a NaN that is passed on
+            l += ml.y;
+            continue;
+        }
+        const float fa = fast_exp2(m - top), fb = fast_exp2(ml.x - top);
+        l = l * fa + ml.y * fb;
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = v[k] * fa + w[k] * fb;
+        m = top;
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) s_o[warp][lane * V + k] = v[k];
+    if (lane == 0) {
+        s_m[warp] = m;
+        s_l[warp] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x < D) {
+        const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+        float sum = 0.0f, x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = top == -INFINITY ? 1.0f : fast_exp2(s_m[w] - top);
+            sum += f * s_l[w];
+            x += f * s_o[w][threadIdx.x];
+        }
+        p.O[((int64_t)(b * (int64_t)p.T + i) * p.Hq + h) * D + threadIdx.x] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : x / sum);
+    }
+}
+
+}  // namespace gmlp

@@ -1,0 +1,229 @@
+// Host side of the 4-bit weight operators: checks, launch shapes, launches.  Included by api.cu inside its namespace.
+
+struct W4Plan {
+    int nt, wr_log2, cluster, chunk, groups;
+    uint32_t smem;
+};
+
+constexpr uint32_t kW4SmemMost = 200 * 1024;
+
+// Launch shape of one product: `units` pairs of 16-column tiles, K in `KB` blocks of 128.
+W4Plan w4_plan(int M, int terms, int KB, int units, int sms) {
+    W4Plan p{};
+    p.nt = (M + 7) / 8;
+    if (p.nt == 5) p.nt = 6;
+    if (p.nt == 7) p.nt = 8;
+    const int per_sm = p.nt <= 2 ? 2 : 1, rows = M * terms;
+    const uint32_t budget = per_sm == 2 ? kW4SmemMost / 2 : kW4SmemMost, pad = (uint32_t)rows * 64u;
+    const int depth = gmlp::w4_prefetch(p.nt);       // a chunk boundary falls between rounds of the register prefetch
+    // Column groups per CTA: X costs M * terms * 256 bytes of shared memory a k-block, the codes of one group 2 KB.
+    p.wr_log2 = rows <= 2 ? 0 : (rows <= 4 ? 1 : (rows <= 16 ? 2 : 3));
+    // Fewer groups for a matrix of few columns, as long as two buffers of the shortest chunk still fit.
+    while (p.wr_log2 > 0 && (units >> p.wr_log2) == 0 &&
+           2u * ((uint32_t)depth * (uint32_t)rows * (16u >> p.wr_log2) * 256u + pad) <= budget)
+        --p.wr_log2;
+    const int WR = 1 << p.wr_log2, WK = 8 >> p.wr_log2;
+    p.groups = (units + WR - 1) / WR;
+    // K over a cluster until the GPU has its share of CTAs (two per SM for the smaller token counts), as long as each
+    // warp keeps a k-block or more.
+    p.cluster = 1;
+    while (p.cluster < 8 && p.groups * p.cluster < sms * per_sm && KB >= WK * (p.cluster + 1)) ++p.cluster;
+    const int kb_cta = (KB + p.cluster - 1) / p.cluster, steps = (kb_cta + WK - 1) / WK;
+    const uint32_t step_bytes = (uint32_t)rows * (uint32_t)WK * 256u;
+    p.chunk = steps;
+    if ((uint64_t)steps * step_bytes + pad > budget) p.chunk = (int)((budget / 2 - pad) / step_bytes) / depth * depth;
+    const uint32_t x = (p.chunk * step_bytes + pad) * (p.chunk < steps ? 2u : 1u), red = gmlp::w4_red_bytes(p.nt);
+    p.smem = x > red ? x : red;
+    return p;
+}
+
+typedef void (*W4Kernel)(gmlp::W4GemmArgs);
+template <int NT>
+W4Kernel w4_kernel_for(int G, bool gated) {
+    if (gated) return G == 32 ? gmlp::w4_gemm_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_gemm_kernel<NT, 64, true> : gmlp::w4_gemm_kernel<NT, 128, true>);
+    return G == 32 ? gmlp::w4_gemm_kernel<NT, 32, false> : (G == 64 ? gmlp::w4_gemm_kernel<NT, 64, false> : gmlp::w4_gemm_kernel<NT, 128, false>);
+}
+
+int check_w4_matrix(const gmlp_w4_matrix& w) {
+    if (w.reserved != 0) return GMLP_ERR_FLAGS;
+    if (w.group != 32 && w.group != 64 && w.group != 128) return GMLP_ERR_SHAPE;
+    if (w.K <= 0 || w.N <= 0 || w.K > kW4MaxDim || w.N > kW4MaxDim || w.K % w.group != 0) return GMLP_ERR_SHAPE;
+    if (w.codes == nullptr || w.scales == nullptr) return GMLP_ERR_NULL;
+    if (!aligned16(w.codes) || !aligned16(w.scales) || !aligned16(w.zeros)) return GMLP_ERR_ALIGN;
+    return GMLP_OK;
+}
+inline gmlp::W4Operand w4_operand(const gmlp_w4_matrix& w) {
+    return {static_cast<const uint8_t*>(w.codes), static_cast<const bf16*>(w.scales), static_cast<const uint8_t*>(w.zeros)};
+}
+
+// One launch chained to its predecessor by programmatic dependent launch.
+template <typename... P, typename... A>
+int launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, uint32_t smem, int cluster, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) return GMLP_ERR_LAUNCH;
+    GMLP_CHECK_LAUNCH();
+    return GMLP_OK;
+}
+
+int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_matrix* w1, const bf16* X, int terms, bf16* out,
+                   int64_t M, gmlp::GateAct act, bool early, cudaStream_t st) {
+    const int K = (int)w0.K, N = (int)w0.N, KB = (K + 127) / 128, n16 = (N + 15) / 16;
+    const bool gated = w1 != nullptr;
+    const W4Plan p = w4_plan((int)M, terms, KB, gated ? n16 : (n16 + 1) / 2, dev->sm_count);
+    if (p.chunk < 1 || p.smem > kW4SmemMost) return GMLP_ERR_UNSUPPORTED;       // w4_plan yields no such shape
+    W4Kernel kernel;
+    switch (p.nt) {
+        case 1: kernel = w4_kernel_for<1>(w0.group, gated); break;
+        case 2: kernel = w4_kernel_for<2>(w0.group, gated); break;
+        case 3: kernel = w4_kernel_for<3>(w0.group, gated); break;
+        case 4: kernel = w4_kernel_for<4>(w0.group, gated); break;
+        case 6: kernel = w4_kernel_for<6>(w0.group, gated); break;
+        default: kernel = w4_kernel_for<8>(w0.group, gated); break;
+    }
+    const int slot = (p.nt - 1) * 6 + (gated ? 3 : 0) + (w0.group == 32 ? 0 : (w0.group == 64 ? 1 : 2));
+    if (!dev->w4_attr_set[slot]) {
+        if (cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kW4SmemMost) != cudaSuccess)
+            return GMLP_ERR_LAUNCH;
+        dev->w4_attr_set[slot] = true;
+    }
+    gmlp::W4GemmArgs a{};
+    a.w[0] = w4_operand(w0);
+    a.w[1] = gated ? w4_operand(*w1) : a.w[0];
+    a.X = X;
+    a.out = out;
+    a.M = (int)M;
+    a.K = K;
+    a.N = N;
+    a.KB = KB;
+    a.n16 = n16;
+    a.terms = terms;
+    a.wr_log2 = p.wr_log2;
+    a.cluster = p.cluster;
+    a.chunk = p.chunk;
+    a.early = early ? 1 : 0;
+    a.act = act;
+    return launch_chained(kernel, dim3((unsigned)(p.groups * p.cluster)), gmlp::kW4Threads, p.smem, p.cluster, st, a);
+}
+
+int finish_checked(uint32_t flags, cudaStream_t st) {
+    if (!(flags & GMLP_FLAG_CHECKED)) return GMLP_OK;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
+    const int s = read_device_status();
+    if (s < 0) return s;
+    if ((s >> 16) == gmlp::kIndexStatus) return GMLP_ERR_INDEX;
+    return s != 0 ? GMLP_ERR_TIMEOUT : GMLP_OK;
+}
+
+int w4_matmul_impl(const gmlp_w4_matmul_args* a) {
+    if (a == nullptr) return GMLP_ERR_NULL;
+    if (a->struct_bytes != sizeof(gmlp_w4_matmul_args) || (a->flags & ~(uint32_t)GMLP_FLAG_CHECKED)) return GMLP_ERR_FLAGS;
+    int rc = check_w4_matrix(a->W);
+    if (rc != GMLP_OK) return rc;
+    if (a->M < 0 || a->M > gmlp::kW4MaxM) return GMLP_ERR_SHAPE;
+    if (a->M == 0) return GMLP_OK;
+    if (!a->X || !a->Y) return GMLP_ERR_NULL;
+    if (!aligned16(a->X) || !aligned16(a->Y)) return GMLP_ERR_ALIGN;
+    DeviceState* dev = current_device(&rc);
+    if (dev == nullptr) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(a->stream);
+    prof_begin(st);
+    rc = launch_w4_gemm(dev, a->W, nullptr, static_cast<const bf16*>(a->X), 1, static_cast<bf16*>(a->Y), a->M, kSilu, false, st);
+    if (rc != GMLP_OK) return rc;
+    prof_mark("w4_matmul", st);
+    return finish_checked(a->flags, st);
+}
+
+uint64_t w4_forward_workspace(int64_t M, int64_t d_model, int64_t d_ff, uint32_t flags) {
+    if (M < 0 || M > gmlp::kW4MaxM || d_model <= 0 || d_ff <= 0 || d_model > kW4MaxDim || d_ff > kW4MaxDim) return 0;
+    const uint64_t xn = (flags & GMLP_FLAG_RMSNORM) ? align256((uint64_t)M * d_model * 4) : 0;
+    return xn + align256((uint64_t)M * d_ff * 4);
+}
+
+int w4_forward_impl(const gmlp_w4_args* a) {
+    if (a == nullptr) return GMLP_ERR_NULL;
+    const uint32_t known = GMLP_FLAG_CHECKED | GMLP_FLAG_RMSNORM | GMLP_FLAG_ACT_SWISH | GMLP_FLAG_ACT_GLU | GMLP_FLAG_ACT_GELU;
+    if (a->struct_bytes != sizeof(gmlp_w4_args) || (a->flags & ~known) || a->reserved != 0) return GMLP_ERR_FLAGS;
+    gmlp::GateAct act;
+    if (!gate_act_from(a->flags, a->act_beta, &act)) return GMLP_ERR_FLAGS;
+    int rc = GMLP_OK;
+    for (const gmlp_w4_matrix* w : {&a->Wg, &a->Wu, &a->Wd}) {
+        rc = check_w4_matrix(*w);
+        if (rc != GMLP_OK) return rc;
+    }
+    const int64_t d_model = a->Wg.K, d_ff = a->Wg.N;
+    if (a->Wu.K != d_model || a->Wu.N != d_ff || a->Wd.K != d_ff || a->Wd.N != d_model || a->Wu.group != a->Wg.group ||
+        (a->Wu.zeros == nullptr) != (a->Wg.zeros == nullptr) || a->M < 0 || a->M > gmlp::kW4MaxM)
+        return GMLP_ERR_SHAPE;
+    if (a->M == 0) return GMLP_OK;
+    if (!a->X || !a->Y || !a->workspace) return GMLP_ERR_NULL;
+    if (!aligned16(a->X) || !aligned16(a->Y) || !aligned16(a->rms_gain)) return GMLP_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return GMLP_ERR_ALIGN;
+    if (a->workspace_bytes < w4_forward_workspace(a->M, d_model, d_ff, a->flags)) return GMLP_ERR_WORKSPACE;
+    DeviceState* dev = current_device(&rc);
+    if (dev == nullptr) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(a->stream);
+    uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+    const bool norm = (a->flags & GMLP_FLAG_RMSNORM) != 0;
+    claim_workspace(dev, ws, w4_forward_workspace(a->M, d_model, d_ff, a->flags), nullptr, 0);
+    bf16* Xn = reinterpret_cast<bf16*>(ws);
+    bf16* H = reinterpret_cast<bf16*>(ws + (norm ? align256((uint64_t)a->M * d_model * 4) : 0));
+    const bf16* X = static_cast<const bf16*>(a->X);
+    prof_begin(st);
+    if (norm) {
+        rc = launch_chained(gmlp::w4_norm_kernel, dim3((unsigned)a->M), gmlp::kRmsThreads, 0, 1, st, X,
+                            static_cast<const bf16*>(a->rms_gain), Xn, (int)a->M, (int)d_model, a->rms_eps);
+        if (rc != GMLP_OK) return rc;
+        prof_mark("w4_norm", st);
+    }
+    // the call's first kernel waits for everything before the call; later kernels may fetch their weights at once
+    rc = launch_w4_gemm(dev, a->Wg, &a->Wu, norm ? Xn : X, norm ? 2 : 1, H, a->M, act, norm, st);
+    if (rc != GMLP_OK) return rc;
+    prof_mark("w4_gate_up", st);
+    rc = launch_w4_gemm(dev, a->Wd, nullptr, H, 2, static_cast<bf16*>(a->Y), a->M, kSilu, true, st);
+    if (rc != GMLP_OK) return rc;
+    prof_mark("w4_down", st);
+    return finish_checked(a->flags, st);
+}
+
+// kind: gmlp::kW4From* to pack, -1 to unpack
+int w4_layout_impl(const gmlp_w4_layout_args* a, int kind) {
+    if (a == nullptr) return GMLP_ERR_NULL;
+    if (a->struct_bytes != sizeof(gmlp_w4_layout_args) || (a->flags & ~(uint32_t)(GMLP_FLAG_CHECKED | GMLP_FLAG_WEIGHTS_OUT_IN)))
+        return GMLP_ERR_FLAGS;
+    int rc = check_w4_matrix(a->m);
+    if (rc != GMLP_OK) return rc;
+    if (!a->W || (kind == gmlp::kW4FromCodes && (!a->scales || (a->zeros == nullptr) != (a->m.zeros == nullptr)))) return GMLP_ERR_NULL;
+    DeviceState* dev = current_device(&rc);
+    if (dev == nullptr) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(a->stream);
+    const int K = (int)a->m.K, N = (int)a->m.N, G = a->m.group, out_in = (a->flags & GMLP_FLAG_WEIGHTS_OUT_IN) ? 1 : 0;
+    const dim3 grid((unsigned)(((N + 15) / 16 * 16 + 127) / 128), (unsigned)((K + 127) / 128));
+    uint8_t* codes = static_cast<uint8_t*>(const_cast<void*>(a->m.codes));
+    bf16* scales = static_cast<bf16*>(const_cast<void*>(a->m.scales));
+    uint8_t* zeros = static_cast<uint8_t*>(const_cast<void*>(a->m.zeros));
+    const bf16* s_in = static_cast<const bf16*>(a->scales);
+    const uint8_t* z_in = static_cast<const uint8_t*>(a->zeros);
+    if (kind < 0)
+        rc = launch_chained(gmlp::w4_unpack_kernel, grid, 128, 0, 1, st, codes, scales, zeros, static_cast<bf16*>(a->W), out_in, K, N, G);
+    else if (kind == gmlp::kW4FromCodes)
+        rc = launch_chained(gmlp::w4_pack_kernel<gmlp::kW4FromCodes>, grid, 128, 0, 1, st, a->W, out_in, s_in, z_in, codes, scales, zeros, K, N, G);
+    else if (zeros == nullptr)
+        rc = launch_chained(gmlp::w4_pack_kernel<gmlp::kW4FromBf16>, grid, 128, 0, 1, st, a->W, out_in, s_in, z_in, codes, scales, zeros, K, N, G);
+    else
+        rc = launch_chained(gmlp::w4_pack_kernel<gmlp::kW4FromBf16Zeros>, grid, 128, 0, 1, st, a->W, out_in, s_in, z_in, codes, scales, zeros, K, N, G);
+    if (rc != GMLP_OK) return rc;
+    return finish_checked(a->flags, st);
+}

@@ -16,6 +16,7 @@ OK = 0
 ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_FLAGS, ERR_WORKSPACE, ERR_ARCH, ERR_LAUNCH, ERR_TIMEOUT, ERR_UNSUPPORTED = \
     -1, -2, -3, -4, -5, -6, -7, -8, -9
 ERR_STATIC_LIMIT = -10
+ERR_INDEX = -11
 STATIC_MAX_M = 16
 STATIC_SCRATCH_BYTES = 12 << 20
 FLAG_RMSNORM = 1 << 0
@@ -92,6 +93,72 @@ class GmlpMmAddNormArgs(ctypes.Structure):
     ]
 
 
+W4_MAX_M = 64
+KV4_MAX_QUERIES = 16
+
+
+class GmlpW4Matrix(ctypes.Structure):
+    _fields_ = [
+        ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
+        ("K", ctypes.c_int64), ("N", ctypes.c_int64), ("group", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class GmlpW4LayoutArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("W", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
+        ("m", GmlpW4Matrix), ("stream", ctypes.c_void_p),
+    ]
+
+
+class GmlpW4MatmulArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("X", ctypes.c_void_p), ("Y", ctypes.c_void_p), ("M", ctypes.c_int64),
+        ("W", GmlpW4Matrix), ("stream", ctypes.c_void_p),
+    ]
+
+
+class GmlpW4Args(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("X", ctypes.c_void_p), ("Y", ctypes.c_void_p), ("M", ctypes.c_int64),
+        ("Wg", GmlpW4Matrix), ("Wu", GmlpW4Matrix), ("Wd", GmlpW4Matrix),
+        ("rms_gain", ctypes.c_void_p), ("rms_eps", ctypes.c_float), ("act_beta", ctypes.c_float),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+        ("reserved", ctypes.c_uint64),
+    ]
+
+
+class GmlpKv4Cache(ctypes.Structure):
+    _fields_ = [
+        ("k_codes", ctypes.c_void_p), ("k_params", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_params", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64),
+        ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("group", ctypes.c_int32),
+        ("reserved", ctypes.c_int64),
+    ]
+
+
+class GmlpKv4RowsArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("T", ctypes.c_int64),
+        ("cache", GmlpKv4Cache), ("stream", ctypes.c_void_p),
+    ]
+
+
+class GmlpKv4AttentionArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("Q", ctypes.c_void_p), ("O", ctypes.c_void_p), ("cache", GmlpKv4Cache),
+        ("block_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+        ("B", ctypes.c_int64), ("table_width", ctypes.c_int64),
+        ("n_q_heads", ctypes.c_int32), ("q_len", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
 class GmlpError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -127,6 +194,21 @@ def lib() -> ctypes.CDLL:
         L.gmlp_gqa_attention.argtypes = [ctypes.POINTER(GmlpGqaArgs)]
         L.gmlp_qkv_proj.restype = ctypes.c_int
         L.gmlp_qkv_proj.argtypes = [ctypes.POINTER(GmlpQkvArgs)]
+        for name, args in (("w4_quantize", GmlpW4LayoutArgs), ("w4_pack", GmlpW4LayoutArgs), ("w4_dequantize", GmlpW4LayoutArgs),
+                           ("w4_matmul", GmlpW4MatmulArgs), ("w4_forward", GmlpW4Args), ("kv4_append", GmlpKv4RowsArgs),
+                           ("kv4_gather", GmlpKv4RowsArgs), ("kv4_attention", GmlpKv4AttentionArgs)):
+            f = getattr(L, "gmlp_" + name)
+            f.restype, f.argtypes = ctypes.c_int, [ctypes.POINTER(args)]
+        L.gmlp_w4_code_bytes.restype = u64
+        L.gmlp_w4_code_bytes.argtypes = [i64, i64]
+        L.gmlp_w4_scale_count.restype = u64
+        L.gmlp_w4_scale_count.argtypes = [i64, i64, i32]
+        L.gmlp_w4_workspace_bytes.restype = u64
+        L.gmlp_w4_workspace_bytes.argtypes = [i64, i64, i64, u32]
+        L.gmlp_w4_plan.restype = ctypes.c_int
+        L.gmlp_w4_plan.argtypes = [i64, i32, i64, i64, i32, i32, ctypes.POINTER(i32)]
+        L.gmlp_kv4_workspace_bytes.restype = u64
+        L.gmlp_kv4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
         L.gmlp_autotune.restype = ctypes.c_int
         L.gmlp_autotune.argtypes = [ctypes.POINTER(GmlpArgs), ctypes.c_int, ctypes.POINTER(ctypes.c_int32),
                                     ctypes.POINTER(ctypes.c_float)]
@@ -600,3 +682,292 @@ def sum_partials(parts, Y=None, stream=None) -> "torch.Tensor":
     if rc != OK:
         raise GmlpError(rc)
     return Y
+
+
+# ---------------------------------------------------------------------------------------------- 4-bit weights and cache
+
+def _on_one_device(device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+
+
+def _check_tensor(t, name: str, dtype, shape) -> None:
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise TypeError(f"{name}: expected a contiguous CUDA {dtype} tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _run(entry, args, device) -> None:
+    """One library call with `device` current."""
+    if torch.cuda.current_device() == device.index:
+        rc = entry(ctypes.byref(args))
+    else:
+        with torch.cuda.device(device):
+            rc = entry(ctypes.byref(args))
+    if rc != OK:
+        raise GmlpError(rc)
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on `stream`: from that stream's pool, so that it is not handed out again while the call runs."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _stream_handle(stream, device) -> int:
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+class W4Matrix:
+    """A [K, N] weight matrix in 4 bits (gmlp_w4_matrix): made by w4_quantize or w4_pack, used by the w4_* operators.
+
+    ``codes``, ``scales``, ``zeros`` (None: every zero point is 8) hold the library's tiles; treat them as opaque.  To
+    reload a saved matrix, construct it from them."""
+    __slots__ = ("codes", "scales", "zeros", "K", "N", "group", "device", "struct")
+
+    def __init__(self, codes, scales, zeros, K: int, N: int, group: int):
+        n_codes, n_scales = w4_sizes(K, N, group)
+        _check_tensor(codes, "codes", torch.uint8, (n_codes,))
+        _check_tensor(scales, "scales", torch.bfloat16, (n_scales,))
+        if zeros is not None:
+            _check_tensor(zeros, "zeros", torch.uint8, (n_scales,))
+        _on_one_device(codes.device, scales=scales, zeros=zeros)
+        self.codes, self.scales, self.zeros, self.K, self.N, self.group = codes, scales, zeros, K, N, group
+        self.device = codes.device
+        self.struct = GmlpW4Matrix(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), K, N, group, 0)
+
+
+def w4_sizes(K: int, N: int, group: int):
+    """(bytes of codes, number of scales) of a 4-bit [K, N] matrix; raises GmlpError for sizes the library does not take."""
+    n_codes = int(lib().gmlp_w4_code_bytes(K, N))
+    n_scales = int(lib().gmlp_w4_scale_count(K, N, group))
+    if n_codes == 0 or n_scales == 0 or K % group != 0:
+        raise GmlpError(ERR_SHAPE)
+    return n_codes, n_scales
+
+
+def _w4_empty(K: int, N: int, group: int, zeros: bool, device, stream) -> W4Matrix:
+    n_codes, n_scales = w4_sizes(K, N, group)
+    return W4Matrix(_empty(n_codes, torch.uint8, device, stream), _empty(n_scales, torch.bfloat16, device, stream),
+                    _empty(n_scales, torch.uint8, device, stream) if zeros else None, K, N, group)
+
+
+def _w4_layout(entry, W, scales, zeros, m: W4Matrix, weights_out_in: bool, stream, checked: bool) -> None:
+    a = GmlpW4LayoutArgs(ctypes.sizeof(GmlpW4LayoutArgs), (FLAG_CHECKED if checked else 0) | (FLAG_WEIGHTS_OUT_IN if weights_out_in else 0),
+                         W.data_ptr(), None if scales is None else scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
+                         m.struct, _stream_handle(stream, m.device))
+    _run(entry, a, m.device)
+
+
+def w4_quantize(W, group: int = 128, zero_points: bool = False, weights_out_in: bool = False, stream=None,
+                checked: bool = False) -> W4Matrix:
+    """gmlp_w4_quantize: a bf16 matrix [K, N] (``weights_out_in``: [N, K]) in 4 bits, one scale (and with ``zero_points`` one
+    zero point) per ``group`` input rows and output column."""
+    _check_bf16_cuda(W, "W")
+    if W.dim() != 2:
+        raise ValueError("W: expected a matrix")
+    K, N = (W.shape[1], W.shape[0]) if weights_out_in else W.shape
+    m = _w4_empty(K, N, group, zero_points, W.device, stream)
+    _w4_layout(lib().gmlp_w4_quantize, W, None, None, m, weights_out_in, stream, checked)
+    return m
+
+
+def w4_pack(codes, scales, zeros=None, weights_out_in: bool = False, stream=None, checked: bool = False) -> W4Matrix:
+    """gmlp_w4_pack: codes (uint8 [K, N], one per byte), scales (bf16 [K / group, N]) and zero points (uint8, the scales'
+    shape, or None: 8) of a matrix that was quantised elsewhere; with ``weights_out_in`` all three transposed."""
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes and scales: expected matrices")
+    axis = 1 if weights_out_in else 0
+    K, N = codes.shape[axis], codes.shape[1 - axis]
+    groups = scales.shape[axis]
+    if groups < 1 or K % groups != 0:
+        raise ValueError("shape mismatch: the number of scales must divide the number of input rows")
+    _check_tensor(codes, "codes", torch.uint8, (N, K) if weights_out_in else (K, N))
+    _check_tensor(scales, "scales", torch.bfloat16, (N, groups) if weights_out_in else (groups, N))
+    if zeros is not None:
+        _check_tensor(zeros, "zeros", torch.uint8, scales.shape)
+    _on_one_device(codes.device, scales=scales, zeros=zeros)
+    m = _w4_empty(K, N, K // groups, zeros is not None, codes.device, stream)
+    _w4_layout(lib().gmlp_w4_pack, codes, scales, zeros, m, weights_out_in, stream, checked)
+    return m
+
+
+def w4_dequantize(W4: W4Matrix, weights_out_in: bool = False, W=None, stream=None, checked: bool = False) -> torch.Tensor:
+    """gmlp_w4_dequantize: the bf16 matrix [K, N] ([N, K] with ``weights_out_in``), e.g. for gmlp.forward over a prompt."""
+    shape = (W4.N, W4.K) if weights_out_in else (W4.K, W4.N)
+    if W is None:
+        W = _empty(shape, torch.bfloat16, W4.device, stream)
+    _check_tensor(W, "W", torch.bfloat16, shape)
+    _on_one_device(W4.device, W=W)
+    _w4_layout(lib().gmlp_w4_dequantize, W, None, None, W4, weights_out_in, stream, checked)
+    return W
+
+
+def w4_matmul(X, W4: W4Matrix, Y=None, stream=None, checked: bool = False) -> torch.Tensor:
+    """gmlp_w4_matmul: Y = X W for a 4-bit W and up to W4_MAX_M rows of X."""
+    if X.dim() != 2:
+        raise ValueError("X: expected a matrix")
+    M = X.shape[0]
+    _check_tensor(X, "X", torch.bfloat16, (M, W4.K))
+    if Y is None:
+        Y = _empty((M, W4.N), torch.bfloat16, X.device, stream)
+    else:
+        _check_tensor(Y, "Y", torch.bfloat16, (M, W4.N))
+    _on_one_device(W4.device, X=X, Y=Y)
+    a = GmlpW4MatmulArgs(ctypes.sizeof(GmlpW4MatmulArgs), FLAG_CHECKED if checked else 0, X.data_ptr(), Y.data_ptr(), M, W4.struct,
+                         _stream_handle(stream, X.device))
+    _run(lib().gmlp_w4_matmul, a, W4.device)
+    return Y
+
+
+def w4_plan(M: int, K: int, N: int, terms: int = 1, gated: bool = False, sm_count: int = 0):
+    """gmlp_w4_plan: (columns of eight tokens, column groups per CTA, CTAs per cluster, steps per chunk, steps, bytes of shared
+    memory, CTAs) of one product."""
+    out = (ctypes.c_int32 * 7)()
+    rc = lib().gmlp_w4_plan(M, terms, K, N, int(gated), sm_count, out)
+    if rc != OK:
+        raise GmlpError(rc)
+    return tuple(out)
+
+
+def w4_workspace_bytes(M: int, d_model: int, d_ff: int, rmsnorm: bool = False) -> int:
+    return int(lib().gmlp_w4_workspace_bytes(M, d_model, d_ff, FLAG_RMSNORM if rmsnorm else 0))
+
+
+def w4_forward(X, Wg: W4Matrix, Wu: W4Matrix, Wd: W4Matrix, Y=None, gamma=None, eps: float = 1e-5, rmsnorm: bool = False,
+               workspace=None, stream=None, checked: bool = False, act: str = "silu", beta: float = 1.0) -> torch.Tensor:
+    """gmlp_w4_forward: Y = (act(Xn Wg) * (Xn Wu)) Wd on 4-bit weights, up to W4_MAX_M rows of X; the options are those of
+    forward().  ``workspace``: a uint8 tensor of at least w4_workspace_bytes(), by default allocated for the call."""
+    if X.dim() != 2:
+        raise ValueError("X: expected a matrix")
+    M = X.shape[0]
+    _check_tensor(X, "X", torch.bfloat16, (M, Wg.K))
+    if Y is None:
+        Y = _empty((M, Wg.K), torch.bfloat16, X.device, stream)
+    else:
+        _check_tensor(Y, "Y", torch.bfloat16, (M, Wg.K))
+    if gamma is not None:
+        _check_tensor(gamma, "gamma", torch.bfloat16, (Wg.K,))
+    if workspace is None:
+        workspace = _empty(max(256, w4_workspace_bytes(M, Wg.K, Wg.N, rmsnorm)), torch.uint8, X.device, stream)
+    _on_one_device(X.device, Y=Y, gamma=gamma, workspace=workspace, Wg=Wg, Wu=Wu, Wd=Wd)
+    a = GmlpW4Args(ctypes.sizeof(GmlpW4Args), (FLAG_RMSNORM if rmsnorm else 0) | (FLAG_CHECKED if checked else 0) | ACT_FLAGS[act],
+                   X.data_ptr(), Y.data_ptr(), M, Wg.struct, Wu.struct, Wd.struct, None if gamma is None else gamma.data_ptr(),
+                   eps, beta, _stream_handle(stream, X.device), workspace.data_ptr(), workspace.numel() * workspace.element_size(), 0)
+    _run(lib().gmlp_w4_forward, a, X.device)
+    return Y
+
+
+class Kv4Cache:
+    """A paged key/value cache in 4 bits (gmlp_kv4_cache): codes uint8 [n_pages, n_kv_heads, page_size, head_dim / 2] and
+    parameters bf16 [n_pages, n_kv_heads, page_size, head_dim / group, 2] for keys and for values."""
+    __slots__ = ("k_codes", "k_params", "v_codes", "v_params", "n_pages", "n_kv_heads", "page_size", "head_dim", "group", "device",
+                 "struct")
+
+    def __init__(self, k_codes, k_params, v_codes, v_params):
+        if k_codes.dim() != 4 or k_params.dim() != 5 or k_params.shape[3] < 1:
+            raise ValueError("expected codes [n_pages, n_kv_heads, page_size, head_dim / 2] and parameters "
+                             "[n_pages, n_kv_heads, page_size, head_dim / group, 2]")
+        n_pages, heads, page, half = k_codes.shape
+        groups = k_params.shape[3]
+        for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
+            _check_tensor(t, name, torch.uint8, (n_pages, heads, page, half))
+        for t, name in ((k_params, "k_params"), (v_params, "v_params")):
+            _check_tensor(t, name, torch.bfloat16, (n_pages, heads, page, groups, 2))
+        _on_one_device(k_codes.device, k_params=k_params, v_codes=v_codes, v_params=v_params)
+        if 2 * half % groups != 0:
+            raise ValueError("the number of groups must divide head_dim")
+        self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim, self.group = n_pages, heads, page, 2 * half, 2 * half // groups
+        self.device = k_codes.device
+        self.struct = GmlpKv4Cache(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(), n_pages, heads,
+                                   page, self.head_dim, self.group, 0)
+
+
+def kv4_cache(n_pages: int, n_kv_heads: int, head_dim: int = 128, page_size: int = 64, group: int = 64, device="cuda") -> Kv4Cache:
+    """An empty cache (all rows stand for zeros)."""
+    codes = lambda: torch.zeros(n_pages, n_kv_heads, page_size, head_dim // 2, dtype=torch.uint8, device=device)
+    params = lambda: torch.zeros(n_pages, n_kv_heads, page_size, head_dim // group, 2, dtype=torch.bfloat16, device=device)
+    return Kv4Cache(codes(), params(), codes(), params())
+
+
+def _kv4_rows(entry, K, V, cache: Kv4Cache, slots, stream, checked: bool) -> None:
+    T = slots.shape[0]
+    _check_tensor(slots, "slots", torch.int64, (T,))
+    for t, name in ((K, "K"), (V, "V")):
+        _check_tensor(t, name, torch.bfloat16, (T, cache.n_kv_heads * cache.head_dim))
+    _on_one_device(cache.device, K=K, V=V, slots=slots)
+    a = GmlpKv4RowsArgs(ctypes.sizeof(GmlpKv4RowsArgs), FLAG_CHECKED if checked else 0, K.data_ptr(), V.data_ptr(), slots.data_ptr(), T,
+                        cache.struct, _stream_handle(stream, cache.device))
+    _run(entry, a, cache.device)
+
+
+def kv4_append(K, V, cache: Kv4Cache, slots, stream=None, checked: bool = False) -> None:
+    """gmlp_kv4_append: rows of K and V [T, n_kv_heads * head_dim] into the cache at ``slots`` (int64, all different; negative:
+    the row is skipped)."""
+    if slots.dim() != 1:
+        raise ValueError("slots: expected a vector")
+    _kv4_rows(lib().gmlp_kv4_append, K, V, cache, slots, stream, checked)
+
+
+def kv4_gather(cache: Kv4Cache, slots, K=None, V=None, stream=None, checked: bool = False):
+    """gmlp_kv4_gather: the rows at ``slots`` as bf16 (K, V), each [T, n_kv_heads * head_dim]."""
+    if slots.dim() != 1:
+        raise ValueError("slots: expected a vector")
+    shape = (slots.shape[0], cache.n_kv_heads * cache.head_dim)
+    if K is None:
+        K = _empty(shape, torch.bfloat16, cache.device, stream)
+    if V is None:
+        V = _empty(shape, torch.bfloat16, cache.device, stream)
+    _kv4_rows(lib().gmlp_kv4_gather, K, V, cache, slots, stream, checked)
+    return K, V
+
+
+def kv4_workspace_bytes(B: int, q_len: int, n_q_heads: int, n_kv_heads: int, head_dim: int, table_width: int, page_size: int,
+                        sm_count: int = 0) -> int:
+    return int(lib().gmlp_kv4_workspace_bytes(B, q_len, n_q_heads, n_kv_heads, head_dim, table_width, page_size, sm_count))
+
+
+def kv4_attention(Q, cache: Kv4Cache, block_table, lengths, n_q_heads: int, q_len: int = 1, scale: Optional[float] = None, O=None,
+                  workspace=None, stream=None, checked: bool = False) -> torch.Tensor:
+    """gmlp_kv4_attention: the newest ``q_len`` positions of B requests, Q [B * q_len, n_q_heads * head_dim], over the cache;
+    ``block_table`` int32 [B, pages], ``lengths`` int32 [B] (keys of each request, the new ones included); ``scale`` defaults to
+    1 / sqrt(head_dim)."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected a matrix")
+    B, width = block_table.shape
+    shape = (B * q_len, n_q_heads * cache.head_dim)
+    _check_tensor(Q, "Q", torch.bfloat16, shape)
+    _check_tensor(block_table, "block_table", torch.int32, (B, width))
+    _check_tensor(lengths, "lengths", torch.int32, (B,))
+    if O is None:
+        O = _empty(shape, torch.bfloat16, cache.device, stream)
+    else:
+        _check_tensor(O, "O", torch.bfloat16, shape)
+    if workspace is None:
+        n = kv4_workspace_bytes(B, q_len, n_q_heads, cache.n_kv_heads, cache.head_dim, width, cache.page_size, _sm_count(cache.device))
+        if n:
+            workspace = _empty(n, torch.uint8, cache.device, stream)
+    _on_one_device(cache.device, Q=Q, block_table=block_table, lengths=lengths, O=O, workspace=workspace)
+    a = GmlpKv4AttentionArgs(ctypes.sizeof(GmlpKv4AttentionArgs), FLAG_CHECKED if checked else 0, Q.data_ptr(), O.data_ptr(),
+                             cache.struct, block_table.data_ptr(), lengths.data_ptr(), B, width, n_q_heads, q_len,
+                             cache.head_dim ** -0.5 if scale is None else scale, 0, _stream_handle(stream, cache.device),
+                             None if workspace is None else workspace.data_ptr(),
+                             0 if workspace is None else workspace.numel() * workspace.element_size())
+    _run(lib().gmlp_kv4_attention, a, cache.device)
+    return O
+
+
+_sm_counts: dict = {}
+
+
+def _sm_count(device) -> int:
+    """Multiprocessors of a device (a fixed property, asked once)."""
+    n = _sm_counts.get(device.index)
+    if n is None:
+        n = _sm_counts[device.index] = torch.cuda.get_device_properties(device).multi_processor_count
+    return n

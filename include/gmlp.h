@@ -295,7 +295,7 @@ int gmlp_gqa_attention(const gmlp_gqa_args* args);
  *                       q = clamp(rint(w / s) + z, 0, 15).  A scale of 0 makes the group 0; a group with an infinity or a NaN
  *                       (or a range past float's) becomes NaN throughout.
  *     gmlp_w4_pack      from codes (one byte each, low four bits), scales and zero points that some other tool made.
- * Their order is the library's own (tiles of 16 columns by 128 rows); gmlp_w4_dequantize writes the bf16 matrix back, e.g. for a
+ * Their order is the library's own (tiles of 16 columns by 128 rows, K padded to 256); gmlp_w4_dequantize writes the bf16 matrix back, e.g. for a
  * prompt's gmlp_forward (rounded once; pass GMLP_FLAG_WEIGHTS_IN_STREAM_ORDER to a gmlp_forward that follows on the stream).
  * K must be a multiple of `group`; N is any positive number; both at most 2^20.
  */
@@ -340,10 +340,11 @@ typedef struct gmlp_w4_matmul_args {
 } gmlp_w4_matmul_args;
 int gmlp_w4_matmul(const gmlp_w4_matmul_args* args);
 /* How a product of M tokens (terms = 1 for bf16 input, 2 for the two-term inputs inside gmlp_w4_forward) with a [K, N] matrix (gated:
- * with two of them) is launched on a device with `sm_count` SMs (0: the current device, 148 if there is none): plan[0] = columns of
- * eight tokens, [1] = column groups per CTA (32 columns each; gated: 16), [2] = CTAs per cluster (K is split over them), [3] = steps of
- * K per chunk of X in shared memory, [4] = steps in all, [5] = bytes of shared memory, [6] = CTAs.  Pure host arithmetic. */
-int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t sm_count, int32_t plan[7]);
+ * with two of them) is launched on a device with `sm_count` SMs (0: the current device, 148 if there is none): plan[0] = 1 for the
+ * persistent kernel, 0 for the tile kernel, [1] = columns of eight rows of X (rows are tokens times terms) per CTA, [2] = warps
+ * of a team (persistent kernel), [3] = groups of two column tiles per CTA (tile kernel), [4] = CTAs per cluster (K is split over them), [5] =
+ * parts the tokens are cut into, [6] = CTAs per part, [7] = bytes of shared memory per CTA.  Pure host arithmetic. */
+int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t group, int32_t sm_count, int32_t plan[8]);
 
 /*
  * The Gated MLP on 4-bit weights: Y = (act(Xn Wg) (.) (Xn Wu)) Wd with Wg, Wu [d_model, d_ff] and Wd [d_ff, d_model] as

@@ -13,6 +13,12 @@
 
 namespace gmlp {
 
+// The nibbles at bit `shift` (0, 4, 8, 12) of both halves of a word as bf16 16 + q (the nibble in the upper four mantissa bits).  The
+// lowest one comes up by a multiplication: on another pipe than the shifts, whose pipe is the busier.
+__device__ __forceinline__ uint32_t kv4_codes_plus_16(uint32_t w, int shift) {
+    return and_or(shift == 0 ? w * 8u : w >> (shift - 3), 0x00780078u, 0x41804180u);
+}
+
 struct Kv4Cache {
     uint8_t* codes[2];         // K, V
     uint32_t* params[2];       // bf16 pairs: scale in the low half, zero point in the high half
@@ -87,7 +93,7 @@ kv4_append_kernel(const bf16* K, const bf16* V, const Kv4Cache c, const int64_t*
             unit |= (uint32_t)q << (4 * (gi * PER + j));
         }
     }
-    uint8_t* codes = c.codes[which] + row * (D / 2);
+    uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + row * (D / 2);
     if constexpr (D == 128) reinterpret_cast<uint16_t*>(codes)[lane] = (uint16_t)unit;
     else codes[lane] = (uint8_t)unit;
     if (lane < NG) {
@@ -95,7 +101,7 @@ kv4_append_kernel(const bf16* K, const bf16* V, const Kv4Cache c, const int64_t*
 #pragma unroll
         for (int gi = 1; gi < NG; ++gi)
             if (lane == gi) mine = par[gi];
-        c.params[which][row * NG + lane] = mine;
+        (which ? c.params[1] : c.params[0])[row * NG + lane] = mine;
     }
 }
 
@@ -125,7 +131,7 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
     const uint32_t page = (uint32_t)slot / (uint32_t)c.page_size;
     const int64_t row = ((int64_t)page * c.n_kv_heads + head) * c.page_size + ((uint32_t)slot - page * (uint32_t)c.page_size);
     uint32_t w[D / 32], par[NG];
-    const uint8_t* codes = c.codes[which] + row * (D / 2) + t * (D / 8);
+    const uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + row * (D / 2) + t * (D / 8);
     if constexpr (D == 128) {
         const uint4 u = *reinterpret_cast<const uint4*>(codes);
         w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
@@ -134,7 +140,7 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
         w[0] = u.x; w[1] = u.y;
     }
 #pragma unroll
-    for (int gi = 0; gi < NG; ++gi) par[gi] = c.params[which][row * NG + gi];
+    for (int gi = 0; gi < NG; ++gi) par[gi] = (which ? c.params[1] : c.params[0])[row * NG + gi];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const float s = bf16_lo(par[j * 32 / G]), z = bf16_hi(par[j * 32 / G]);
@@ -159,13 +165,17 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 // T new positions per request (the last T of its sequence), O = softmax(scale * Q K^T) V over the keys up to each position's
 // own.  A CTA takes one request, one key/value head, up to 8 NT of its T * (query heads per key/value head) query rows and a range
 // of the keys; its four warps take 16-token tiles in turn.  Per tile and warp (flash-style, running maximum and sum in fp32):
-//   S^T = K Q^T   tokens are the 16 mma rows, query rows the 8 columns, (q - z) exact in bf16; the token's scale is a row
-//                 factor in fp32, per group of channels;
+//   S^T = K Q^T   tokens are the 16 mma rows, query rows the 8 columns, 16 + q exact in bf16; (16 + z) times the query row's sum
+//                 over the group comes off, and the token's scale (times the softmax scale) is a factor, both in fp32;
 //   P'  = exp2(S - m) * s_v, rounded to bf16 once as the operand of the second product; transposed in registers (movmatrix);
-//   O^T += V^T P'^T   with 8 instead of z subtracted from the codes (one constant); the rest, sum of P' (z - 8), is a scalar per
-//                 query row and group, summed in fp32 from the same rounded P' and taken off at the end.
+//   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same
+//                 rounded P' and taken off at the end (a warp sums a few hundred tokens before that: the part that cancels costs
+//                 some 2^-12 of a quantiser's step).
 // Bound by HBM and by the issue slots of the unpacking (about two instructions per value); the tensor pipe idles.
-// The next tile's codes and parameters are loaded while the current one is computed, the page-table entry one tile earlier.
+// Each warp has a ring of three tiles in shared memory that asynchronous copies fill, two tiles ahead; the page-table entry is read
+// one tile earlier still.  Row g of a tile's products is token g ^ (g >> 1) of its eight (and so for the second eight), and for
+// D = 128 the 16-byte chunks of rows 2, 3, 6, 7, ... swap places by two: so the keys' reads (a row by four lanes) and the values' (a
+// row by eight) are both free of bank conflicts.
 constexpr int kKv4Warps = 4;
 constexpr int kKv4Threads = 32 * kKv4Warps;
 constexpr int kKv4Tile = 16;
@@ -204,22 +214,22 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return r;
 }
 
-template <int D, int G>
-struct Kv4Tile {
-    uint32_t k[2][D / 32];     // rows (tokens) g and g + 8: units 8 t .. 8 t + 7
-    uint32_t v[4][D / 64];     // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9: units 4 g .. 4 g + 3
-    uint32_t kp[2][D / G], vp[2][D / G];
-};
-
-template <int NG>
-__device__ __forceinline__ void kv4_load_params(uint32_t (&d)[NG], const uint32_t* p) {
-    if constexpr (NG == 1) {
-        d[0] = ld_4B(p);
-    } else if constexpr (NG == 2) {
-        const uint2 v = ld_8B(p);
+// A tile in shared memory: codes of K, codes of V (16 rows of D / 2 bytes), parameters of K, of V (16 rows of 4 * D / G bytes).
+constexpr int kKv4Depth = 3;
+__host__ __device__ constexpr int kv4_slot_bytes(int D, int G) { return 16 * D + 128 * (D / G); }
+__host__ __device__ constexpr int kv4_smem_bytes(int D, int G, int NT) {       // rings; at the end the warps' results in their place
+    const int rings = kKv4Warps * kKv4Depth * kv4_slot_bytes(D, G), results = kKv4Warps * 8 * NT * (D + 4) * 4;
+    return rings > results ? rings : results;
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t (&d)[N], const uint8_t* p) {
+    if constexpr (N == 1) {
+        d[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
         d[0] = v.x; d[1] = v.y;
     } else {
-        const uint4 v = ld_16B(p);
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
         d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
     }
 }
@@ -229,7 +239,9 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
 {
     constexpr int NJ = D / 32, NG = D / G, PER = G / 32, MT = D / 16;        // blocks of 32, groups, output tiles
     constexpr int COLS = 8 * NT;
-    __shared__ float s_o[kKv4Warps][COLS][D + 4];
+    constexpr int SLOT = kv4_slot_bytes(D, G);
+    extern __shared__ __align__(128) uint8_t kv4_smem[];
+    float (*s_o)[COLS][D + 4] = reinterpret_cast<float (*)[COLS][D + 4]>(kv4_smem);        // [warp][column][channel]
     __shared__ float s_m[kKv4Warps][COLS], s_l[kKv4Warps][COLS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = blockIdx.x, head = (int)blockIdx.y / p.col_tiles, ct = (int)blockIdx.y % p.col_tiles, b = blockIdx.z;
@@ -271,6 +283,24 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
         }
     }
 
+    // sums of the query rows over the groups, at the lane's columns (2 t and 2 t + 1): what (16 + z) is multiplied with
+    float qsum[NT][NG][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+            float v = 0.0f;
+#pragma unroll
+            for (int jj = 0; jj < PER; ++jj)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v += bf16_lo(q[n][gi * PER + jj][u]) + bf16_hi(q[n][gi * PER + jj][u]);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+            qsum[n][gi][0] = __shfl_sync(0xFFFFFFFFu, v, 8 * t);             // lane 4 g holds column g
+            qsum[n][gi][1] = __shfl_sync(0xFFFFFFFFu, v, 8 * t + 4);
+        }
+    const int full_limit = min(last, len - p.T + 1 + col0 / p.ratio);       // below it every column sees every key
+
     float o[MT][NT][4], m[NT][2], l[NT][2], zsum[NG][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -298,58 +328,74 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             ++entry;
         }
     };
-    // A tile's loads; a page outside of the cache is not read.  Tokens past the end of a request may hold anything.
-    auto fetch = [&](Kv4Tile<D, G>& d, int page, int place) {
-        if ((uint32_t)page >= (uint32_t)p.c.n_pages) return;
-        const int64_t row = ((int64_t)page * p.c.n_kv_heads + head) * p.c.page_size + place;
-        const uint8_t* k = p.c.codes[0] + (row + g) * (D / 2) + t * (D / 8);
-        const uint8_t* v = p.c.codes[1] + (row + 2 * t) * (D / 2) + g * (D / 16);
+    // Asks for the warp's next tile, one commit group per call; a page outside of the cache is not read.  Tokens past the end of a
+    // request may hold anything.  Bit i of `ok`: the i-th tile from the current one lies in the cache.
+    uint8_t* ring = kv4_smem + warp * (kKv4Depth * SLOT);
+    const int lane_code = D == 128 ? (lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 3) & 1) << 1)) * 16) : lane * 16;
+    const bool lane_param = (lane & 15) < 4 * NG;
+    const int lane_param_to = 16 * D + (lane >> 4) * (64 * NG) + (lane & 15) * 16;
+    const uint8_t* param_base = reinterpret_cast<const uint8_t*>(lane >> 4 ? p.c.params[1] : p.c.params[0]) + (lane & 15) * 16;
+    int ask_token = first + warp * kKv4Tile, entry = ask_token / p.c.page_size, place = ask_token - entry * p.c.page_size;
+    int page = ask_token < last ? (int)ld_4B(table + entry) : -1;
+    uint32_t ok = 0, ask_to = ptx::smem_addr(ring);
+    const uint32_t ring_end = ask_to + kKv4Depth * SLOT;
+    auto ask = [&](int bit) {
+        if (ask_token < last) {
+            if ((uint32_t)page < (uint32_t)p.c.n_pages) {
+                const int64_t row = ((int64_t)page * p.c.n_kv_heads + head) * p.c.page_size + place;
+                const uint8_t* k = p.c.codes[0] + row * (D / 2) + lane * 16;
+                const uint8_t* v = p.c.codes[1] + row * (D / 2) + lane * 16;
+                const uint32_t to = ask_to + lane_code;
+                cp_async_16(to, k);
+                cp_async_16(to + 8 * D, v);
+                if constexpr (D == 128) {
+                    cp_async_16(to + 512, k + 512);
+                    cp_async_16(to + 8 * D + 512, v + 512);
+                }
+                if (lane_param) cp_async_16(ask_to + lane_param_to, param_base + row * (4 * NG));
+                ok |= 1u << bit;
+            }
+            ask_token += stride;
+            advance(entry, place);
+            if (ask_token < last) page = (int)ld_4B(table + entry);
+        }
+        ask_to += SLOT;
+        if (ask_to == ring_end) ask_to -= kKv4Depth * SLOT;
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kKv4Depth - 1; ++i) ask(i);
+
+    const int gray = g ^ (g >> 1);                   // the token of row g
+    const int swap = D == 128 ? ((gray >> 1) & 1) << 1 : 0;
+    const uint8_t* slot = ring;
+    for (int token = first + warp * kKv4Tile; token < last; token += stride) {
+        cp_async_wait_but<kKv4Depth - 2>();          // this tile has landed,
+        __syncwarp();                                // for every lane, and the slot of the tile before is free
+        ask(kKv4Depth - 1);
+        const bool page_ok = ok & 1;
+        ok >>= 1;
+        if (!page_ok && lane == 0) report_index(4);
+        struct {
+            uint32_t k[2][D / 32];                   // rows g and g + 8: units 8 t .. 8 t + 7
+            uint32_t v[4][D / 64];                   // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9: units 4 g .. 4 g + 3
+            uint32_t kp[2][NG], vp[2][NG];
+        } cur;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if constexpr (D == 128) {
-                const uint4 x = ld_once_16B(k + h * 8 * (D / 2));
-                d.k[h][0] = x.x; d.k[h][1] = x.y; d.k[h][2] = x.z; d.k[h][3] = x.w;
-            } else {
-                const uint2 x = ld_8B(k + h * 8 * (D / 2));
-                d.k[h][0] = x.x; d.k[h][1] = x.y;
-            }
-            kv4_load_params<NG>(d.kp[h], p.c.params[0] + (row + g + 8 * h) * NG);
-            kv4_load_params<NG>(d.vp[h], p.c.params[1] + (row + g + 8 * h) * NG);
-        }
+            const int row = gray + 8 * h;
+            lds_words<D / 32>(cur.k[h], slot + row * (D / 2) + (t ^ swap) * (D / 8));
+            lds_words<NG>(cur.kp[h], slot + 16 * D + row * (4 * NG));
+            lds_words<NG>(cur.vp[h], slot + 16 * D + 64 * NG + row * (4 * NG));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint8_t* a = v + ((i >> 1) * 8 + (i & 1)) * (D / 2);
-            if constexpr (D == 128) {
-                const uint2 x = ld_8B(a);
-                d.v[i][0] = x.x; d.v[i][1] = x.y;
-            } else {
-                d.v[i][0] = ld_4B(a);
+            for (int i = 0; i < 2; ++i) {
+                const int r = 2 * t + i, tok = (r ^ (r >> 1)) + 8 * h;
+                const int chunk = D == 128 ? (((g >> 1) ^ (((tok >> 1) & 1) << 1)) * 16 + (g & 1) * 8) : g * 4;
+                lds_words<D / 64>(cur.v[2 * h + i], slot + 8 * D + tok * (D / 2) + chunk);
             }
         }
-    };
-
-    int token = first + warp * kKv4Tile;
-    int entry = token / p.c.page_size, place = token - entry * p.c.page_size;        // of the tile whose entry is read next
-    int page = token < last ? (int)ld_4B(table + entry) : -1, cur_place = place;
-    advance(entry, place);
-    int next_page = token + stride < last ? (int)ld_4B(table + entry) : -1, next_place = place;
-    advance(entry, place);
-    Kv4Tile<D, G> cur, nxt;
-    {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&cur);
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(cur) / 4); ++i) w[i] = 0;
-        nxt = cur;
-    }
-    if (token < last) fetch(cur, page, cur_place);
-
-    for (; token < last; token += stride) {
-        const int page_ahead = token + 2 * stride < last ? (int)ld_4B(table + entry) : -1;
-        if (token + stride < last) fetch(nxt, next_page, next_place);
-        next_place = place;
-        advance(entry, place);
-        const bool page_ok = (uint32_t)page < (uint32_t)p.c.n_pages;
-        if (!page_ok && lane == 0) report_index(4);
+        slot += SLOT;
+        if (slot == ring + kKv4Depth * SLOT) slot = ring;
 
         // scores of tokens (rows) g and g + 8, columns 2 t and 2 t + 1
         float s[NT][4];
@@ -361,16 +407,6 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
         for (int gi = 0; gi < NG; ++gi) {
             float acc[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
-            uint32_t zc[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {            // 128 + z in both halves (z <= 15: exact)
-                const uint32_t z2 = __byte_perm(cur.kp[h][gi], 0, 0x3232);
-                asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(zc[h]) : "r"(z2), "r"(0x43004300u));
-            }
-#pragma unroll
             for (int jj = 0; jj < PER; ++jj) {
                 const int j = gi * PER + jj;
                 uint32_t a[8];
@@ -378,62 +414,74 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                 for (int u = 0; u < 4; ++u) {
                     const int at = (u >> 1) * 4 + (u & 1) * 2;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t w = D == 128 ? cur.k[h][u] >> (4 * j) : cur.k[h][u >> 1] >> (8 * (u & 1) + 4 * j);
-                        a[at + h] = bf16x2_sub((w & 0x000F000Fu) | 0x43004300u, zc[h]);
-                    }
+                    for (int h = 0; h < 2; ++h) a[at + h] = kv4_codes_plus_16(D == 128 ? cur.k[h][u] : cur.k[h][u >> 1], D == 128 ? 4 * j : 8 * (u & 1) + 4 * j);
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    mma_bf16_16816(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
+                    if (jj == 0) mma_bf16_16816_first(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
+                    else mma_bf16_16816(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
                     mma_bf16_16816(acc[n], a[4], a[5], a[6], a[7], q[n][j][2], q[n][j][3]);
                 }
             }
-            const float s0 = bf16_lo(cur.kp[0][gi]), s1 = bf16_lo(cur.kp[1][gi]);
+            const float s0 = bf16_lo(cur.kp[0][gi]) * p.scale_log2, s1 = bf16_lo(cur.kp[1][gi]) * p.scale_log2;
+            const float z0 = bf16_hi(cur.kp[0][gi]) + 16.0f, z1 = bf16_hi(cur.kp[1][gi]) + 16.0f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                s[n][0] = fmaf(acc[n][0], s0, s[n][0]);
-                s[n][1] = fmaf(acc[n][1], s0, s[n][1]);
-                s[n][2] = fmaf(acc[n][2], s1, s[n][2]);
-                s[n][3] = fmaf(acc[n][3], s1, s[n][3]);
+                s[n][0] = fmaf(fmaf(-z0, qsum[n][gi][0], acc[n][0]), s0, s[n][0]);
+                s[n][1] = fmaf(fmaf(-z0, qsum[n][gi][1], acc[n][1]), s0, s[n][1]);
+                s[n][2] = fmaf(fmaf(-z1, qsum[n][gi][0], acc[n][2]), s1, s[n][2]);
+                s[n][3] = fmaf(fmaf(-z1, qsum[n][gi][1], acc[n][3]), s1, s[n][3]);
             }
         }
-        // mask, running maximum; a masked score is -inf whatever its token holds
-        const int t0 = page_ok ? token + g : INT_MAX - 16;
-        bool moved = false;
-        float alpha[NT][2];
+        // Masks, where a tile needs them: a masked score is -inf whatever its token holds.
+        const bool full = page_ok && token + kKv4Tile <= full_limit;         // of the whole warp
+        const int t0 = page_ok ? token + gray : INT_MAX - 16;
+        if (!full) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (t0 >= limit[n][e]) s[n][e] = -INFINITY;
+                    if (t0 + 8 >= limit[n][e]) s[n][2 + e] = -INFINITY;
+#pragma unroll
+                    for (int gi = 0; gi < NG; ++gi) {                        // past the request's end: parameters of no effect
+                        if (t0 >= last) cur.vp[0][gi] = 0;
+                        if (t0 + 8 >= last) cur.vp[1][gi] = 0;
+                    }
+                }
+        }
+        // The base of the exponentials follows the maximum of a column only once a score is more than 8 (in powers of two) above it:
+        // sums of up to 2^8 are as good as sums of up to 1, and most tiles need no reduction over the lanes.
+        bool above = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                s[n][e] = t0 < limit[n][e] ? s[n][e] * p.scale_log2 : -INFINITY;
-                s[n][2 + e] = t0 + 8 < limit[n][e] ? s[n][2 + e] * p.scale_log2 : -INFINITY;
-                float top = fmaxf(s[n][e], s[n][2 + e]);
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                alpha[n][e] = 1.0f;
-                if (top > m[n][e]) {
-                    alpha[n][e] = fast_exp2(m[n][e] - top);                  // 0 from -inf
-                    m[n][e] = top;
-                    moved = true;
-                }
-            }
-        if (__any_sync(0xFFFFFFFFu, moved)) {
+            for (int e = 0; e < 2; ++e) above = above || fmaxf(s[n][e], s[n][2 + e]) > m[n][e] + 8.0f;
+        if (__any_sync(0xFFFFFFFFu, above)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+                float alpha[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    l[n][e] *= alpha[n][e];
+                    float top = fmaxf(s[n][e], s[n][2 + e]);
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                    alpha[e] = 1.0f;
+                    if (top > m[n][e]) {
+                        alpha[e] = fast_exp2(m[n][e] - top);                 // 0 from -inf
+                        m[n][e] = top;
+                    }
+                    l[n][e] *= alpha[e];
 #pragma unroll
-                    for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] *= alpha[n][e];
+                    for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] *= alpha[e];
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    o[i][n][0] *= alpha[n][0];
-                    o[i][n][1] *= alpha[n][1];
-                    o[i][n][2] *= alpha[n][0];
-                    o[i][n][3] *= alpha[n][1];
+                    o[i][n][0] *= alpha[0];
+                    o[i][n][1] *= alpha[1];
+                    o[i][n][2] *= alpha[0];
+                    o[i][n][3] *= alpha[1];
                 }
             }
         }
@@ -455,11 +503,13 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float sv = bf16_lo(cur.vp[h][gi]);
-                    // a masked token adds nothing, not even 0 * NaN
-                    const float a = t0 + 8 * h < limit[n][0] ? s[n][2 * h] * sv : 0.0f;
-                    const float c = t0 + 8 * h < limit[n][1] ? s[n][2 * h + 1] * sv : 0.0f;
+                    float a = s[n][2 * h] * sv, c = s[n][2 * h + 1] * sv;
+                    if (!full) {                     // a masked token adds nothing, not even 0 * NaN
+                        a = t0 + 8 * h < limit[n][0] ? a : 0.0f;
+                        c = t0 + 8 * h < limit[n][1] ? c : 0.0f;
+                    }
                     const uint32_t w = pack_bf16x2(a, c);
-                    const float z = t0 + 8 * h < last ? bf16_hi(cur.vp[h][gi]) - 8.0f : 0.0f;
+                    const float z = bf16_hi(cur.vp[h][gi]) + 16.0f;
                     zsum[gi][n][0] = fmaf(bf16_lo(w), z, zsum[gi][n][0]);
                     zsum[gi][n][1] = fmaf(bf16_hi(w), z, zsum[gi][n][1]);
                     pb[n][h] = movmatrix_trans(w);
@@ -482,20 +532,16 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
 #pragma unroll
                 for (int jj = 0; jj < PER; ++jj) {
                     const int j = gi * PER + jj;
-                    const uint32_t eight = 0x43084308u;                      // 128 + 8
-                    const uint32_t a0 = bf16x2_sub(((lo01 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
-                    const uint32_t a1 = bf16x2_sub(((hi01 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
-                    const uint32_t a2 = bf16x2_sub(((lo89 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
-                    const uint32_t a3 = bf16x2_sub(((hi89 >> (4 * j)) & 0x000F000Fu) | 0x43004300u, eight);
+                    const uint32_t a0 = kv4_codes_plus_16(lo01, 4 * j), a2 = kv4_codes_plus_16(lo89, 4 * j);
+                    const uint32_t a1 = kv4_codes_plus_16(hi01, 4 * j), a3 = kv4_codes_plus_16(hi89, 4 * j);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
                 }
             }
         }
-        cur = nxt;
-        page = next_page;
-        next_page = page_ahead;
     }
+    cp_async_wait_all();
+    __syncthreads();                                 // the rings are done with: the results take their place
 
     // sums over the lanes that share a column, then the warps' results side by side
 #pragma unroll
@@ -555,14 +601,15 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
     }
 }
 
-// Joins the splits of one query row: every warp a share of them, in a fixed order.
-template <int D, int NT>
-__global__ void __launch_bounds__(128) kv4_join_kernel(const Kv4AttnArgs p)
+// Joins the splits of one query row: their largest maximum, their weights, then the weighted sums, a share of the splits per group
+// of threads; all in a fixed order.
+constexpr int kKv4MaxSplits = 256;
+template <int D, int NT, int THREADS>
+__global__ void __launch_bounds__(THREADS) kv4_join_kernel(const Kv4AttnArgs p)
 {
-    constexpr int COLS = 8 * NT, V = D / 32;         // channels per lane
-    __shared__ float s_o[4][D];
-    __shared__ float s_m[4], s_l[4];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int COLS = 8 * NT, V = D / 4, SHARES = THREADS / V;            // a thread takes four channels of every SHARES-th split
+    __shared__ float s_w[kKv4MaxSplits], s_l[kKv4MaxSplits];
+    __shared__ float4 s_o[SHARES][V];
     const int row = blockIdx.x, b = row / (p.T * p.Hq), rest = row % (p.T * p.Hq), i = rest / p.Hq, h = rest % p.Hq;
     const int head = h / p.ratio, col = i * p.ratio + h % p.ratio, ct = col / COLS, c = col % COLS;
     ptx::grid_dependency_wait();
@@ -571,49 +618,43 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const Kv4AttnArgs p)
     const int used = len == 0 ? 1 : (len + keys - 1) / keys;
     const float* base = p.part + ((((int64_t)b * p.c.n_kv_heads + head) * p.col_tiles + ct) * p.splits * COLS + c) * (D + 4);
     const int64_t step = (int64_t)COLS * (D + 4);
-    float m = -INFINITY, l = 0.0f, v[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = 0.0f;
-#pragma unroll 4
-    for (int s = warp; s < used; s += 4) {
-        const float* x = base + s * step;
-        const float2 ml = *reinterpret_cast<const float2*>(x + D);
-        float w[V];
-        if constexpr (V == 4) {
-            const float4 f = *reinterpret_cast<const float4*>(x + lane * 4);
-            w[0] = f.x; w[1] = f.y; w[2] = f.z; w[3] = f.w;
-        } else {
-            const float2 f = *reinterpret_cast<const float2*>(x + lane * 2);
-            w[0] = f.x; w[1] = f.y;
-        }
-        const float top = fmaxf(m, ml.x);
-        if (top == -INFINITY) {                      // nothing seen so far: 0, or a NaN that is passed on
-            l += ml.y;
-            continue;
-        }
-        const float fa = fast_exp2(m - top), fb = fast_exp2(ml.x - top);
-        l = l * fa + ml.y * fb;
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = v[k] * fa + w[k] * fb;
-        m = top;
+    for (int s = threadIdx.x; s < used; s += THREADS) {
+        const float2 ml = *reinterpret_cast<const float2*>(base + s * step + D);
+        s_w[s] = ml.x;
+        s_l[s] = ml.y;
     }
-#pragma unroll
-    for (int k = 0; k < V; ++k) s_o[warp][lane * V + k] = v[k];
-    if (lane == 0) {
-        s_m[warp] = m;
-        s_l[warp] = l;
-    }
+    const int share = threadIdx.x / V, v = threadIdx.x % V;
     __syncthreads();
-    if (threadIdx.x < D) {
-        const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-        float sum = 0.0f, x = 0.0f;
+    float top = -INFINITY;
+    for (int s = 0; s < used; ++s) top = fmaxf(top, s_w[s]);
+    if (top == -INFINITY) top = 0.0f;                // nothing seen: every weight is 0
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int s = share; s < used; s += SHARES) {
+        const float f = fast_exp2(s_w[s] - top);
+        const float4 x = *reinterpret_cast<const float4*>(base + s * step + v * 4);
+        o.x = fmaf(f, x.x, o.x);
+        o.y = fmaf(f, x.y, o.y);
+        o.z = fmaf(f, x.z, o.z);
+        o.w = fmaf(f, x.w, o.w);
+    }
+    s_o[share][v] = o;
+    __syncthreads();
+    if (threadIdx.x < V) {
+        float sum = 0.0f;                            // a split of which every score was NaN has a NaN sum and no maximum: it is kept
+        for (int s = 0; s < used; ++s) sum += s_l[s] != s_l[s] ? s_l[s] : fast_exp2(s_w[s] - top) * s_l[s];
+        float4 x = s_o[0][threadIdx.x];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = top == -INFINITY ? 1.0f : fast_exp2(s_m[w] - top);
-            sum += f * s_l[w];
-            x += f * s_o[w][threadIdx.x];
+        for (int w = 1; w < SHARES; ++w) {
+            const float4 a = s_o[w][threadIdx.x];
+            x.x += a.x;
+            x.y += a.y;
+            x.z += a.z;
+            x.w += a.w;
         }
-        p.O[((int64_t)(b * (int64_t)p.T + i) * p.Hq + h) * D + threadIdx.x] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : x / sum);
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        bf16* out = p.O + ((int64_t)(b * (int64_t)p.T + i) * p.Hq + h) * D + threadIdx.x * 4;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
     }
 }
 

@@ -60,13 +60,13 @@ Kv4Plan kv4_plan(int64_t B, int T, int ratio, int n_kv_heads, int head_dim, int6
     p.nt = cols <= 8 ? 1 : 2;
     p.col_tiles = (int)((cols + 8 * p.nt - 1) / (8 * p.nt));
     const int64_t ctas = B * n_kv_heads * p.col_tiles;
-    int64_t target = (int64_t)sms * 6;
+    int64_t target = (int64_t)sms * 4;
     int64_t long_keys = 2048;
     int64_t splits = (target + ctas - 1) / ctas;
     const int64_t by_length = (most_keys + long_keys - 1) / long_keys, most = (most_keys + 127) / 128;
     if (splits < by_length && ctas * by_length <= 1 << 20) splits = by_length;
     if (splits > most) splits = most;
-    if (splits > 256) splits = 256;
+    if (splits > gmlp::kKv4MaxSplits) splits = gmlp::kKv4MaxSplits;
     if (splits < 1) splits = 1;
     p.splits = (int)splits;
     p.workspace = splits > 1 ? (uint64_t)ctas * splits * 8 * p.nt * (head_dim + 4) * 4 : 0;
@@ -122,19 +122,19 @@ int kv4_attention_impl(const gmlp_kv4_attention_args* a) {
     const dim3 grid((unsigned)plan.splits, (unsigned)(k.c.n_kv_heads * plan.col_tiles), (unsigned)a->B);
     if (grid.y > 65535u) return GMLP_ERR_SHAPE;
     prof_begin(st);
-#define GMLP_KV4_ATTN1(D, G) launch_chained(gmlp::kv4_attention_kernel<D, G, 1>, grid, gmlp::kKv4Threads, 0, 1, st, k)
-#define GMLP_KV4_ATTN2(D, G) launch_chained(gmlp::kv4_attention_kernel<D, G, 2>, grid, gmlp::kKv4Threads, 0, 1, st, k)
+#define GMLP_KV4_ATTN1(D, G) launch_chained(gmlp::kv4_attention_kernel<D, G, 1>, grid, gmlp::kKv4Threads, (uint32_t)gmlp::kv4_smem_bytes(D, G, 1), 1, st, k)
+#define GMLP_KV4_ATTN2(D, G) launch_chained(gmlp::kv4_attention_kernel<D, G, 2>, grid, gmlp::kKv4Threads, (uint32_t)gmlp::kv4_smem_bytes(D, G, 2), 1, st, k)
     rc = plan.nt == 1 ? GMLP_KV4_DISPATCH(k.c, GMLP_KV4_ATTN1) : GMLP_KV4_DISPATCH(k.c, GMLP_KV4_ATTN2);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv4_attention", st);
     if (plan.splits > 1) {
         const dim3 rows((unsigned)(a->B * a->q_len * a->n_q_heads));
-        if (k.c.head_dim == 128)
-            rc = plan.nt == 1 ? launch_chained(gmlp::kv4_join_kernel<128, 1>, rows, 128, 0, 1, st, k)
-                              : launch_chained(gmlp::kv4_join_kernel<128, 2>, rows, 128, 0, 1, st, k);
-        else
-            rc = plan.nt == 1 ? launch_chained(gmlp::kv4_join_kernel<64, 1>, rows, 128, 0, 1, st, k)
-                              : launch_chained(gmlp::kv4_join_kernel<64, 2>, rows, 128, 0, 1, st, k);
+        // few splits of many rows: small CTAs; many splits: sixteen or more shares of them at once
+#define GMLP_KV4_JOIN(D, NT)                                                                                        \
+    (plan.splits <= 16 ? launch_chained(gmlp::kv4_join_kernel<D, NT, 128>, rows, 128, 0, 1, st, k)                  \
+                       : launch_chained(gmlp::kv4_join_kernel<D, NT, 512>, rows, 512, 0, 1, st, k))
+        if (k.c.head_dim == 128) rc = plan.nt == 1 ? GMLP_KV4_JOIN(128, 1) : GMLP_KV4_JOIN(128, 2);
+        else rc = plan.nt == 1 ? GMLP_KV4_JOIN(64, 1) : GMLP_KV4_JOIN(64, 2);
         if (rc != GMLP_OK) return rc;
         prof_mark("kv4_join", st);
     }

@@ -1,47 +1,62 @@
 // Host side of the 4-bit weight operators: checks, launch shapes, launches.  Included by api.cu inside its namespace.
 
 struct W4Plan {
-    int nt, wr_log2, cluster, chunk, groups;
+    bool stream;                                     // w4_stream_kernel, else w4_tile_kernel
+    int nt, ctas, threads, group_warps;
+    int m_cta, m_parts, wr_log2, cluster, groups;    // tile kernel
     uint32_t smem;
 };
+inline int w4_k_blocks(int64_t K) { return (int)((K + 255) / 256) * 2; }      // of 128 rows, an even number
+constexpr uint32_t kW4SmemMost = 224 * 1024;
 
-constexpr uint32_t kW4SmemMost = 200 * 1024;
-
-// Launch shape of one product: `units` pairs of 16-column tiles, K in `KB` blocks of 128.
-W4Plan w4_plan(int M, int terms, int KB, int units, int sms) {
+// Launch shape of one product: `n16` column tiles (gated: of each matrix), K in `KB` blocks of 128, groups of G.
+W4Plan w4_plan(int M, int terms, int KB, int n16, bool gated, int G, int sms) {
     W4Plan p{};
-    p.nt = (M + 7) / 8;
-    if (p.nt == 5) p.nt = 6;
-    if (p.nt == 7) p.nt = 8;
-    const int per_sm = p.nt <= 2 ? 2 : 1, rows = M * terms;
-    const uint32_t budget = per_sm == 2 ? kW4SmemMost / 2 : kW4SmemMost, pad = (uint32_t)rows * 64u;
-    const int depth = gmlp::w4_prefetch(p.nt);       // a chunk boundary falls between rounds of the register prefetch
-    // Column groups per CTA: X costs M * terms * 256 bytes of shared memory a k-block, the codes of one group 2 KB.
-    p.wr_log2 = rows <= 2 ? 0 : (rows <= 4 ? 1 : (rows <= 16 ? 2 : 3));
-    // Fewer groups for a matrix of few columns, as long as two buffers of the shortest chunk still fit.
-    while (p.wr_log2 > 0 && (units >> p.wr_log2) == 0 &&
-           2u * ((uint32_t)depth * (uint32_t)rows * (16u >> p.wr_log2) * 256u + pad) <= budget)
-        --p.wr_log2;
+    const int rows = M * terms;
+    // The persistent kernel, where all of X fits beside the rings.
+        const uint64_t smem = gmlp::w4_stream_bytes(rows, KB, G);
+        if (smem <= kW4SmemMost) {
+            p.stream = true;
+            p.nt = rows <= 8 ? 1 : 2;
+            p.threads = gmlp::kW4StreamThreads;
+            // eight warps a tile where K is long or there are few tiles, else four (fewer hand-overs of sums)
+            p.group_warps = KB >= 64 || n16 <= sms ? 8 : 4;
+            p.ctas = n16 < sms ? n16 : sms;
+            p.m_cta = M;
+            p.m_parts = p.cluster = 1;
+            p.smem = (uint32_t)smem;
+            return p;
+        }
+    }
+    p.m_parts = (rows + 31) / 32;
+    p.m_cta = (M + p.m_parts - 1) / p.m_parts;
+    p.m_parts = (M + p.m_cta - 1) / p.m_cta;
+    const int rows_cta = p.m_cta * terms, units = gated ? n16 : (n16 + 1) / 2;
+    p.nt = (rows_cta + 7) / 8;
+    // Column groups per CTA: few, so that a CTA's warps share long ranges of K and their sums stay in the CTA, unless there are
+    // columns enough to fill the GPU with more (each group reads its CTA's copy of X).
+    p.wr_log2 = rows_cta <= 16 ? 0 : (units * p.m_parts >= 4 * sms ? 2 : 1);
     const int WR = 1 << p.wr_log2, WK = 8 >> p.wr_log2;
     p.groups = (units + WR - 1) / WR;
-    // K over a cluster until the GPU has its share of CTAs (two per SM for the smaller token counts), as long as each
-    // warp keeps a k-block or more.
+    // K over a cluster only where the CTAs would leave a third of the SMs idle: its hand-over costs about two microseconds
     p.cluster = 1;
-    while (p.cluster < 8 && p.groups * p.cluster < sms * per_sm && KB >= WK * (p.cluster + 1)) ++p.cluster;
-    const int kb_cta = (KB + p.cluster - 1) / p.cluster, steps = (kb_cta + WK - 1) / WK;
-    const uint32_t step_bytes = (uint32_t)rows * (uint32_t)WK * 256u;
-    p.chunk = steps;
-    if ((uint64_t)steps * step_bytes + pad > budget) p.chunk = (int)((budget / 2 - pad) / step_bytes) / depth * depth;
-    const uint32_t x = (p.chunk * step_bytes + pad) * (p.chunk < steps ? 2u : 1u), red = gmlp::w4_red_bytes(p.nt);
-    p.smem = x > red ? x : red;
+    while (p.cluster < 4 && 3 * p.groups * p.m_parts * p.cluster <= 2 * sms && KB >= 2 * WK * (p.cluster + 1)) ++p.cluster;
+    p.ctas = p.groups * p.cluster;
+    p.threads = gmlp::kW4Threads;
+    p.smem = gmlp::w4_tile_smem(p.nt, rows_cta, WK, G);
     return p;
 }
 
 typedef void (*W4Kernel)(gmlp::W4GemmArgs);
 template <int NT>
-W4Kernel w4_kernel_for(int G, bool gated) {
-    if (gated) return G == 32 ? gmlp::w4_gemm_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_gemm_kernel<NT, 64, true> : gmlp::w4_gemm_kernel<NT, 128, true>);
-    return G == 32 ? gmlp::w4_gemm_kernel<NT, 32, false> : (G == 64 ? gmlp::w4_gemm_kernel<NT, 64, false> : gmlp::w4_gemm_kernel<NT, 128, false>);
+W4Kernel w4_stream_kernel_for(int G, bool gated) {
+    if (gated) return G == 32 ? gmlp::w4_stream_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_stream_kernel<NT, 64, true> : gmlp::w4_stream_kernel<NT, 128, true>);
+    return G == 32 ? gmlp::w4_stream_kernel<NT, 32, false> : (G == 64 ? gmlp::w4_stream_kernel<NT, 64, false> : gmlp::w4_stream_kernel<NT, 128, false>);
+}
+template <int NT>
+W4Kernel w4_tile_kernel_for(int G, bool gated) {
+    if (gated) return G == 32 ? gmlp::w4_tile_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_tile_kernel<NT, 64, true> : gmlp::w4_tile_kernel<NT, 128, true>);
+    return G == 32 ? gmlp::w4_tile_kernel<NT, 32, false> : (G == 64 ? gmlp::w4_tile_kernel<NT, 64, false> : gmlp::w4_tile_kernel<NT, 128, false>);
 }
 
 int check_w4_matrix(const gmlp_w4_matrix& w) {
@@ -80,20 +95,21 @@ int launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, uint32_t s
 
 int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_matrix* w1, const bf16* X, int terms, bf16* out,
                    int64_t M, gmlp::GateAct act, bool early, cudaStream_t st) {
-    const int K = (int)w0.K, N = (int)w0.N, KB = (K + 127) / 128, n16 = (N + 15) / 16;
+    const int K = (int)w0.K, N = (int)w0.N, KB = w4_k_blocks(K), n16 = (N + 15) / 16;
     const bool gated = w1 != nullptr;
-    const W4Plan p = w4_plan((int)M, terms, KB, gated ? n16 : (n16 + 1) / 2, dev->sm_count);
-    if (p.chunk < 1 || p.smem > kW4SmemMost) return GMLP_ERR_UNSUPPORTED;       // w4_plan yields no such shape
+    const W4Plan p = w4_plan((int)M, terms, KB, n16, gated, w0.group, dev->sm_count);
     W4Kernel kernel;
-    switch (p.nt) {
-        case 1: kernel = w4_kernel_for<1>(w0.group, gated); break;
-        case 2: kernel = w4_kernel_for<2>(w0.group, gated); break;
-        case 3: kernel = w4_kernel_for<3>(w0.group, gated); break;
-        case 4: kernel = w4_kernel_for<4>(w0.group, gated); break;
-        case 6: kernel = w4_kernel_for<6>(w0.group, gated); break;
-        default: kernel = w4_kernel_for<8>(w0.group, gated); break;
+    if (p.stream) {
+        kernel = p.nt == 1 ? w4_stream_kernel_for<1>(w0.group, gated) : w4_stream_kernel_for<2>(w0.group, gated);
+    } else {
+        switch (p.nt) {
+            case 1: kernel = w4_tile_kernel_for<1>(w0.group, gated); break;
+            case 2: kernel = w4_tile_kernel_for<2>(w0.group, gated); break;
+            case 3: kernel = w4_tile_kernel_for<3>(w0.group, gated); break;
+            default: kernel = w4_tile_kernel_for<4>(w0.group, gated); break;
+        }
     }
-    const int slot = (p.nt - 1) * 6 + (gated ? 3 : 0) + (w0.group == 32 ? 0 : (w0.group == 64 ? 1 : 2));
+    const int slot = ((p.stream ? 4 : 0) + p.nt - 1) * 6 + (gated ? 3 : 0) + (w0.group == 32 ? 0 : (w0.group == 64 ? 1 : 2));
     if (!dev->w4_attr_set[slot]) {
         if (cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kW4SmemMost) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
@@ -110,12 +126,13 @@ int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_mat
     a.KB = KB;
     a.n16 = n16;
     a.terms = terms;
+    a.m_cta = p.m_cta;
     a.wr_log2 = p.wr_log2;
     a.cluster = p.cluster;
-    a.chunk = p.chunk;
+    a.group_warps = p.group_warps;
     a.early = early ? 1 : 0;
     a.act = act;
-    return launch_chained(kernel, dim3((unsigned)(p.groups * p.cluster)), gmlp::kW4Threads, p.smem, p.cluster, st, a);
+    return launch_chained(kernel, dim3((unsigned)p.ctas, (unsigned)p.m_parts), (unsigned)p.threads, p.smem, p.cluster, st, a);
 }
 
 int finish_checked(uint32_t flags, cudaStream_t st) {
@@ -210,7 +227,7 @@ int w4_layout_impl(const gmlp_w4_layout_args* a, int kind) {
     if (dev == nullptr) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(a->stream);
     const int K = (int)a->m.K, N = (int)a->m.N, G = a->m.group, out_in = (a->flags & GMLP_FLAG_WEIGHTS_OUT_IN) ? 1 : 0;
-    const dim3 grid((unsigned)(((N + 15) / 16 * 16 + 127) / 128), (unsigned)((K + 127) / 128));
+    const dim3 grid((unsigned)(((N + 15) / 16 * 16 + 127) / 128), (unsigned)w4_k_blocks(K));
     uint8_t* codes = static_cast<uint8_t*>(const_cast<void*>(a->m.codes));
     bf16* scales = static_cast<bf16*>(const_cast<void*>(a->m.scales));
     uint8_t* zeros = static_cast<uint8_t*>(const_cast<void*>(a->m.zeros));

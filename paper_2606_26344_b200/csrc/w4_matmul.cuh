@@ -2,20 +2,21 @@
 // q in 0..15, one scale s (bf16) and one zero point z (0..15; 8 without stored zero points) per group of G = 32, 64 or 128
 // input rows.  Bound by HBM: the codes are read once, half a byte per weight.
 //
-// Storage (made once by the pack kernels below): tiles of 16 output columns x 128 input rows, 1 KB each, [N / 16][K / 128],
-// so that the stream of a warp is contiguous.  In a tile, lane 4 g + t of a warp finds its 16 bytes for column g at
-// 16 * lane and for column g + 8 at 512 + 16 * lane: eight 16-bit units r = 8 t .. 8 t + 7, unit r holding the codes of
-// k = r, r + 32, r + 64, r + 96 in its four nibbles.  One shift and one and-or turn a 32-bit word into two bf16 numbers
-// 128 + q (128..255 has a step of one in bf16); subtracting 128 + z leaves q - z exactly.  Those pairs are A operands of
-// mma.m16n8k16 as they are, columns of W as its 16 rows and tokens as its 8 columns; the k order they imply
-// (32 j + 8 t + 0..7) makes the matching B operand 16 contiguous bytes of a row of X.  Products of a group are summed in
-// fp32 by the tensor core, then scaled in fp32: no weight is ever rounded.
+// Storage (made once by the pack kernels below): tiles of 16 output columns x 128 input rows, 1 KB each, [N / 16][K / 128] with the
+// second count even, so that the stream of a warp is contiguous.  In a tile, lane 4 g + t of a warp finds its 16 bytes for column g
+// at 16 * lane and for column g + 8 at 512 + 16 * lane: eight 16-bit units r = 8 t .. 8 t + 7, unit r holding the codes of k = r,
+// r + 32, r + 64, r + 96 in its four nibbles; every 32-bit word is rotated left by three bits.  One rotation and one and-or turn a
+// word into two bf16 numbers 16 + q (the nibble lands in the upper four mantissa bits).  Those pairs are A operands of mma.m16n8k16 as
+// they are, columns of W as its 16 rows and tokens as its 8 columns; the k order they imply (32 j + 8 t + 0..7) makes the matching B
+// operand 16 contiguous bytes of a row of X.  Products of a group are summed in fp32 by the tensor core, then scaled in fp32: no
+// weight is ever rounded.  16 + z comes off either before the product (q - z, exact in bf16: one more instruction per pair) or after
+// it, as (16 + z) times the group's sum of X, which is formed once per call.
 //
-// A warp takes two tiles at a time (two neighbouring column tiles, or the gate and the up tile of the same columns), so one
-// B operand serves both; the 8 warps of a CTA are WR column groups x WK ranges of K, and a cluster of C CTAs splits K
-// further; both partial sums are added in a fixed order (shared memory, then distributed shared memory).
+// K is split over the warps of a CTA and, where that helps, over the CTAs of a cluster; partial sums are added in a fixed order
+// (shared memory, then distributed shared memory).
 // X may come as two bf16 terms (hi + lo, 16 bits of significand): activations that are not bf16 by nature - the normed
-// input, the gated product - keep the accuracy of the fp32 they were computed in; both terms go into the same accumulator.
+// input, the gated product - keep the accuracy of the fp32 they were computed in.  The lo terms are further rows of X to the
+// product; the epilogue adds the two sums of a token.
 #pragma once
 #include <type_traits>
 
@@ -38,7 +39,9 @@ struct W4GemmArgs {
     const bf16* X;             // [terms][M][K]
     bf16* out;                 // plain: [M][N]; gated: [2][M][N], hi and lo of the gated product
     int M, K, N, KB, n16, terms;
-    int wr_log2, cluster, chunk;           // column groups per CTA; CTAs per cluster; steps (WK k-blocks each) of X per chunk
+    int m_cta;                 // tokens per CTA: blockIdx.y takes the tokens from blockIdx.y * m_cta on
+    int group_warps;           // stream kernel: warps of a team, a power of two
+    int wr_log2, cluster;      // tile kernel: column groups per CTA; CTAs per cluster
     int early;                 // the weights may be fetched before the preceding kernel of the call has ended
     GateAct act;
 };
@@ -49,19 +52,42 @@ __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t bf16x2_sub(uint32_t a, uint32_t b) {
+// The same onto zeros: a group's first product.
+__device__ __forceinline__ void mma_bf16_16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                     uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+// a + b in both halves.
+__device__ __forceinline__ uint32_t bf16x2_add(uint32_t a, uint32_t b) {
     uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0x3F803F80u), "r"(b));
     return d;
 }
-// The codes of nibble `j` of both halves of a word as bf16 (128 + q), then minus `zc` (128 + z in both halves).
-template <int SHIFT>
-__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t w, uint32_t zc) {
-    return bf16x2_sub(((w >> SHIFT) & 0x000F000Fu) | 0x43004300u, zc);
+// (w & mask) | bits in one instruction (left to itself the compiler splits the and-or of two constants in two, and these run at half
+// rate: a third of the kernel's issue slots).
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(bits));
+    return d;
 }
+// Nibble J of both halves of a (rotated) word as bf16 16 + q.
+template <int J>
+__device__ __forceinline__ uint32_t w4_codes_plus_16(uint32_t w) {
+    return and_or(J == 0 ? w : __funnelshift_r(w, w, 4 * J), 0x00780078u, 0x41804180u);
+}
+constexpr uint32_t kW4NoZeros = 0xC0C0C0C0u;         // zero points are stored as 0x80 | z << 3, the low byte of bf16 16 + z: here z = 8
 __device__ __forceinline__ void cp_async_16_zfill(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until at most N of the thread's newest groups are still on their way.
+template <int N>
+__device__ __forceinline__ void cp_async_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // Loads of codes and parameters.  Volatile, so that none moves ahead of griddepcontrol.wait; plain (not .nc) because the kernel
 // before, which may have written them, can still be running when this one starts.
@@ -101,23 +127,341 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
     return v;
 }
 
-template <int G>
-struct W4Stage {                                     // one k-block (128) of a warp's two tiles
-    uint4 c[2][2];                                   // [tile][column half]
-    uint32_t s[2][2][G == 32 ? 2 : 1];               // 128 / G scales of the lane's columns g and g + 8
-    uint32_t z[2][2];                                // 128 / G zero points, one byte each
-};
+// ------------------------------------------------------------------ one k-block of a tile
+// In shared memory, for B neighbouring k-blocks: their kilobytes of codes, their 16 * NG scales each, their 16 * NG zero points each
+// (NG = 128 / G groups of a column).
+__host__ __device__ constexpr int w4_slot_bytes(int G, int B) { return B * (1024 + 48 * (128 / G)); }
 
-__host__ __device__ constexpr int w4_prefetch(int nt) { return nt <= 8 ? 2 : 1; }      // k-blocks in flight per warp
-__host__ __device__ constexpr int w4_red_stride(int nt) { return 8 * (nt | 1); }      // floats; odd multiples of 8 spread the banks
-__host__ __device__ constexpr uint32_t w4_red_bytes(int nt) { return 8u * 32u * (uint32_t)w4_red_stride(nt) * 4u; }
+// A lane's share of copying k-blocks of one tile: 16 bytes of either half of each kilobyte of codes, and (the first lanes) 16 bytes of
+// scales or zero points.
+struct W4Source {
+    const uint8_t *codes, *params;       // params: nullptr for a lane that copies none
+};
+template <int B>
+__device__ __forceinline__ W4Source w4_source(const W4Operand& w, int64_t block, int lane, int ng) {
+    W4Source s = {w.codes + block * 1024 + lane * 16, nullptr};
+    if (lane < 2 * B * ng) s.params = reinterpret_cast<const uint8_t*>(w.scales) + block * (32 * ng) + lane * 16;
+    else if (lane < 3 * B * ng && w.zeros != nullptr) s.params = w.zeros + block * (16 * ng) + (lane - 2 * B * ng) * 16;
+    return s;
+}
+// Bytes per k-block of the parameters that the lane copies.
+template <int B>
+__device__ __forceinline__ uint32_t w4_param_bytes(int lane, int ng) { return lane < 2 * B * ng ? 32 * ng : 16 * ng; }
+// Copies B k-blocks to shared memory; `to` is the slot's address plus 16 * lane.
+template <int B>
+__device__ __forceinline__ void w4_copy_blocks(uint32_t to, const W4Source& s, bool params) {
+#pragma unroll
+    for (int i = 0; i < 2 * B; ++i) cp_async_16(to + 512 * i, s.codes + 512 * i);
+    if (params) cp_async_16(to + 1024 * B, s.params);
+}
+// The lane's part of a k-block, in registers.
+template <int G>
+struct W4Block {
+    uint32_t c[2][4];                    // columns g and g + 8
+    uint32_t s[2][G == 32 ? 2 : 1];      // their 128 / G scales
+    uint32_t z[2];                       // and zero points, one byte each
+};
+// k-block i of a slot of B.
+template <int G, int B>
+__device__ __forceinline__ void w4_read_block(W4Block<G>& d, const uint8_t* slot, int i, int lane, bool has_zeros) {
+    constexpr int NG = 128 / G;
+    const int g = lane >> 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint4 c = *reinterpret_cast<const uint4*>(slot + i * 1024 + h * 512 + lane * 16);
+        d.c[h][0] = c.x; d.c[h][1] = c.y; d.c[h][2] = c.z; d.c[h][3] = c.w;
+        const uint8_t* s = slot + B * 1024 + i * 32 * NG + (g + 8 * h) * 2 * NG;
+        if constexpr (G == 32) {
+            const uint2 v = *reinterpret_cast<const uint2*>(s);
+            d.s[h][0] = v.x; d.s[h][1] = v.y;
+        } else if constexpr (G == 64) {
+            d.s[h][0] = *reinterpret_cast<const uint32_t*>(s);
+        } else {
+            d.s[h][0] = *reinterpret_cast<const uint16_t*>(s);
+        }
+        const uint8_t* z = slot + B * 1024 + B * 32 * NG + i * 16 * NG + (g + 8 * h) * NG;
+        d.z[h] = kW4NoZeros;
+        if (has_zeros) {
+            if constexpr (G == 32) d.z[h] = *reinterpret_cast<const uint32_t*>(z);
+            else if constexpr (G == 64) d.z[h] = *reinterpret_cast<const uint16_t*>(z);
+            else d.z[h] = *z;
+        }
+    }
+}
+// SUMS: 16 + z comes off after the product; xsum: the sums of X over the k-block's groups, NT * 8 floats each, at the lane's columns.
+template <int J, bool SUMS, int TP, int NT, int G>
+__device__ __forceinline__ void w4_sub_block(float (&y)[TP][NT][4], float (&acc)[TP][NT][4], uint32_t (&zc)[TP][2],
+                                             const W4Block<G> (&d)[TP], const uint8_t* x, const int (&row_at)[NT], const float* xsum) {
+    constexpr int gi = J * 32 / G;                   // 32 of the 128 k, their group
+    constexpr bool first = (J * 32) % G == 0;
+    if constexpr (first && !SUMS) {
+#pragma unroll
+        for (int j = 0; j < TP; ++j)                                         // bf16 -(16 + z), twice: the bytes z, 0xC1, z, 0xC1
+#pragma unroll
+            for (int h = 0; h < 2; ++h) zc[j][h] = __byte_perm(d[j].z[h], 0xC1C1C1C1u, 0x4040u | gi | (gi << 8));
+    }
+    uint32_t a[TP][8];
+#pragma unroll
+    for (int j = 0; j < TP; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v = w4_codes_plus_16<J>(d[j].c[h][u]);
+                if constexpr (!SUMS) v = bf16x2_add(v, zc[j][h]);
+                a[j][(u >> 1) * 4 + (u & 1) * 2 + h] = v;
+            }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint4 b = *reinterpret_cast<const uint4*>(x + row_at[n] + J * 64);
+#pragma unroll
+        for (int j = 0; j < TP; ++j) {
+            if constexpr (first) mma_bf16_16816_first(acc[j][n], a[j][0], a[j][1], a[j][2], a[j][3], b.x, b.y);
+            else mma_bf16_16816(acc[j][n], a[j][0], a[j][1], a[j][2], a[j][3], b.x, b.y);
+            mma_bf16_16816(acc[j][n], a[j][4], a[j][5], a[j][6], a[j][7], b.z, b.w);
+        }
+    }
+    if constexpr ((J * 32 + 32) % G == 0) {
+#pragma unroll
+        for (int j = 0; j < TP; ++j) {
+            const uint32_t w0 = d[j].s[0][gi >> 1], w1 = d[j].s[1][gi >> 1];
+            const float s0 = (gi & 1) ? bf16_hi(w0) : bf16_lo(w0), s1 = (gi & 1) ? bf16_hi(w1) : bf16_lo(w1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (SUMS) {                                        // fp32 16 + z: the bytes 0, 0, z, 0x41
+                    const float2 xs = *reinterpret_cast<const float2*>(xsum + (gi * NT + n) * 8);
+                    const float z0 = __uint_as_float(__byte_perm(d[j].z[0], 0x41000000u, 0x7044u | (gi << 8)));
+                    const float z1 = __uint_as_float(__byte_perm(d[j].z[1], 0x41000000u, 0x7044u | (gi << 8)));
+                    acc[j][n][0] = fmaf(-z0, xs.x, acc[j][n][0]);
+                    acc[j][n][1] = fmaf(-z0, xs.y, acc[j][n][1]);
+                    acc[j][n][2] = fmaf(-z1, xs.x, acc[j][n][2]);
+                    acc[j][n][3] = fmaf(-z1, xs.y, acc[j][n][3]);
+                }
+                y[j][n][0] = fmaf(s0, acc[j][n][0], y[j][n][0]);
+                y[j][n][1] = fmaf(s0, acc[j][n][1], y[j][n][1]);
+                y[j][n][2] = fmaf(s1, acc[j][n][2], y[j][n][2]);
+                y[j][n][3] = fmaf(s1, acc[j][n][3], y[j][n][3]);
+            }
+        }
+    }
+}
+// y += X * W over one k-block of TP tiles, which share the B operand.  x: the lane's 16 bytes (at 16 t) of the k-block's first row of
+// X; row_at[n]: bytes from there to the row of the lane's column of the n-th eight.  Rows past the last one read the last row instead:
+// columns of a product do not mix, and what such a column sums up is not stored.
+template <bool SUMS, int TP, int NT, int G>
+__device__ __forceinline__ void w4_step(float (&y)[TP][NT][4], const W4Block<G> (&d)[TP], const uint8_t* x, const int (&row_at)[NT],
+                                        const float* xsum) {
+    float acc[TP][NT][4];
+    uint32_t zc[TP][2];
+    w4_sub_block<0, SUMS, TP, NT, G>(y, acc, zc, d, x, row_at, xsum);
+    w4_sub_block<1, SUMS, TP, NT, G>(y, acc, zc, d, x, row_at, xsum);
+    w4_sub_block<2, SUMS, TP, NT, G>(y, acc, zc, d, x, row_at, xsum);
+    w4_sub_block<3, SUMS, TP, NT, G>(y, acc, zc, d, x, row_at, xsum);
+}
+// Two terms of the gated product: the down projection reads 16 bits of its significand.  An infinite h has lo = 0 (not
+// inf - inf), a NaN stays in hi.
+__device__ __forceinline__ void w4_store_terms(bf16* out, int64_t at, int64_t term, float h) {
+    const bf16 hi = __float2bfloat16_rn(h);
+    const float rest = h - __bfloat162float(hi);
+    out[at] = hi;
+    out[at + term] = __float2bfloat16_rn(fabsf(rest) < __int_as_float(0x7F800000) ? rest : 0.0f);
+}
+
+// ------------------------------------------------------------------ up to 16 rows of X: a persistent stream
+// One CTA of 16 warps per SM.  A team of GW warps walks over column tiles; its warps deal out the pairs of k-blocks of a tile (gated:
+// half of them those of the gate tile, half those of the up tile), each with a ring of its own in shared memory that asynchronous
+// copies fill, across tiles too, so that the stream of codes does not pause at a tile's end.  (Held in registers instead, the loads of
+// several stages shared the few scoreboards of a warp.)  X stays in shared memory for the whole kernel, with its sums over the groups;
+// only the sums of a tile cross the warps of a team.
+constexpr int kW4StreamWarps = 16;
+__host__ __device__ constexpr int w4_ring_depth(int nt) { return nt == 1 ? 3 : 2; }      // slots; two columns of eight need the room for X
+constexpr int kW4StreamThreads = 32 * kW4StreamWarps;
+// Shared memory: sums of the tiles, rings, sums of X over its groups, X.
+__host__ __device__ constexpr uint32_t w4_stream_fixed_bytes(int nt, int G) {
+    return (uint32_t)kW4StreamWarps * (16u * 8u * 4u + (uint32_t)(w4_ring_depth(nt) * w4_slot_bytes(G, 2)));
+}
+__host__ __device__ constexpr uint64_t w4_stream_bytes(int rows, int KB, int G) {
+    const int nt = rows <= 8 ? 1 : 2;
+    return w4_stream_fixed_bytes(nt, G) + (uint64_t)KB * (128 / G) * nt * 32 + (uint64_t)rows * ((uint64_t)KB * 256 + 64);
+}
 
 template <int NT, int G, bool GATED>
-__global__ void __launch_bounds__(kW4Threads, NT <= 2 ? 2 : 1) w4_gemm_kernel(const W4GemmArgs p)
+__global__ void __launch_bounds__(kW4StreamThreads, 1) w4_stream_kernel(const W4GemmArgs p)
 {
     extern __shared__ __align__(128) uint8_t w4_smem[];
-    constexpr int PF = w4_prefetch(NT);
-    constexpr int NG = 128 / G;
+    constexpr int WARPS = kW4StreamWarps, NG = 128 / G, SLOT = w4_slot_bytes(G, 2), DEPTH = w4_ring_depth(NT);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    // GW and KW are powers of two; a team is GW neighbouring warps, KW of them share the k-blocks of one tile
+    const int GW = p.group_warps, KW = GATED ? GW >> 1 : GW, team = warp / GW, wk = warp & (KW - 1);
+    const int KP = p.KB >> 1, mine = (KP - wk + KW - 1) / KW;                // this warp's pairs of k-blocks: wk, wk + KW, ...
+    const int walkers = (int)gridDim.x * (WARPS / GW), R = p.M * p.terms;
+    const bool has_zeros = p.w[0].zeros != nullptr;
+    int tile = (int)blockIdx.x + team * (int)gridDim.x;
+
+    const int x_stride = p.KB * 256 + 64;
+    float* red = reinterpret_cast<float*>(w4_smem);                          // [WARPS][16][8]
+    uint8_t* ring = w4_smem + WARPS * 512 + warp * (DEPTH * SLOT);
+    float* xsums = reinterpret_cast<float*>(w4_smem + w4_stream_fixed_bytes(NT, G));       // [KB * NG][NT * 8]
+    uint8_t* xs = reinterpret_cast<uint8_t*>(xsums + p.KB * NG * NT * 8);
+
+    // the next pair of k-blocks to ask for; one commit group per call, empty at the end of the stream
+    const bool up = GATED && (warp & KW);
+    const W4Operand operand = {up ? p.w[1].codes : p.w[0].codes, up ? p.w[1].scales : p.w[0].scales, up ? p.w[1].zeros : p.w[0].zeros};
+    W4Source from = w4_source<2>(operand, (int64_t)tile * p.KB + 2 * wk, lane, NG);
+    const bool params = from.params != nullptr;
+    const uint32_t param_block = w4_param_bytes<2>(lane, NG);
+    const uint32_t jump = (uint32_t)(walkers * p.KB - 2 * (mine - 1) * KW);  // k-blocks from a tile's last pair to the next tile's first
+    const uint32_t code_by = 2048u * KW, code_jump = 1024u * jump, param_by = 2 * param_block * KW, param_jump = param_block * jump;
+    int next_i = mine, left = mine > 0 && tile < p.n16 ? mine * ((p.n16 - 1 - tile) / walkers + 1) : 0;
+    uint32_t next_to = ptx::smem_addr(ring) + lane * 16;
+    const uint32_t ring_end = next_to + DEPTH * SLOT;
+    auto ask = [&]() {
+        if (left > 0) {
+            --left;
+            w4_copy_blocks<2>(next_to, from, params);
+            const bool wrap = --next_i == 0;
+            from.codes += wrap ? code_jump : code_by;
+            from.params += wrap ? param_jump : param_by;
+            if (wrap) next_i = mine;
+        }
+        next_to += SLOT;
+        if (next_to == ring_end) next_to -= DEPTH * SLOT;
+        cp_async_commit();
+    };
+    if (!p.early) ptx::grid_dependency_wait();
+    for (int i = 0; i < DEPTH - 1; ++i) ask();
+    if (p.early) ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    {
+        const uint32_t x_at = ptx::smem_addr(xs);
+        for (int row = 0; row < R; ++row)
+            for (int i = threadIdx.x; i < p.KB * 16; i += 32 * WARPS) {
+                const bool in = i * 8 < p.K;
+                cp_async_16_zfill(x_at + row * x_stride + i * 16, p.X + (int64_t)row * p.K + (in ? i * 8 : 0), in ? 16u : 0u);
+            }
+    }
+    cp_async_wait_all();
+    __syncthreads();
+    // Sums of X over the groups, four lanes each; columns past the last row hold the last row's, like the operand itself.  Where X is
+    // not finite or so large that (16 + z) times a sum might not be, the zero points come off before the product instead.
+    bool large = false;
+    const bool two = NT == 2 && p.terms == 2;
+    auto row_of = [&](int n, int c) { return two ? n * p.M + min(c, p.M - 1) : min(n * 8 + c, R - 1); };
+    for (int i = threadIdx.x; i < p.KB * NG * NT * 32; i += 32 * WARPS) {
+        const int part = i & 3, c = (i >> 2) & 7, rest = i >> 5, n = rest % NT, group = rest / NT;
+        const uint8_t* at = xs + row_of(n, c) * x_stride + group * (2 * G) + part * 16;
+        float v = 0.0f, most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < G / 32; ++k) {
+            const uint4 u = *reinterpret_cast<const uint4*>(at + k * 64);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = bf16_lo(w[e]), b = bf16_hi(w[e]);
+                v += a + b;
+                most += fabsf(a) + fabsf(b);
+            }
+        }
+        large = large || !(most < 1e30f);
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+        if (part == 0) xsums[rest * 8 + c] = v;
+    }
+    large = __syncthreads_or(large);
+
+    // two terms in two columns of eight: the lo terms take the second, so that both sums of a token lie in one lane
+    auto team_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(GW * 32) : "memory"); };
+    int row_at[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row_at[n] = row_of(n, g) * x_stride;
+    const uint8_t* x0 = xs + t * 16 + wk * 512;
+    const float* xsum0 = xsums + wk * (2 * NG * NT * 8) + 2 * t;
+    const uint8_t *slot = ring, *slot_end = ring + DEPTH * SLOT;
+
+    for (; tile < p.n16; tile += walkers) {
+        float y[1][NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[0][n][e] = 0.0f;
+        const uint8_t* x = x0;
+        const float* xsum = xsum0;
+        for (int i = 0; i < mine; ++i) {
+            cp_async_wait_but<DEPTH - 2>();   // this step's copies have landed,
+            __syncwarp();                            // every lane's, and the slot of the step before is free
+            ask();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                W4Block<G> d[1];
+                w4_read_block<G, 2>(d[0], slot, h, lane, has_zeros);
+                if (!large) w4_step<true, 1, NT, G>(y, d, x + h * 256, row_at, xsum + h * (NG * NT * 8));
+                else w4_step<false, 1, NT, G>(y, d, x + h * 256, row_at, nullptr);
+            }
+            slot += SLOT;
+            if (slot == slot_end) slot = ring;
+            x += KW * 512;
+            xsum += KW * (2 * NG * NT * 8);
+        }
+        if (two) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[0][0][e] += y[0][NT - 1][e];
+        }
+        // sums over the warps in a fixed order, one column of eight rows at a time
+        const int columns = two ? 1 : (R + 7) / 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (n >= columns) break;
+            team_sync();                             // what lay there before has been read
+            float* at = red + (warp * 16 + g) * 8 + 2 * t;
+            *reinterpret_cast<float2*>(at) = make_float2(y[0][n][0], y[0][n][1]);
+            *reinterpret_cast<float2*>(at + 8 * 8) = make_float2(y[0][n][2], y[0][n][3]);
+            team_sync();
+            const bool folded = p.terms == 2 && !two;                        // up to 4 tokens: the lo terms are columns M ..
+            const int tokens = p.terms == 2 ? p.M : min(8, p.M - n * 8);
+            for (int o = (warp & (GW - 1)) * 32 + lane; o < 16 * tokens; o += GW * 32) {
+                const int r = o & 15, m = o >> 4, col = tile * 16 + r;
+                auto sum = [&](int first_warp) {
+                    const float* e = red + (first_warp * 16 + r) * 8 + m;
+                    float v = 0.0f;
+#pragma unroll 4
+                    for (int w = 0; w < KW; ++w) v += e[w * 128];
+                    if (folded) {
+                        float lo = 0.0f;
+#pragma unroll 4
+                        for (int w = 0; w < KW; ++w) lo += e[w * 128 + p.M];
+                        v += lo;
+                    }
+                    return v;
+                };
+                if (col < p.N) {
+                    const int64_t to = (int64_t)(n * 8 + m) * p.N + col;
+                    if constexpr (GATED) w4_store_terms(p.out, to, (int64_t)p.M * p.N, gate_act_f32(sum(team * GW), p.act) * sum(team * GW + KW));
+                    else p.out[to] = __float2bfloat16_rn(sum(team * GW));
+                }
+            }
+        }
+    }
+    cp_async_wait_all();
+}
+
+// ------------------------------------------------------------------ more rows of X, or X too large to stay: tiles
+// The 8 warps of a CTA are WR groups of two column tiles (gated: of a gate and an up tile) x WK ranges of K; stages of WK k-blocks of
+// codes and X pass through shared memory, three deep.  Up to 32 rows of X per CTA (blockIdx.y: further rows, which read the codes
+// again, from L2: by then the products set the time), and K over a cluster of C CTAs that add their sums in distributed shared memory.
+constexpr int kW4Stages = 3;
+__host__ __device__ constexpr int w4_red_stride(int nt) { return 8 * (nt | 1); }      // floats; odd multiples of 8 spread the banks
+__host__ __device__ constexpr uint32_t w4_tile_smem(int nt, int rows, int wk, int G) {
+    const uint32_t red = 8u * 32u * (uint32_t)w4_red_stride(nt) * 4u;
+    const uint32_t stages = kW4Stages * ((uint32_t)rows * (uint32_t)(wk * 256 + 64) + 16u * (uint32_t)w4_slot_bytes(G, 1));
+    return stages > red ? stages : red;
+}
+
+// NT: columns of eight rows of X (tokens times terms).
+template <int NT, int G, bool GATED>
+__global__ void __launch_bounds__(kW4Threads, 2) w4_tile_kernel(const W4GemmArgs p)
+{
+    extern __shared__ __align__(128) uint8_t w4_smem[];
+    constexpr int NG = 128 / G, BLOCK = w4_slot_bytes(G, 1);
     const uint32_t smem = ptx::smem_addr(w4_smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int WR = 1 << p.wr_log2, wk_log2 = 3 - p.wr_log2, WK = 1 << wk_log2;
@@ -126,83 +470,60 @@ __global__ void __launch_bounds__(kW4Threads, NT <= 2 ? 2 : 1) w4_gemm_kernel(co
     const int kb0 = (int)((int64_t)p.KB * rank / C), kb1 = (int)((int64_t)p.KB * (rank + 1) / C);
     const int steps = (kb1 - kb0 + WK - 1) >> wk_log2;                       // of the CTA (for its barriers)
     const int mine = (kb1 - kb0 - wk + WK - 1) >> wk_log2;                   // of this warp
+    const int m0 = (int)blockIdx.y * p.m_cta, M = min(p.m_cta, p.M - m0), R = M * p.terms;
+    const bool has_zeros = p.w[0].zeros != nullptr;
+    const uint32_t param_block = w4_param_bytes<1>(lane, NG);
 
-    const uint8_t* codes[2];
-    const bf16* scales[2];
-    const uint8_t* zeros[2];
-    bool have[2];
+    W4Source from[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int tile = GATED ? group * WR + wr : (group * WR + wr) * 2 + j;
-        const W4Operand& w = p.w[GATED ? j : 0];
-        have[j] = tile < p.n16;
-        const int64_t block = (int64_t)(have[j] ? tile : 0) * p.KB + kb0 + wk;
-        codes[j] = w.codes + block * 1024 + lane * 16;
-        scales[j] = w.scales + (block * 16 + g) * NG;
-        zeros[j] = w.zeros == nullptr ? nullptr : w.zeros + (block * 16 + g) * NG;
+    for (int j = 0; j < 2; ++j) {                    // a tile past the last column reads the last tile again; its sums are not stored
+        const int tile = min(GATED ? group * WR + wr : (group * WR + wr) * 2 + j, p.n16 - 1);
+        from[j] = w4_source<1>(p.w[GATED ? j : 0], (int64_t)tile * p.KB + kb0 + wk, lane, NG);
     }
-    W4Stage<G> st[PF];
-    auto fetch = [&](W4Stage<G>& d, int i) {
-        const int64_t b = (int64_t)i << wk_log2;                             // k-blocks from the warp's first one
+    const bool params = from[0].params != nullptr;
+    const int x_stride = WK * 256 + 64, x_bytes = p.m_cta * p.terms * x_stride, stage_bytes = x_bytes + 16 * BLOCK;
+    auto ask_codes = [&](int s, int slot) {
+        if (s >= mine) return;
+        const uint32_t to = smem + slot * stage_bytes + x_bytes + warp * 2 * BLOCK + lane * 16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (!have[j]) continue;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                d.c[j][h] = ld_once_16B(codes[j] + b * 1024 + h * 512);
-                const bf16* s = scales[j] + (b * 16 + h * 8) * NG;
-                if constexpr (G == 32) {
-                    const uint2 v = ld_8B(s);
-                    d.s[j][h][0] = v.x;
-                    d.s[j][h][1] = v.y;
-                } else if constexpr (G == 64) {
-                    d.s[j][h][0] = ld_4B(s);
-                } else {
-                    d.s[j][h][0] = ld_2B(s);
-                }
-                if (zeros[j] != nullptr) {
-                    const uint8_t* z = zeros[j] + (b * 16 + h * 8) * NG;
-                    if constexpr (G == 32) d.z[j][h] = ld_4B(z);
-                    else if constexpr (G == 64) d.z[j][h] = ld_2B(z);
-                    else d.z[j][h] = ld_1B(z);
-                } else {
-                    d.z[j][h] = 0x08080808u;
-                }
-            }
+        for (int j = 0; j < 2; ++j) {                // called for s = 0, 1, 2, ... in turn
+            w4_copy_blocks<1>(to + j * BLOCK, from[j], params);
+            from[j].codes += (int64_t)1024 << wk_log2;
+            from[j].params += (int64_t)param_block << wk_log2;
         }
+    };
+    // 16-byte pieces of X: a thread keeps its column of a stage and takes every row_by-th row
+    const int pieces_log2 = wk_log2 + 4, row_by = kW4Threads >> pieces_log2, x_row = threadIdx.x >> pieces_log2;
+    const int x_col = threadIdx.x & ((1 << pieces_log2) - 1);
+    const bf16* x_from = p.X + (int64_t)(m0 + x_row) * p.K + kb0 * 128 + x_col * 8;        // stages are asked for in turn
+    int x_k = kb0 * 128 + x_col * 8;
+    const int64_t x_by = (int64_t)row_by * p.K, lo_jump = (int64_t)(p.M - M) * p.K;
+    const uint32_t x_to = smem + x_row * x_stride + x_col * 16;
+    auto ask_x = [&](int s, int slot) {
+        if (s >= steps) return;
+        const bool in = x_k < p.K;
+        const bf16* from_row = in ? x_from : p.X;
+        uint32_t to = x_to + slot * stage_bytes;
+        for (int row = x_row; row < R; row += row_by) {
+            cp_async_16_zfill(to, in && row >= M ? from_row + lo_jump : from_row, in ? 16u : 0u);
+            if (in) from_row += x_by;
+            to += row_by * x_stride;
+        }
+        x_from += 128 << wk_log2;
+        x_k += 128 << wk_log2;
     };
     if (!p.early) ptx::grid_dependency_wait();
-#pragma unroll
-    for (int i = 0; i < PF; ++i) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {            // a tile past the last column computes on zeros, which are not stored
-                st[i].c[j][h] = make_uint4(0, 0, 0, 0);
-                st[i].s[j][h][0] = 0;
-                if constexpr (G == 32) st[i].s[j][h][1] = 0;
-                st[i].z[j][h] = 0;
-            }
-        if (i < mine) fetch(st[i], i);
+    ask_codes(0, 0);
+    if (p.early) {
+        ask_codes(1, 1);
+        ptx::grid_dependency_wait();
     }
-    if (p.early) ptx::grid_dependency_wait();
     ptx::launch_dependents();
-
-    // X: chunks of `chunk` steps, double buffered when there is more than one
-    const int chunk = max(p.chunk, 1), row_pieces = (chunk << wk_log2) * 16;                       // 16-byte pieces of a row
-    const uint32_t x_stride = (uint32_t)row_pieces * 16u + 64u;                            // + 64: conflict-free quarter warps
-    const uint32_t buf_bytes = x_stride * (uint32_t)(p.M * p.terms);
-    auto load_x = [&](int step0, int buf) {
-        const int kfirst = (kb0 + (step0 << wk_log2)) * 128, klast = min(kb1 * 128, p.K);
-        const int pieces = p.M * p.terms * row_pieces;
-        for (int i = threadIdx.x; i < pieces; i += kW4Threads) {
-            const int row = i / row_pieces, col = i - row * row_pieces;
-            const int k = kfirst + col * 8;
-            const bool in = k < klast;
-            cp_async_16_zfill(smem + buf * buf_bytes + row * x_stride + col * 16, p.X + (int64_t)row * p.K + (in ? k : 0), in ? 16u : 0u);
-        }
-    };
-    load_x(0, 0);
+    ask_x(0, 0);
+    cp_async_commit();
+    if (!p.early) ask_codes(1, 1);
+    ask_x(1, 1);
+    cp_async_commit();
 
     float y[2][NT][4];
 #pragma unroll
@@ -211,91 +532,29 @@ __global__ void __launch_bounds__(kW4Threads, NT <= 2 ? 2 : 1) w4_gemm_kernel(co
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[j][n][e] = 0.0f;
+    int row_at[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row_at[n] = min(n * 8 + g, R - 1) * x_stride;
 
-    auto step = [&](const W4Stage<G>& d, const uint8_t* xaddr) {            // xaddr: the lane's bytes of row g in this k-block
-        float acc[2][NT][4];
-        uint32_t zc[2][2];
-        auto sub_block = [&](auto jc) {
-            constexpr int J = decltype(jc)::value;                           // 32 of the 128 k
-            if constexpr ((J * 32) % G == 0) {
-                constexpr int gi = J * 32 / G;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) zc[j][h] = (((d.z[j][h] >> (8 * gi)) & 15u) * 0x00010001u) | 0x43004300u;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][n][e] = 0.0f;
-                }
-            }
-            uint32_t a[2][8];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t lo[4] = {d.c[j][0].x, d.c[j][0].y, d.c[j][0].z, d.c[j][0].w};
-                const uint32_t hi[4] = {d.c[j][1].x, d.c[j][1].y, d.c[j][1].z, d.c[j][1].w};
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int at = (u >> 1) * 4 + (u & 1) * 2;
-                    a[j][at] = codes_to_bf16x2<4 * J>(lo[u], zc[j][0]);
-                    a[j][at + 1] = codes_to_bf16x2<4 * J>(hi[u], zc[j][1]);
-                }
-            }
-            for (int term = 0; term < p.terms; ++term) {
-                const uint8_t* xt = xaddr + (uint32_t)(term * p.M) * x_stride + J * 64;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint4 b = make_uint4(0, 0, 0, 0);
-                    if (n * 8 + g < p.M) b = *reinterpret_cast<const uint4*>(xt + (uint32_t)(n * 8) * x_stride);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        mma_bf16_16816(acc[j][n], a[j][0], a[j][1], a[j][2], a[j][3], b.x, b.y);
-                        mma_bf16_16816(acc[j][n], a[j][4], a[j][5], a[j][6], a[j][7], b.z, b.w);
-                    }
-                }
-            }
-            if constexpr ((J * 32 + 32) % G == 0) {
-                constexpr int gi = J * 32 / G;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t w0 = d.s[j][0][gi >> 1], w1 = d.s[j][1][gi >> 1];
-                    const float s0 = (gi & 1) ? bf16_hi(w0) : bf16_lo(w0), s1 = (gi & 1) ? bf16_hi(w1) : bf16_lo(w1);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        y[j][n][0] = fmaf(s0, acc[j][n][0], y[j][n][0]);
-                        y[j][n][1] = fmaf(s0, acc[j][n][1], y[j][n][1]);
-                        y[j][n][2] = fmaf(s1, acc[j][n][2], y[j][n][2]);
-                        y[j][n][3] = fmaf(s1, acc[j][n][3], y[j][n][3]);
-                    }
-                }
-            }
-        };
-        sub_block(std::integral_constant<int, 0>{});
-        sub_block(std::integral_constant<int, 1>{});
-        sub_block(std::integral_constant<int, 2>{});
-        sub_block(std::integral_constant<int, 3>{});
-    };
-
-    int buf = 0;
-    for (int c0 = 0; c0 < steps; c0 += chunk) {
-        cp_async_wait_all();
-        __syncthreads();
-        if (c0 + chunk < steps) load_x(c0 + chunk, buf ^ 1);
-        const uint8_t* x0 = w4_smem + buf * buf_bytes + g * x_stride + t * 16 + (uint32_t)wk * 256u;
-        const int end = min(chunk, mine - c0);
-        for (int i = 0; i < end; i += PF) {          // chunk is a multiple of PF wherever there are several chunks
-#pragma unroll
-            for (int q = 0; q < PF; ++q) {
-                if (i + q < end) {
-                    step(st[q], x0 + ((uint32_t)(i + q) << (8 + wk_log2)));
-                    if (c0 + i + q + PF < mine) fetch(st[q], c0 + i + q + PF);
-                }
-            }
+    for (int s = 0, slot = 0; s < steps; ++s) {
+        cp_async_wait_but<1>();
+        __syncthreads();                             // this stage has landed, the one before it has been read
+        const int next = slot == 0 ? 2 : slot - 1;
+        ask_codes(s + 2, next);
+        ask_x(s + 2, next);
+        cp_async_commit();
+        if (s < mine) {
+            const uint8_t* stage = w4_smem + slot * stage_bytes;
+            W4Block<G> d[2];
+            w4_read_block<G, 1>(d[0], stage + x_bytes + warp * 2 * BLOCK, 0, lane, has_zeros);
+            w4_read_block<G, 1>(d[1], stage + x_bytes + warp * 2 * BLOCK + BLOCK, 0, lane, has_zeros);
+            w4_step<false, 2, NT, G>(y, d, stage + wk * 256 + t * 16, row_at, nullptr);
         }
-        buf ^= 1;
+        if (++slot == kW4Stages) slot = 0;
     }
 
     // partial sums of the warps that share columns, then of the CTAs of the cluster, each in a fixed order
+    cp_async_wait_all();
     __syncthreads();
     constexpr int S = w4_red_stride(NT);
     float* red = reinterpret_cast<float*>(w4_smem);                          // [WK][WR * 32][S]
@@ -310,50 +569,47 @@ __global__ void __launch_bounds__(kW4Threads, NT <= 2 ? 2 : 1) w4_gemm_kernel(co
             }
     }
     __syncthreads();
-    const int rows = WR * 32, total = rows * p.M, rows_log2 = p.wr_log2 + 5;
-    const int part = rows * S;
+    const int rows = WR * 32, rows_log2 = p.wr_log2 + 5, part = rows * S;
+    auto own = [&](int row, int m) {                                         // this CTA's sum, terms and warps
+        const float* e = red + row * S + m;
+        float v = e[0];
+        for (int w = 1; w < WK; ++w) v += e[w * part];
+        if (p.terms == 2) {
+            e += M;
+            float lo = e[0];
+            for (int w = 1; w < WK; ++w) lo += e[w * part];
+            v += lo;
+        }
+        return v;
+    };
     if (C > 1) {
-        for (int i = threadIdx.x; i < total; i += kW4Threads) {
-            float* e = red + (i & (rows - 1)) * S + (i >> rows_log2);
-            float v = e[0];
-            for (int w = 1; w < WK; ++w) v += e[w * part];
-            e[0] = v;
+        // every element is read and replaced by one thread; a token's lo term is only read by that thread
+        for (int i = threadIdx.x; i < rows * M; i += kW4Threads) {
+            const int row = i & (rows - 1), m = i >> rows_log2;
+            red[row * S + m] = own(row, m);
         }
         __syncwarp();
         ptx::cluster_sync();
     }
     auto sum = [&](int row, int m) {
-        float v;
-        if (C > 1) {
-            const uint32_t at = smem + (uint32_t)(row * S + m) * 4u;
-            v = ld_cluster_f32(ptx::map_to_cta(at, 0));
-            for (int r = 1; r < C; ++r) v += ld_cluster_f32(ptx::map_to_cta(at, (uint32_t)r));
-        } else {
-            const float* e = red + row * S + m;
-            v = e[0];
-            for (int w = 1; w < WK; ++w) v += e[w * part];
-        }
+        if (C == 1) return own(row, m);
+        const uint32_t at = smem + (uint32_t)(row * S + m) * 4u;
+        float v = ld_cluster_f32(ptx::map_to_cta(at, 0));
+        for (int r = 1; r < C; ++r) v += ld_cluster_f32(ptx::map_to_cta(at, (uint32_t)r));
         return v;
     };
-    const int outputs = GATED ? total >> 1 : total, out_log2 = GATED ? rows_log2 - 1 : rows_log2;
+    const int out_log2 = GATED ? rows_log2 - 1 : rows_log2, outputs = M << out_log2;
     const int first = (int)((int64_t)outputs * rank / C), last = (int)((int64_t)outputs * (rank + 1) / C);
     for (int i = first + threadIdx.x; i < last; i += kW4Threads) {
         const int r = i & ((1 << out_log2) - 1), m = i >> out_log2;
         const int n = (group << out_log2) + r;
         if (n >= p.N) continue;
+        const int64_t at = (int64_t)(m0 + m) * p.N + n;
         if constexpr (GATED) {
             const int row = (r >> 4) * 32 + (r & 15);
-            const float gate = sum(row, m), up = sum(row + 16, m);
-            const float h = gate_act_f32(gate, p.act) * up;
-            // two terms: the down projection reads 16 bits of the product's significand.  An infinite h has lo = 0 (not
-            // inf - inf), a NaN stays in hi.
-            const bf16 hi = __float2bfloat16_rn(h);
-            const float rest = h - __bfloat162float(hi);
-            const int64_t at = (int64_t)m * p.N + n;
-            p.out[at] = hi;
-            p.out[(int64_t)p.M * p.N + at] = __float2bfloat16_rn(fabsf(rest) < __int_as_float(0x7F800000) ? rest : 0.0f);
+            w4_store_terms(p.out, at, (int64_t)p.M * p.N, gate_act_f32(sum(row, m), p.act) * sum(row + 16, m));
         } else {
-            p.out[(int64_t)m * p.N + n] = __float2bfloat16_rn(sum(r, m));
+            p.out[at] = __float2bfloat16_rn(sum(r, m));
         }
     }
     __syncwarp();
@@ -415,7 +671,7 @@ w4_pack_kernel(const void* src, int out_in, const bf16* scales_in, const uint8_t
                uint8_t* codes, bf16* scales, uint8_t* zeros, int K, int N, int G)
 {
     ptx::grid_dependency_wait();
-    const int n = blockIdx.x * 128 + threadIdx.x, kb = blockIdx.y, KB = (K + 127) / 128, n16 = (N + 15) / 16;
+    const int n = blockIdx.x * 128 + threadIdx.x, kb = blockIdx.y, KB = gridDim.y, n16 = (N + 15) / 16;
     if (n >= n16 * 16) return;
     const int ng = 128 / G;
     const int64_t block = (int64_t)(n >> 4) * KB + kb;
@@ -466,9 +722,11 @@ w4_pack_kernel(const void* src, int out_in, const bf16* scales_in, const uint8_t
         }
         const int64_t at = (block * 16 + (n & 15)) * ng + gi;
         scales[at] = __float2bfloat16_rn(s);
-        if (zeros != nullptr) zeros[at] = (uint8_t)z;
+        if (zeros != nullptr) zeros[at] = (uint8_t)(0x80 | ((int)z << 3));
     }
     uint8_t* out = codes + block * 1024 + ((n & 15) >> 3) * 512 + (n & 7) * 64;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) word[j] = __funnelshift_l(word[j], word[j], 3);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         reinterpret_cast<uint4*>(out)[j] = make_uint4(word[4 * j], word[4 * j + 1], word[4 * j + 2], word[4 * j + 3]);
@@ -479,13 +737,14 @@ w4_unpack_kernel(const uint8_t* codes, const bf16* scales, const uint8_t* zeros,
                  bf16* W, int out_in, int K, int N, int G)
 {
     ptx::grid_dependency_wait();
-    const int n = blockIdx.x * 128 + threadIdx.x, kb = blockIdx.y, KB = (K + 127) / 128, ng = 128 / G;
+    const int n = blockIdx.x * 128 + threadIdx.x, kb = blockIdx.y, KB = gridDim.y, ng = 128 / G;
     if (n >= N) return;
     const int64_t block = (int64_t)(n >> 4) * KB + kb;
-    const uint16_t* unit = reinterpret_cast<const uint16_t*>(codes + block * 1024 + ((n & 15) >> 3) * 512 + (n & 7) * 64);
+    const uint32_t* word = reinterpret_cast<const uint32_t*>(codes + block * 1024 + ((n & 15) >> 3) * 512 + (n & 7) * 64);
     for (int k = 0; k < 128 && kb * 128 + k < K; ++k) {
         const int64_t at = (block * 16 + (n & 15)) * ng + k / G;
-        const float q = (float)((unit[k & 31] >> (4 * (k >> 5))) & 15), z = zeros != nullptr ? (float)zeros[at] : 8.0f;
+        const uint32_t w = __funnelshift_r(word[(k & 31) >> 1], word[(k & 31) >> 1], 3);
+        const float q = (float)((w >> (4 * (k >> 5) + 16 * (k & 1))) & 15), z = zeros != nullptr ? (float)((zeros[at] >> 3) & 15) : 8.0f;
         const int64_t to = out_in ? (int64_t)n * K + kb * 128 + k : (int64_t)(kb * 128 + k) * N + n;
         W[to] = __float2bfloat16_rn((q - z) * __bfloat162float(scales[at]));
     }

@@ -206,7 +206,7 @@ def lib() -> ctypes.CDLL:
         L.gmlp_w4_workspace_bytes.restype = u64
         L.gmlp_w4_workspace_bytes.argtypes = [i64, i64, i64, u32]
         L.gmlp_w4_plan.restype = ctypes.c_int
-        L.gmlp_w4_plan.argtypes = [i64, i32, i64, i64, i32, i32, ctypes.POINTER(i32)]
+        L.gmlp_w4_plan.argtypes = [i64, i32, i64, i64, i32, i32, i32, ctypes.POINTER(i32)]
         L.gmlp_kv4_workspace_bytes.restype = u64
         L.gmlp_kv4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
         L.gmlp_autotune.restype = ctypes.c_int
@@ -686,26 +686,36 @@ def sum_partials(parts, Y=None, stream=None) -> "torch.Tensor":
 
 # ---------------------------------------------------------------------------------------------- 4-bit weights and cache
 
-def _on_one_device(device, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
-
-
-def _check_tensor(t, name: str, dtype, shape) -> None:
+def _pointer(t, name: str, dtype, shape, device) -> int:
+    """The address of a contiguous tensor of this type, shape and device; raises what the mismatch calls for.  (These calls
+    take a few microseconds on the GPU: the good case is one line.)"""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA {dtype} tensor")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+
+
+def _workspace(workspace, n: int, device, stream):
+    """(tensor, address, bytes) of the caller's workspace, or of one for this call; the tensor has to outlive the launch."""
+    if workspace is None:
+        if n == 0:
+            return None, None, 0
+        workspace = _empty(n, torch.uint8, device, stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _run(entry, args, device) -> None:
     """One library call with `device` current."""
     if torch.cuda.current_device() == device.index:
-        rc = entry(ctypes.byref(args))
+        rc = entry(args)
     else:
         with torch.cuda.device(device):
-            rc = entry(ctypes.byref(args))
+            rc = entry(args)
     if rc != OK:
         raise GmlpError(rc)
 
@@ -719,7 +729,7 @@ def _empty(shape, dtype, device, stream):
 
 
 def _stream_handle(stream, device) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
 class W4Matrix:
@@ -731,14 +741,14 @@ class W4Matrix:
 
     def __init__(self, codes, scales, zeros, K: int, N: int, group: int):
         n_codes, n_scales = w4_sizes(K, N, group)
-        _check_tensor(codes, "codes", torch.uint8, (n_codes,))
-        _check_tensor(scales, "scales", torch.bfloat16, (n_scales,))
-        if zeros is not None:
-            _check_tensor(zeros, "zeros", torch.uint8, (n_scales,))
-        _on_one_device(codes.device, scales=scales, zeros=zeros)
+        device = codes.device
+        pointers = (_pointer(codes, "codes", torch.uint8, (n_codes,), device), _pointer(scales, "scales", torch.bfloat16, (n_scales,), device),
+                    None if zeros is None else _pointer(zeros, "zeros", torch.uint8, (n_scales,), device))
+        if device.type != "cuda":
+            raise TypeError("codes: expected a CUDA tensor")
         self.codes, self.scales, self.zeros, self.K, self.N, self.group = codes, scales, zeros, K, N, group
-        self.device = codes.device
-        self.struct = GmlpW4Matrix(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), K, N, group, 0)
+        self.device = device
+        self.struct = GmlpW4Matrix(*pointers, K, N, group, 0)
 
 
 def w4_sizes(K: int, N: int, group: int):
@@ -756,10 +766,9 @@ def _w4_empty(K: int, N: int, group: int, zeros: bool, device, stream) -> W4Matr
                     _empty(n_scales, torch.uint8, device, stream) if zeros else None, K, N, group)
 
 
-def _w4_layout(entry, W, scales, zeros, m: W4Matrix, weights_out_in: bool, stream, checked: bool) -> None:
+def _w4_layout(entry, W: int, scales, zeros, m: W4Matrix, weights_out_in: bool, stream, checked: bool) -> None:
     a = GmlpW4LayoutArgs(ctypes.sizeof(GmlpW4LayoutArgs), (FLAG_CHECKED if checked else 0) | (FLAG_WEIGHTS_OUT_IN if weights_out_in else 0),
-                         W.data_ptr(), None if scales is None else scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
-                         m.struct, _stream_handle(stream, m.device))
+                         W, scales, zeros, m.struct, _stream_handle(stream, m.device))
     _run(entry, a, m.device)
 
 
@@ -772,7 +781,7 @@ def w4_quantize(W, group: int = 128, zero_points: bool = False, weights_out_in: 
         raise ValueError("W: expected a matrix")
     K, N = (W.shape[1], W.shape[0]) if weights_out_in else W.shape
     m = _w4_empty(K, N, group, zero_points, W.device, stream)
-    _w4_layout(lib().gmlp_w4_quantize, W, None, None, m, weights_out_in, stream, checked)
+    _w4_layout(lib().gmlp_w4_quantize, W.data_ptr(), None, None, m, weights_out_in, stream, checked)
     return m
 
 
@@ -786,13 +795,14 @@ def w4_pack(codes, scales, zeros=None, weights_out_in: bool = False, stream=None
     groups = scales.shape[axis]
     if groups < 1 or K % groups != 0:
         raise ValueError("shape mismatch: the number of scales must divide the number of input rows")
-    _check_tensor(codes, "codes", torch.uint8, (N, K) if weights_out_in else (K, N))
-    _check_tensor(scales, "scales", torch.bfloat16, (N, groups) if weights_out_in else (groups, N))
-    if zeros is not None:
-        _check_tensor(zeros, "zeros", torch.uint8, scales.shape)
-    _on_one_device(codes.device, scales=scales, zeros=zeros)
+    device = codes.device
+    if device.type != "cuda":
+        raise TypeError("codes: expected a CUDA tensor")
+    pointers = (_pointer(codes, "codes", torch.uint8, (N, K) if weights_out_in else (K, N), device),
+                _pointer(scales, "scales", torch.bfloat16, (N, groups) if weights_out_in else (groups, N), device),
+                None if zeros is None else _pointer(zeros, "zeros", torch.uint8, scales.shape, device))
     m = _w4_empty(K, N, K // groups, zeros is not None, codes.device, stream)
-    _w4_layout(lib().gmlp_w4_pack, codes, scales, zeros, m, weights_out_in, stream, checked)
+    _w4_layout(lib().gmlp_w4_pack, *pointers, m, weights_out_in, stream, checked)
     return m
 
 
@@ -801,9 +811,7 @@ def w4_dequantize(W4: W4Matrix, weights_out_in: bool = False, W=None, stream=Non
     shape = (W4.N, W4.K) if weights_out_in else (W4.K, W4.N)
     if W is None:
         W = _empty(shape, torch.bfloat16, W4.device, stream)
-    _check_tensor(W, "W", torch.bfloat16, shape)
-    _on_one_device(W4.device, W=W)
-    _w4_layout(lib().gmlp_w4_dequantize, W, None, None, W4, weights_out_in, stream, checked)
+    _w4_layout(lib().gmlp_w4_dequantize, _pointer(W, "W", torch.bfloat16, shape, W4.device), None, None, W4, weights_out_in, stream, checked)
     return W
 
 
@@ -811,24 +819,23 @@ def w4_matmul(X, W4: W4Matrix, Y=None, stream=None, checked: bool = False) -> to
     """gmlp_w4_matmul: Y = X W for a 4-bit W and up to W4_MAX_M rows of X."""
     if X.dim() != 2:
         raise ValueError("X: expected a matrix")
-    M = X.shape[0]
-    _check_tensor(X, "X", torch.bfloat16, (M, W4.K))
+    M, device = X.shape[0], W4.device
+    x = _pointer(X, "X", torch.bfloat16, (M, W4.K), device)
     if Y is None:
-        Y = _empty((M, W4.N), torch.bfloat16, X.device, stream)
+        Y = _empty((M, W4.N), torch.bfloat16, device, stream)
+        y = Y.data_ptr()
     else:
-        _check_tensor(Y, "Y", torch.bfloat16, (M, W4.N))
-    _on_one_device(W4.device, X=X, Y=Y)
-    a = GmlpW4MatmulArgs(ctypes.sizeof(GmlpW4MatmulArgs), FLAG_CHECKED if checked else 0, X.data_ptr(), Y.data_ptr(), M, W4.struct,
-                         _stream_handle(stream, X.device))
-    _run(lib().gmlp_w4_matmul, a, W4.device)
+        y = _pointer(Y, "Y", torch.bfloat16, (M, W4.N), device)
+    _run(lib().gmlp_w4_matmul, GmlpW4MatmulArgs(_SIZE_W4_MATMUL, FLAG_CHECKED if checked else 0, x, y, M, W4.struct,
+                                                _stream_handle(stream, device)), device)
     return Y
 
 
-def w4_plan(M: int, K: int, N: int, terms: int = 1, gated: bool = False, sm_count: int = 0):
-    """gmlp_w4_plan: (columns of eight tokens, column groups per CTA, CTAs per cluster, steps per chunk, steps, bytes of shared
-    memory, CTAs) of one product."""
-    out = (ctypes.c_int32 * 7)()
-    rc = lib().gmlp_w4_plan(M, terms, K, N, int(gated), sm_count, out)
+def w4_plan(M: int, K: int, N: int, group: int = 128, terms: int = 1, gated: bool = False, sm_count: int = 0):
+    """gmlp_w4_plan: (persistent kernel, columns of eight rows, warps of a team, column groups per CTA, CTAs per cluster, parts,
+    CTAs per part, bytes of shared memory) of one product."""
+    out = (ctypes.c_int32 * 8)()
+    rc = lib().gmlp_w4_plan(M, terms, K, N, int(gated), group, sm_count, out)
     if rc != OK:
         raise GmlpError(rc)
     return tuple(out)
@@ -844,21 +851,21 @@ def w4_forward(X, Wg: W4Matrix, Wu: W4Matrix, Wd: W4Matrix, Y=None, gamma=None, 
     forward().  ``workspace``: a uint8 tensor of at least w4_workspace_bytes(), by default allocated for the call."""
     if X.dim() != 2:
         raise ValueError("X: expected a matrix")
-    M = X.shape[0]
-    _check_tensor(X, "X", torch.bfloat16, (M, Wg.K))
+    M, device = X.shape[0], Wg.device
+    if Wu.device != device or Wd.device != device:
+        raise ValueError(f"Wu, Wd: expected matrices on {device}")
+    x = _pointer(X, "X", torch.bfloat16, (M, Wg.K), device)
     if Y is None:
-        Y = _empty((M, Wg.K), torch.bfloat16, X.device, stream)
+        Y = _empty((M, Wg.K), torch.bfloat16, device, stream)
+        y = Y.data_ptr()
     else:
-        _check_tensor(Y, "Y", torch.bfloat16, (M, Wg.K))
-    if gamma is not None:
-        _check_tensor(gamma, "gamma", torch.bfloat16, (Wg.K,))
-    if workspace is None:
-        workspace = _empty(max(256, w4_workspace_bytes(M, Wg.K, Wg.N, rmsnorm)), torch.uint8, X.device, stream)
-    _on_one_device(X.device, Y=Y, gamma=gamma, workspace=workspace, Wg=Wg, Wu=Wu, Wd=Wd)
-    a = GmlpW4Args(ctypes.sizeof(GmlpW4Args), (FLAG_RMSNORM if rmsnorm else 0) | (FLAG_CHECKED if checked else 0) | ACT_FLAGS[act],
-                   X.data_ptr(), Y.data_ptr(), M, Wg.struct, Wu.struct, Wd.struct, None if gamma is None else gamma.data_ptr(),
-                   eps, beta, _stream_handle(stream, X.device), workspace.data_ptr(), workspace.numel() * workspace.element_size(), 0)
-    _run(lib().gmlp_w4_forward, a, X.device)
+        y = _pointer(Y, "Y", torch.bfloat16, (M, Wg.K), device)
+    gain = None if gamma is None else _pointer(gamma, "gamma", torch.bfloat16, (Wg.K,), device)
+    flags = (FLAG_RMSNORM if rmsnorm else 0) | (FLAG_CHECKED if checked else 0) | ACT_FLAGS[act]
+    # one byte stands for no workspace where the sizes are refused anyway
+    keep, ws, ws_bytes = _workspace(workspace, lib().gmlp_w4_workspace_bytes(M, Wg.K, Wg.N, flags) or 1, device, stream)
+    _run(lib().gmlp_w4_forward, GmlpW4Args(_SIZE_W4, flags, x, y, M, Wg.struct, Wu.struct, Wd.struct, gain, eps, beta,
+                                           _stream_handle(stream, device), ws, ws_bytes, 0), device)
     return Y
 
 
@@ -874,18 +881,18 @@ class Kv4Cache:
                              "[n_pages, n_kv_heads, page_size, head_dim / group, 2]")
         n_pages, heads, page, half = k_codes.shape
         groups = k_params.shape[3]
-        for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
-            _check_tensor(t, name, torch.uint8, (n_pages, heads, page, half))
-        for t, name in ((k_params, "k_params"), (v_params, "v_params")):
-            _check_tensor(t, name, torch.bfloat16, (n_pages, heads, page, groups, 2))
-        _on_one_device(k_codes.device, k_params=k_params, v_codes=v_codes, v_params=v_params)
+        device, rows, pairs = k_codes.device, (n_pages, heads, page, half), (n_pages, heads, page, groups, 2)
+        pointers = [_pointer(t, name, dtype, shape, device) for t, name, dtype, shape in
+                    ((k_codes, "k_codes", torch.uint8, rows), (k_params, "k_params", torch.bfloat16, pairs),
+                     (v_codes, "v_codes", torch.uint8, rows), (v_params, "v_params", torch.bfloat16, pairs))]
+        if device.type != "cuda":
+            raise TypeError("k_codes: expected a CUDA tensor")
         if 2 * half % groups != 0:
             raise ValueError("the number of groups must divide head_dim")
         self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim, self.group = n_pages, heads, page, 2 * half, 2 * half // groups
-        self.device = k_codes.device
-        self.struct = GmlpKv4Cache(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(), n_pages, heads,
-                                   page, self.head_dim, self.group, 0)
+        self.device = device
+        self.struct = GmlpKv4Cache(*pointers, n_pages, heads, page, self.head_dim, self.group, 0)
 
 
 def kv4_cache(n_pages: int, n_kv_heads: int, head_dim: int = 128, page_size: int = 64, group: int = 64, device="cuda") -> Kv4Cache:
@@ -895,15 +902,9 @@ def kv4_cache(n_pages: int, n_kv_heads: int, head_dim: int = 128, page_size: int
     return Kv4Cache(codes(), params(), codes(), params())
 
 
-def _kv4_rows(entry, K, V, cache: Kv4Cache, slots, stream, checked: bool) -> None:
-    T = slots.shape[0]
-    _check_tensor(slots, "slots", torch.int64, (T,))
-    for t, name in ((K, "K"), (V, "V")):
-        _check_tensor(t, name, torch.bfloat16, (T, cache.n_kv_heads * cache.head_dim))
-    _on_one_device(cache.device, K=K, V=V, slots=slots)
-    a = GmlpKv4RowsArgs(ctypes.sizeof(GmlpKv4RowsArgs), FLAG_CHECKED if checked else 0, K.data_ptr(), V.data_ptr(), slots.data_ptr(), T,
-                        cache.struct, _stream_handle(stream, cache.device))
-    _run(entry, a, cache.device)
+def _kv4_rows(entry, K: int, V: int, cache: Kv4Cache, slots: int, T: int, stream, checked: bool) -> None:
+    _run(entry, GmlpKv4RowsArgs(_SIZE_KV4_ROWS, FLAG_CHECKED if checked else 0, K, V, slots, T, cache.struct,
+                                _stream_handle(stream, cache.device)), cache.device)
 
 
 def kv4_append(K, V, cache: Kv4Cache, slots, stream=None, checked: bool = False) -> None:
@@ -911,19 +912,24 @@ def kv4_append(K, V, cache: Kv4Cache, slots, stream=None, checked: bool = False)
     the row is skipped)."""
     if slots.dim() != 1:
         raise ValueError("slots: expected a vector")
-    _kv4_rows(lib().gmlp_kv4_append, K, V, cache, slots, stream, checked)
+    T, device = slots.shape[0], cache.device
+    shape = (T, cache.n_kv_heads * cache.head_dim)
+    _kv4_rows(lib().gmlp_kv4_append, _pointer(K, "K", torch.bfloat16, shape, device), _pointer(V, "V", torch.bfloat16, shape, device),
+              cache, _pointer(slots, "slots", torch.int64, (T,), device), T, stream, checked)
 
 
 def kv4_gather(cache: Kv4Cache, slots, K=None, V=None, stream=None, checked: bool = False):
     """gmlp_kv4_gather: the rows at ``slots`` as bf16 (K, V), each [T, n_kv_heads * head_dim]."""
     if slots.dim() != 1:
         raise ValueError("slots: expected a vector")
-    shape = (slots.shape[0], cache.n_kv_heads * cache.head_dim)
+    T, device = slots.shape[0], cache.device
+    shape = (T, cache.n_kv_heads * cache.head_dim)
     if K is None:
-        K = _empty(shape, torch.bfloat16, cache.device, stream)
+        K = _empty(shape, torch.bfloat16, device, stream)
     if V is None:
-        V = _empty(shape, torch.bfloat16, cache.device, stream)
-    _kv4_rows(lib().gmlp_kv4_gather, K, V, cache, slots, stream, checked)
+        V = _empty(shape, torch.bfloat16, device, stream)
+    _kv4_rows(lib().gmlp_kv4_gather, _pointer(K, "K", torch.bfloat16, shape, device), _pointer(V, "V", torch.bfloat16, shape, device),
+              cache, _pointer(slots, "slots", torch.int64, (T,), device), T, stream, checked)
     return K, V
 
 
@@ -940,28 +946,27 @@ def kv4_attention(Q, cache: Kv4Cache, block_table, lengths, n_q_heads: int, q_le
     if block_table.dim() != 2:
         raise ValueError("block_table: expected a matrix")
     B, width = block_table.shape
-    shape = (B * q_len, n_q_heads * cache.head_dim)
-    _check_tensor(Q, "Q", torch.bfloat16, shape)
-    _check_tensor(block_table, "block_table", torch.int32, (B, width))
-    _check_tensor(lengths, "lengths", torch.int32, (B,))
+    device, D = cache.device, cache.head_dim
+    shape = (B * q_len, n_q_heads * D)
+    q = _pointer(Q, "Q", torch.bfloat16, shape, device)
+    table = _pointer(block_table, "block_table", torch.int32, (B, width), device)
+    n = _pointer(lengths, "lengths", torch.int32, (B,), device)
     if O is None:
-        O = _empty(shape, torch.bfloat16, cache.device, stream)
+        O = _empty(shape, torch.bfloat16, device, stream)
+        o = O.data_ptr()
     else:
-        _check_tensor(O, "O", torch.bfloat16, shape)
-    if workspace is None:
-        n = kv4_workspace_bytes(B, q_len, n_q_heads, cache.n_kv_heads, cache.head_dim, width, cache.page_size, _sm_count(cache.device))
-        if n:
-            workspace = _empty(n, torch.uint8, cache.device, stream)
-    _on_one_device(cache.device, Q=Q, block_table=block_table, lengths=lengths, O=O, workspace=workspace)
-    a = GmlpKv4AttentionArgs(ctypes.sizeof(GmlpKv4AttentionArgs), FLAG_CHECKED if checked else 0, Q.data_ptr(), O.data_ptr(),
-                             cache.struct, block_table.data_ptr(), lengths.data_ptr(), B, width, n_q_heads, q_len,
-                             cache.head_dim ** -0.5 if scale is None else scale, 0, _stream_handle(stream, cache.device),
-                             None if workspace is None else workspace.data_ptr(),
-                             0 if workspace is None else workspace.numel() * workspace.element_size())
-    _run(lib().gmlp_kv4_attention, a, cache.device)
+        o = _pointer(O, "O", torch.bfloat16, shape, device)
+    need = 0 if workspace is not None else lib().gmlp_kv4_workspace_bytes(B, q_len, n_q_heads, cache.n_kv_heads, D, width, cache.page_size,
+                                                                          _sm_count(device))
+    keep, ws, ws_bytes = _workspace(workspace, need, device, stream)
+    _run(lib().gmlp_kv4_attention,
+         GmlpKv4AttentionArgs(_SIZE_KV4_ATTENTION, FLAG_CHECKED if checked else 0, q, o, cache.struct, table, n, B, width, n_q_heads, q_len,
+                              D ** -0.5 if scale is None else scale, 0, _stream_handle(stream, device), ws, ws_bytes), device)
     return O
 
 
+_SIZE_W4_MATMUL, _SIZE_W4 = ctypes.sizeof(GmlpW4MatmulArgs), ctypes.sizeof(GmlpW4Args)
+_SIZE_KV4_ROWS, _SIZE_KV4_ATTENTION = ctypes.sizeof(GmlpKv4RowsArgs), ctypes.sizeof(GmlpKv4AttentionArgs)
 _sm_counts: dict = {}
 
 

@@ -32,20 +32,23 @@ def values(q, s, z, G):
 
 
 def weights(gen, K, N, G, zero_points, device):
-    """A random quantised matrix: codes [K, N], scales, zeros (or None) and its 64-bit values [K, N]."""
+    """A random quantised matrix: codes [K, N], scales, zeros (or None), its 64-bit values [K, N], and the largest terms an
+    evaluation may form of them, ((16 + q) + (16 + z)) * |s| (see product_bound)."""
     w = torch.randn(N, K, generator=gen, device=device) * K ** -0.5
     q, s, z = quantize(w, G, zero_points)
     c = lambda t: t.t().contiguous()
-    return c(q), c(s), c(z.to(torch.uint8)) if zero_points else None, c(values(q, s, z, G))
+    terms = ((32 + q.double().unflatten(-1, (-1, G)) + z.double()[..., None]) * s.double().abs()[..., None]).flatten(-2)
+    return c(q), c(s), c(z.to(torch.uint8)) if zero_points else None, c(values(q, s, z, G)), c(terms)
 
 
-def product_bound(x, w, G):
-    """How far an fp32 evaluation of x @ w may be off, element by element.  Products of a bf16 number and a code are exact.
-    A group is at most G / 16 accumulation steps of 16 products, the groups are K / G fused multiply-adds, at most 16 more
-    additions join the partial sums; each addition (16 per step) is off by at most one unit in the last place, 2^-23, of
-    the sum of the absolute values."""
+def product_bound(x, terms, G):
+    """How far an fp32 evaluation of x @ w may be off, element by element, where it sums (16 + q) x over a group and takes
+    (16 + z) sum(x) off afterwards.  Products of a bf16 number and a number below 32 are exact.  A group is at most G / 16
+    accumulation steps of 16 products, sum(x) at most G additions, the difference one fused step, the groups are K / G fused
+    multiply-adds, at most 16 more additions join the partial sums; each addition (16 per step) is off by at most one unit in
+    the last place, 2^-23, of the sum of the absolute values, which is at most |x| @ terms."""
     K = x.shape[1]
-    return (G + K / G + 16) * 2.0 ** -23 * (x.abs() @ w.abs())
+    return (G + 1 + K / G + 16) * 2.0 ** -23 * (x.abs() @ terms)
 
 
 def channel_places(D):
@@ -85,13 +88,14 @@ def attention(Q, k, v, lengths, Hq, T, scale):
                 p = torch.softmax(s, 0)
                 O[b * T + i, at] = p @ v[b][:m, g]
                 A[b * T + i, at] = p @ v[b][:m, g].abs()
-                # up to D additions of 16-product steps and scalings, then the scaling to base 2: one unit each
-                E[b * T + i, at] = ((k[b][:m, g].abs() @ q.abs()).max() * abs(scale) * (D + 8) + s.abs().max()) * 2.0 ** -23
+                # the terms are (16 + q) and (16 + z), at most 62 steps s of a quantiser together, and s <= max |k| / 7 (the 15 steps
+                # of a group reach at least 7 to one side); D additions and a few scalings, one unit each
+                E[b * T + i, at] = (62 / 7 * k[b][:m, g].abs().max() * q.abs().sum() * abs(scale) * (D + 8) + s.abs().max()) * 2.0 ** -23
     return O, A, E
 
 
 def attention_bound(O, A, E, steps, spread):
     """P' is rounded to bf16 once (2^-8 of each term), O once (2^-8); a score off by E changes p by a factor e^(2 E) at most
-    (numerator and sum); exp2 is good to 2^-21 on both sides; the fp32 sums over `steps` accumulations see terms of up to
-    16 steps of the quantiser (`spread`: largest 16 * scale) weighted by p."""
+    (numerator and sum); exp2 is good to 2^-21 on both sides; the fp32 sums over `steps` accumulations see (16 + q) and
+    (16 + z), at most 62 steps of a quantiser together, weighted by p (`spread`: 62 / 7 of the largest |v|, as for the scores)."""
     return 2.0 ** -8 * (O.abs() + A) * 1.01 + (2 * E + 2.0 ** -20) * A * 1.01 + steps * 2.0 ** -23 * spread

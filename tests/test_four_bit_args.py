@@ -48,8 +48,8 @@ BAD_MATRICES = [(dict(group=16), gmlp.ERR_SHAPE), (dict(group=0), gmlp.ERR_SHAPE
 
 
 def test_w4_sizes(lib):
-    # tiles of 16 columns by 128 rows, a kilobyte each
-    assert gmlp.w4_sizes(128, 16, 128) == (1024, 16)
+    # tiles of 16 columns by 128 rows, a kilobyte each, an even number of them along K
+    assert gmlp.w4_sizes(128, 16, 128) == (2048, 32)
     assert gmlp.w4_sizes(160, 17, 32) == (2 * 2 * 1024, 2 * 2 * 16 * 4)
     assert gmlp.w4_sizes(4096, 14336, 64) == (4096 * 14336 // 2, 4096 * 14336 // 64)
     for K, N, G in ((0, 16, 128), (128, 0, 128), (100, 16, 32), (128, 16, 48), (1 << 21, 16, 128)):
@@ -113,22 +113,29 @@ def test_w4_layout_refusals(lib):
 
 @pytest.mark.parametrize("terms", [1, 2])
 @pytest.mark.parametrize("gated", [False, True])
-def test_w4_plan_of_every_size(lib, terms, gated):
-    """Every launch shape makes progress and fits: a chunk of at least a step, whole rounds of the two-deep prefetch where there
-    is more than one chunk, X and the partial sums within 200 KB (half of that for up to 16 tokens: two CTAs per SM)."""
+@pytest.mark.parametrize("G", [32, 64, 128])
+def test_w4_plan_of_every_size(lib, terms, gated, G):
+    """Every launch shape covers its rows, fits a CTA's shared memory (227 KB) and keeps its cluster's CTAs busy."""
+    block = 1024 + 48 * (128 // G)                               # codes, scales, zero points of a tile's k-block
     for M in range(1, gmlp.W4_MAX_M + 1):
-        for K in (32, 128, 160, 1024, 2080, 4096, 4128, 8192, 11008, 14336, 28672, 1 << 20):
+        for K in (128, 256, 1024, 2048 + 128, 4096, 4096 + 128, 8192, 11008, 14336, 28672, 1 << 20):
             for N in (1, 16, 20, 33, 48, 64, 100, 256, 1000, 4096, 14336, 28672, 1 << 20):
-                nt, wr, c, chunk, steps, smem, ctas = gmlp.w4_plan(M, K, N, terms, gated, 148)
-                kb, wk, rows = -(-K // 128), 8 // wr, M * terms
-                assert 8 * nt >= M and wr in (1, 2, 4, 8) and 1 <= c <= 8 and c <= kb and steps == -(-(-(-kb // c)) // wk)
-                assert 1 <= chunk <= steps and (chunk == steps or chunk % 2 == 0)
-                x = (chunk * wk * 256 + 64) * rows * (1 if chunk == steps else 2)
-                assert smem >= x and smem >= 8 * 32 * 8 * (nt | 1) * 4 and smem <= (100 if nt <= 2 else 200) * 1024
-                assert ctas == c * -(-(-(-N // (16 if gated else 32))) // wr)
-    out = (ctypes.c_int32 * 7)()
-    assert lib.gmlp_w4_plan(65, 1, 128, 16, 0, 148, out) == gmlp.ERR_SHAPE and lib.gmlp_w4_plan(1, 3, 128, 16, 0, 148, out) == gmlp.ERR_SHAPE
-    assert lib.gmlp_w4_plan(1, 1, 128, 16, 0, 148, None) == gmlp.ERR_NULL
+                stream, nt, gw, wr, c, parts, ctas, smem = gmlp.w4_plan(M, K, N, G, terms, gated, 148)
+                kb, tiles, m_cta = -(-K // 256) * 2, -(-N // 16), -(-M // parts)
+                rows = m_cta * terms
+                assert 8 * nt >= rows > 8 * (nt - 1) and (parts - 1) * m_cta < M and smem <= 227 * 1024
+                if stream:                                       # per warp: its sums and a ring of three; all of X
+                    assert rows <= 16 and parts == 1 and c == 1 and gw in (2, 4, 8, 16) and ctas == min(tiles, 148)
+                    assert smem >= 16 * (512 + (3 if nt == 1 else 2) * 2 * block) + kb * 128 // G * nt * 32 + rows * (kb * 256 + 64)
+                    continue
+                wk = 8 // wr
+                assert rows <= 32 and wr in (1, 2, 4, 8) and gw == 0 and 1 <= c <= 8 and (c == 1 or kb >= 2 * wk * c)
+                assert smem >= 3 * (rows * (wk * 256 + 64) + 16 * block) and smem >= 8 * 32 * 8 * (nt | 1) * 4
+                assert ctas == c * -(-(-(-N // (16 if gated else 32))) // wr) and 1 <= parts <= 4
+    out = (ctypes.c_int32 * 8)()
+    for bad in ((65, 1, 128, 16, 0, 128), (0, 1, 128, 16, 0, 128), (1, 3, 128, 16, 0, 128), (1, 1, 0, 16, 0, 128), (1, 1, 128, 16, 0, 48)):
+        assert lib.gmlp_w4_plan(*bad, 148, out) == gmlp.ERR_SHAPE
+    assert lib.gmlp_w4_plan(1, 1, 128, 16, 0, 128, 148, None) == gmlp.ERR_NULL
 
 
 def test_w4_workspace(lib):

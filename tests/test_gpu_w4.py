@@ -40,7 +40,7 @@ def test_quantise_and_dequantise_are_exact(K, N, G, out_in, zero_points):
 @pytest.mark.parametrize("out_in", [False, True])
 @pytest.mark.parametrize("K,N,G", [(32, 3, 32), (320, 33, 64), (384, 48, 128), (1024, 1000, 32)])
 def test_pack_round_trip(K, N, G, out_in, zero_points):
-    q, s, z, w = F.weights(gen(7 * K + N), K, N, G, zero_points, DEV)
+    q, s, z, w, _ = F.weights(gen(7 * K + N), K, N, G, zero_points, DEV)
     t = (lambda x: None if x is None else x.t().contiguous()) if out_in else (lambda x: x)
     m = gmlp.w4_pack(t(q), t(s), t(z), weights_out_in=out_in, checked=True)
     assert m.K == K and m.N == N and m.group == G
@@ -49,12 +49,12 @@ def test_pack_round_trip(K, N, G, out_in, zero_points):
 
 def check_matmul(M, K, N, G, zero_points, seed=0):
     g = gen(1000 * seed + M + K + N + G)
-    q, s, z, w = F.weights(g, K, N, G, zero_points, DEV)
+    q, s, z, w, terms = F.weights(g, K, N, G, zero_points, DEV)
     X = bf16(g, M, K)
     Y = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device=DEV)
     gmlp.w4_matmul(X, gmlp.w4_pack(q, s, z), Y, checked=True)
     want = X.double() @ w
-    bound = F.product_bound(X.double(), w, G) + 2.0 ** -8 * want.abs()
+    bound = F.product_bound(X.double(), terms, G) + 2.0 ** -8 * want.abs()
     err = (Y.double() - want).abs() / bound
     assert bool(torch.isfinite(Y.float()).all()) and float(err.max()) <= 1.0, f"{float(err.max()):.3f} of the bound"
 
@@ -85,7 +85,7 @@ def test_matmul_layer_sizes(M, K, N, G):
 
 def test_matmul_extreme_values_and_groups_of_zeros():
     K, N, G, M = 512, 96, 64, 6
-    q, s, z, w = F.weights(gen(3), K, N, G, True, DEV)
+    q, s, z, w, _ = F.weights(gen(3), K, N, G, True, DEV)
     s[:, 5] = 0
     s[3, 7] = float("nan")
     s[2, 9] = float("inf")
@@ -99,6 +99,19 @@ def test_matmul_extreme_values_and_groups_of_zeros():
     rest = [c for c in range(N) if c not in (7, 9)]
     assert bool((Y[3, rest] == 0).all()) and bool((Y[[0, 3, 4, 5], 5] == 0).all())
     assert bool(torch.isfinite(Y[[0, 4, 5]][:, rest]).all())
+
+
+def test_matmul_of_activations_near_the_largest_bf16():
+    # (16 + q) x would overflow where (q - z) x does not: the sums of a row stay finite, and its neighbours exact
+    K, N, G = 256, 64, 128
+    q = torch.randint(7, 10, (K, N), generator=gen(1), device=DEV, dtype=torch.uint8)
+    s = torch.full((2, N), 2.0 ** -20, dtype=torch.bfloat16, device=DEV)
+    X = torch.zeros(3, K, device=DEV)
+    X[0, 5], X[0, 200], X[1] = 2.5e38, -1.25e38, 1.0
+    X = X.to(torch.bfloat16)
+    Y = gmlp.w4_matmul(X, gmlp.w4_pack(q, s), checked=True)
+    want = X.double() @ ((q.double() - 8) * 2.0 ** -20)
+    assert bool(((Y.double() - want).abs() <= 2.0 ** -8 * want.abs()).all())
 
 
 def test_matmul_of_every_code_and_zero_point():
@@ -122,6 +135,7 @@ def check_forward(M, D, Fd, G, Gd, zero_points, norm, gain, act, eps=1e-5):
     mats = [F.weights(g, D, Fd, G, zero_points, DEV), F.weights(g, D, Fd, G, zero_points, DEV), F.weights(g, Fd, D, Gd, not zero_points, DEV)]
     packed = [gmlp.w4_pack(*m[:3]) for m in mats]
     wg, wu, wd = (m[3] for m in mats)
+    tg, tu, td = (m[4] for m in mats)
     X = bf16(g, M, D)
     gamma = (torch.rand(D, generator=g, device=DEV) + 0.5).to(torch.bfloat16) if gain else None
     Y = torch.full((M, D), float("nan"), dtype=torch.bfloat16, device=DEV)
@@ -133,13 +147,13 @@ def check_forward(M, D, Fd, G, Gd, zero_points, norm, gain, act, eps=1e-5):
         # two bf16 terms leave 2^-17 of the value (2^-9 of 2^-8), the fp32 statistic and its products 2^-20
         slack = 2.0 ** -16
     a, u = x @ wg, x @ wu
-    da, du = (F.product_bound(x, w, G) + slack * (x.abs() @ w.abs()) for w in (wg, wu))
+    da, du = (F.product_bound(x, t, G) + slack * (x.abs() @ w.abs()) for w, t in ((wg, tg), (wu, tu)))
     h = ACT[act](a) * u
     # |act'| <= 1.2 for all four (GELU's largest slope is 1.13; swish with beta 1.5 stays below 1.1), fast exponential and
     # division 2^-19, two bf16 terms of h 2^-16
     dh = 1.2 * da * u.abs() + ACT[act](a).abs() * du + 1.2 * da * du + (2.0 ** -16 + 2.0 ** -19) * h.abs()
     want = h @ wd
-    bound = dh @ wd.abs() + F.product_bound(h, wd, Gd) + 2.0 ** -8 * want.abs()
+    bound = dh @ wd.abs() + F.product_bound(h, td, Gd) + 2.0 ** -8 * want.abs()
     err = (Y.double() - want).abs() / bound
     assert float(err.max()) <= 1.0, f"{float(err.max()):.3f} of the bound"
     # the intermediate values keep their accuracy: the whole is hardly further off than its last rounding
@@ -178,7 +192,7 @@ def test_forward_of_infinities():
 
 
 def test_results_repeat_and_empty_batches():
-    q, s, z, _ = F.weights(gen(1), 2048, 1024, 128, False, DEV)
+    q, s, z, _, _ = F.weights(gen(1), 2048, 1024, 128, False, DEV)
     m = gmlp.w4_pack(q, s, z)
     X = bf16(gen(2), 24, 2048)
     first = gmlp.w4_matmul(X, m)
@@ -229,7 +243,7 @@ def test_streams_graphs_and_weights_made_just_before():
 
 
 def test_binding_refusals():
-    q, s, z, _ = F.weights(gen(1), 256, 64, 128, False, DEV)
+    q, s, z, _, _ = F.weights(gen(1), 256, 64, 128, False, DEV)
     m = gmlp.w4_pack(q, s, z)
     X = bf16(gen(2), 4, 256)
     for bad in (X.float(), X.t().contiguous().t(), X.cpu()):

@@ -432,7 +432,7 @@ typedef struct gmlp_kv4_attention_args {
     gmlp_kv4_cache cache;
     const void* block_table;  /* device, [B, table_width] int32 */
     const void* lengths;      /* device, [B] int32 */
-    int64_t B, table_width;
+    int64_t B, table_width;   /* B at most 65535, table_width * page_size at most 2^30 */
     int32_t n_q_heads, q_len;
     float scale;              /* e.g. 1 / sqrt(head_dim); any finite number */
     int32_t reserved;         /* must be 0 */

@@ -73,9 +73,10 @@ Kv4Plan kv4_plan(int64_t B, int T, int ratio, int n_kv_heads, int head_dim, int6
     return p;
 }
 
+constexpr int64_t kKv4MostKeys = (int64_t)1 << 30;       // of one request: positions stay well inside 31 bits
 int check_kv4_attention(int64_t B, int T, int Hq, int Hkv, int64_t width, int page_size) {
     if (B < 0 || B > 65535 || T < 1 || T > GMLP_KV4_MAX_QUERIES || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq > 65535 || width < 1 ||
-        width > INT32_MAX / page_size || B * T * Hq > INT32_MAX)
+        width > kKv4MostKeys / page_size || B * T * Hq > INT32_MAX)
         return GMLP_ERR_SHAPE;
     return GMLP_OK;
 }

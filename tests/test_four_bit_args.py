@@ -186,6 +186,7 @@ def attention_args():
                                        (dict(B=-1), gmlp.ERR_SHAPE), (dict(B=65536), gmlp.ERR_SHAPE), (dict(q_len=0), gmlp.ERR_SHAPE),
                                        (dict(q_len=17), gmlp.ERR_SHAPE), (dict(n_q_heads=7), gmlp.ERR_SHAPE), (dict(n_q_heads=0), gmlp.ERR_SHAPE),
                                        (dict(table_width=0), gmlp.ERR_SHAPE), (dict(table_width=1 << 40), gmlp.ERR_SHAPE),
+                                       (dict(table_width=(1 << 24) + 1), gmlp.ERR_SHAPE),
                                        (dict(B=0, Q=None, O=None), gmlp.OK), (dict(Q=None), gmlp.ERR_NULL), (dict(lengths=None), gmlp.ERR_NULL),
                                        (dict(O=0x2008), gmlp.ERR_ALIGN), (dict(block_table=0x3002), gmlp.ERR_ALIGN),
                                        (dict(workspace=0x100), gmlp.ERR_ARCH if not torch.cuda.is_available() else gmlp.ERR_WORKSPACE),

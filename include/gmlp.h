@@ -340,11 +340,12 @@ typedef struct gmlp_w4_matmul_args {
 } gmlp_w4_matmul_args;
 int gmlp_w4_matmul(const gmlp_w4_matmul_args* args);
 /* How a product of M tokens (terms = 1 for bf16 input, 2 for the two-term inputs inside gmlp_w4_forward) with a [K, N] matrix (gated:
- * with two of them) is launched on a device with `sm_count` SMs (0: the current device, 148 if there is none): plan[0] = 1 for the
- * persistent kernel, 0 for the tile kernel, [1] = columns of eight rows of X (rows are tokens times terms) per CTA, [2] = warps
- * of a team (persistent kernel), [3] = groups of two column tiles per CTA (tile kernel), [4] = CTAs per cluster (K is split over them), [5] =
- * parts the tokens are cut into, [6] = CTAs per part, [7] = bytes of shared memory per CTA.  Pure host arithmetic. */
-int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t group, int32_t sm_count, int32_t plan[8]);
+ * with two of them) is launched on a device with `sm_count` SMs (0: the current device, 148 if there is none): plan[0] = 0 for the
+ * persistent mma.sync kernel that keeps X in shared memory (up to 16 rows, tokens times terms), 1 for the mma.sync tiles, 2 for the
+ * tcgen05 kernel, [1] = rows of X per CTA, padded, [2] = warps of a team (persistent) or column groups per CTA (tiles), [3] = CTAs per
+ * cluster (K is split over them), [4] = parts the tokens are cut into, [5] = CTAs per part, [6] = bytes of shared memory per CTA.
+ * Pure host arithmetic. */
+int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t group, int32_t sm_count, int32_t plan[7]);
 
 /*
  * The Gated MLP on 4-bit weights: Y = (act(Xn Wg) (.) (Xn Wu)) Wd with Wg, Wu [d_model, d_ff] and Wd [d_ff, d_model] as

@@ -144,7 +144,7 @@ struct DeviceState {
     bool skinny_attr_set = false;
     bool skinny_cluster_attr_set = false;
     bool skinny_fused_attr_set = false;
-    bool w4_attr_set[36] = {};                   // (stream * 4 + columns - 1) * 6 + gated * 3 + group
+    bool w4_attr_set[48] = {};                   // kernel (two stream, two umma, four tile) * 6 + gated * 3 + group
     int fused_capacity[9] = {};                  // the same for the fused small-M kernel
     int cluster_capacity[2][9] = {};             // clusters of C CTAs of the cluster-form kernels resident at once (0 = not asked yet)
     // arrival-counter regions zeroed by the library (the kernels leave them zero after every call); a few are
@@ -2207,13 +2207,13 @@ uint64_t gmlp_w4_scale_count(int64_t K, int64_t N, int32_t group) {
     if (group != 32 && group != 64 && group != 128) return 0;
     return gmlp_w4_code_bytes(K, N) / 1024u * 16u * (uint64_t)(128 / group);
 }
-int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t group, int32_t sm_count, int32_t plan[8]) {
+int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, int32_t group, int32_t sm_count, int32_t plan[7]) {
     if (plan == nullptr) return GMLP_ERR_NULL;
     if (M < 1 || M > gmlp::kW4MaxM || terms < 1 || terms > 2 || gmlp_w4_scale_count(K, N, group) == 0) return GMLP_ERR_SHAPE;
     const W4Plan p = w4_plan((int)M, terms, w4_k_blocks(K), (int)((N + 15) / 16), gated != 0, group,
                              sm_count > 0 ? sm_count : current_sm_count());
-    const int32_t out[8] = {p.stream ? 1 : 0, p.nt, p.stream ? p.group_warps : 0, p.stream ? 0 : 1 << p.wr_log2, p.cluster, p.m_parts, p.ctas, (int32_t)p.smem};
-    for (int i = 0; i < 8; ++i) plan[i] = out[i];
+    const int32_t out[7] = {p.kind, 8 * p.nt, p.kind == kW4Stream ? p.group_warps : (p.kind == kW4Tile ? 1 << p.wr_log2 : 0), p.cluster, p.m_parts, p.ctas, (int32_t)p.smem};
+    for (int i = 0; i < 7; ++i) plan[i] = out[i];
     return GMLP_OK;
 }
 uint64_t gmlp_w4_workspace_bytes(int64_t M, int64_t d_model, int64_t d_ff, uint32_t flags) {

@@ -1,9 +1,10 @@
 // Host side of the 4-bit weight operators: checks, launch shapes, launches.  Included by api.cu inside its namespace.
 
+enum { kW4Stream = 0, kW4Tile = 1, kW4Umma = 2 };
 struct W4Plan {
-    bool stream;                                     // w4_stream_kernel, else w4_tile_kernel
+    int kind;                                        // the kernel, kW4Stream, kW4Tile or kW4Umma
     int nt, ctas, threads, group_warps;
-    int m_cta, m_parts, wr_log2, cluster, groups;    // tile kernel
+    int m_cta, m_parts, wr_log2, cluster;            // tile and umma kernels
     uint32_t smem;
 };
 inline int w4_k_blocks(int64_t K) { return (int)((K + 255) / 256) * 2; }      // of 128 rows, an even number
@@ -16,7 +17,7 @@ W4Plan w4_plan(int M, int terms, int KB, int n16, bool gated, int G, int sms) {
     // The persistent kernel, where all of X fits beside the rings.
         const uint64_t smem = gmlp::w4_stream_bytes(rows, KB, G);
         if (smem <= kW4SmemMost) {
-            p.stream = true;
+            p.kind = kW4Stream;
             p.nt = rows <= 8 ? 1 : 2;
             p.threads = gmlp::kW4StreamThreads;
             // eight warps a tile where K is long or there are few tiles, else four (fewer hand-overs of sums)
@@ -28,26 +29,42 @@ W4Plan w4_plan(int M, int terms, int KB, int n16, bool gated, int G, int sms) {
             return p;
         }
     }
-    p.m_parts = (rows + 31) / 32;
+    // tcgen05 for more than 16 rows where its groups of 128 columns fill most of the GPU, in one wave or with K of 4096 or more
+    // (1024 x 14336 at M = 64: 10.4 us against 18.5 for the tiles; 1024 x 28672 at M = 20, two short waves: 18.4 against 12.9), or where K
+    // is long enough to pay for a cluster (14336 x 4096 at M = 64: 34.6 against 52; 4096 x 4096: 22.1 against 17.4); else tiles.
+    const int groups128 = gated ? (n16 + 3) / 4 : (n16 + 7) / 8, ctas128 = groups128 * ((rows + 63) / 64);
+    p.kind = rows > 16 && ((ctas128 >= 96 && (ctas128 <= sms || KB >= 32)) || (ctas128 >= 32 && KB >= 64)) ? kW4Umma : kW4Tile;
+    const int rows_most = p.kind == kW4Umma ? 64 : 32;
+    p.m_parts = (rows + rows_most - 1) / rows_most;
     p.m_cta = (M + p.m_parts - 1) / p.m_parts;
     p.m_parts = (M + p.m_cta - 1) / p.m_cta;
-    const int rows_cta = p.m_cta * terms, units = gated ? n16 : (n16 + 1) / 2;
+    const int rows_cta = p.m_cta * terms;
+    p.cluster = 1;
+    if (p.kind == kW4Umma) {
+        p.nt = rows_cta <= 32 ? 4 : 8;               // rows are padded to 32 or 64
+        // K over a cluster of up to four while the CTAs fit one wave, as long as each keeps eight k-blocks
+        while (p.cluster < 4 && groups128 * p.m_parts <= cluster_capacity_estimate(p.cluster + 1, sms) && KB >= 8 * (p.cluster + 1)) ++p.cluster;
+        p.ctas = groups128 * p.cluster;
+        p.threads = gmlp::kW4UmmaThreads;
+        p.smem = gmlp::w4_umma_smem(8 * p.nt, G);
+        return p;
+    }
     p.nt = (rows_cta + 7) / 8;
+    const int units = gated ? n16 : (n16 + 1) / 2;
     // Column groups per CTA: few, so that a CTA's warps share long ranges of K and their sums stay in the CTA, unless there are
     // columns enough to fill the GPU with more (each group reads its CTA's copy of X).
     p.wr_log2 = rows_cta <= 16 ? 0 : (units * p.m_parts >= 4 * sms ? 2 : 1);
-    const int WR = 1 << p.wr_log2, WK = 8 >> p.wr_log2;
-    p.groups = (units + WR - 1) / WR;
+    const int WR = 1 << p.wr_log2, WK = 8 >> p.wr_log2, groups = (units + WR - 1) / WR;
     // K over a cluster only where the CTAs would leave a third of the SMs idle: its hand-over costs about two microseconds
-    p.cluster = 1;
-    while (p.cluster < 4 && 3 * p.groups * p.m_parts * p.cluster <= 2 * sms && KB >= 2 * WK * (p.cluster + 1)) ++p.cluster;
-    p.ctas = p.groups * p.cluster;
+    while (p.cluster < 4 && 3 * groups * p.m_parts * p.cluster <= 2 * sms && KB >= 2 * WK * (p.cluster + 1)) ++p.cluster;
+    p.ctas = groups * p.cluster;
     p.threads = gmlp::kW4Threads;
     p.smem = gmlp::w4_tile_smem(p.nt, rows_cta, WK, G);
     return p;
 }
 
 typedef void (*W4Kernel)(gmlp::W4GemmArgs);
+typedef void (*W4UmmaKernel)(gmlp::W4GemmArgs, CUtensorMap);
 template <int NT>
 W4Kernel w4_stream_kernel_for(int G, bool gated) {
     if (gated) return G == 32 ? gmlp::w4_stream_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_stream_kernel<NT, 64, true> : gmlp::w4_stream_kernel<NT, 128, true>);
@@ -57,6 +74,11 @@ template <int NT>
 W4Kernel w4_tile_kernel_for(int G, bool gated) {
     if (gated) return G == 32 ? gmlp::w4_tile_kernel<NT, 32, true> : (G == 64 ? gmlp::w4_tile_kernel<NT, 64, true> : gmlp::w4_tile_kernel<NT, 128, true>);
     return G == 32 ? gmlp::w4_tile_kernel<NT, 32, false> : (G == 64 ? gmlp::w4_tile_kernel<NT, 64, false> : gmlp::w4_tile_kernel<NT, 128, false>);
+}
+template <int RPAD>
+W4UmmaKernel w4_umma_kernel_for(int G, bool gated) {
+    if (gated) return G == 32 ? gmlp::w4_umma_kernel<RPAD, 32, true> : (G == 64 ? gmlp::w4_umma_kernel<RPAD, 64, true> : gmlp::w4_umma_kernel<RPAD, 128, true>);
+    return G == 32 ? gmlp::w4_umma_kernel<RPAD, 32, false> : (G == 64 ? gmlp::w4_umma_kernel<RPAD, 64, false> : gmlp::w4_umma_kernel<RPAD, 128, false>);
 }
 
 int check_w4_matrix(const gmlp_w4_matrix& w) {
@@ -98,9 +120,15 @@ int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_mat
     const int K = (int)w0.K, N = (int)w0.N, KB = w4_k_blocks(K), n16 = (N + 15) / 16;
     const bool gated = w1 != nullptr;
     const W4Plan p = w4_plan((int)M, terms, KB, n16, gated, w0.group, dev->sm_count);
-    W4Kernel kernel;
-    if (p.stream) {
+    W4Kernel kernel = nullptr;
+    W4UmmaKernel umma = nullptr;
+    int row = 0;                                     // of the kernels, for the attribute below
+    if (p.kind == kW4Stream) {
         kernel = p.nt == 1 ? w4_stream_kernel_for<1>(w0.group, gated) : w4_stream_kernel_for<2>(w0.group, gated);
+        row = p.nt - 1;
+    } else if (p.kind == kW4Umma) {
+        umma = p.nt == 4 ? w4_umma_kernel_for<32>(w0.group, gated) : w4_umma_kernel_for<64>(w0.group, gated);
+        row = p.nt == 4 ? 2 : 3;
     } else {
         switch (p.nt) {
             case 1: kernel = w4_tile_kernel_for<1>(w0.group, gated); break;
@@ -108,11 +136,12 @@ int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_mat
             case 3: kernel = w4_tile_kernel_for<3>(w0.group, gated); break;
             default: kernel = w4_tile_kernel_for<4>(w0.group, gated); break;
         }
+        row = 3 + p.nt;
     }
-    const int slot = ((p.stream ? 4 : 0) + p.nt - 1) * 6 + (gated ? 3 : 0) + (w0.group == 32 ? 0 : (w0.group == 64 ? 1 : 2));
+    const int slot = row * 6 + (gated ? 3 : 0) + (w0.group == 32 ? 0 : (w0.group == 64 ? 1 : 2));
     if (!dev->w4_attr_set[slot]) {
-        if (cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kW4SmemMost) != cudaSuccess)
-            return GMLP_ERR_LAUNCH;
+        const void* f = umma != nullptr ? reinterpret_cast<const void*>(umma) : reinterpret_cast<const void*>(kernel);
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kW4SmemMost) != cudaSuccess) return GMLP_ERR_LAUNCH;
         dev->w4_attr_set[slot] = true;
     }
     gmlp::W4GemmArgs a{};
@@ -127,12 +156,16 @@ int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_mat
     a.n16 = n16;
     a.terms = terms;
     a.m_cta = p.m_cta;
-    a.wr_log2 = p.wr_log2;
     a.cluster = p.cluster;
     a.group_warps = p.group_warps;
+    a.wr_log2 = p.wr_log2;
     a.early = early ? 1 : 0;
     a.act = act;
-    return launch_chained(kernel, dim3((unsigned)p.ctas, (unsigned)p.m_parts), (unsigned)p.threads, p.smem, p.cluster, st, a);
+    const dim3 grid((unsigned)p.ctas, (unsigned)p.m_parts);
+    if (umma == nullptr) return launch_chained(kernel, grid, (unsigned)p.threads, p.smem, p.cluster, st, a);
+    CUtensorMap tmX;                                 // rows of X in boxes of 64 k; two terms: a box each
+    if (!encode_2d(&tmX, X, (uint64_t)K, (uint64_t)M * terms, 64, (uint32_t)(8 * p.nt / terms))) return GMLP_ERR_LAUNCH;
+    return launch_chained(umma, grid, (unsigned)p.threads, p.smem, p.cluster, st, a, tmX);
 }
 
 int finish_checked(uint32_t flags, cudaStream_t st) {

@@ -23,6 +23,7 @@
 #include "common.cuh"
 #include "ptx.cuh"
 #include "umma_gemm_2cta.cuh"
+#include "umma_skinny.cuh"
 
 namespace gmlp {
 
@@ -39,9 +40,9 @@ struct W4GemmArgs {
     const bf16* X;             // [terms][M][K]
     bf16* out;                 // plain: [M][N]; gated: [2][M][N], hi and lo of the gated product
     int M, K, N, KB, n16, terms;
-    int m_cta;                 // tokens per CTA: blockIdx.y takes the tokens from blockIdx.y * m_cta on
+    int m_cta;                 // tile and umma kernels: tokens per CTA; blockIdx.y takes the tokens from blockIdx.y * m_cta on
     int group_warps;           // stream kernel: warps of a team, a power of two
-    int wr_log2, cluster;      // tile kernel: column groups per CTA; CTAs per cluster
+    int wr_log2, cluster;      // tile kernel: column groups per CTA; tile and umma kernels: CTAs that share K
     int early;                 // the weights may be fetched before the preceding kernel of the call has ended
     GateAct act;
 };
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(kW4StreamThreads, 1) w4_stream_kernel(const W4
     cp_async_wait_all();
 }
 
-// ------------------------------------------------------------------ more rows of X, or X too large to stay: tiles
+// ------------------------------------------------------------------ X too large to stay, or more rows of a small matrix: tiles
 // The 8 warps of a CTA are WR groups of two column tiles (gated: of a gate and an up tile) x WK ranges of K; stages of WK k-blocks of
 // codes and X pass through shared memory, three deep.  Up to 32 rows of X per CTA (blockIdx.y: further rows, which read the codes
 // again, from L2: by then the products set the time), and K over a cluster of C CTAs that add their sums in distributed shared memory.
@@ -611,6 +612,285 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_tile_kernel(const W4GemmArgs
         } else {
             p.out[at] = __float2bfloat16_rn(sum(r, m));
         }
+    }
+    __syncwarp();
+    if (C > 1) ptx::cluster_sync();                  // the peers may still be reading this CTA's sums
+}
+
+// ------------------------------------------------------------------ more than 16 rows of X: tcgen05
+// One CTA per 128 columns of W (gated: 64 gate and the same 64 up columns) and up to 64 rows of X (blockIdx.y: further rows), K over a
+// cluster of C CTAs that add their sums in distributed shared memory.  Four kinds of warps pass k-blocks of 128 on:
+//   4 producers   bulk copies of two tiles' codes and parameters each, TMA boxes of X (the B operand: K-major, 128-byte swizzle);
+//                 a bulk copy costs its thread some 90 cycles, so one thread for all would set the pace;
+//   8 unpackers   a tile each: codes to q - z, exact in bf16, straight into the same layout as the A operand (a lane's eight
+//                 neighbouring k of a column are one 16-byte store; two buffers);
+//   1 issuer      the tcgen05.mma of each group of G rows of K, into columns of TMEM of its own (two buffers);
+//   8 readers     tcgen05.ld of the sums (a lane per column of W, half of the rows of X per warp), scaled in fp32 and added in
+//                 registers: no weight is rounded here either.
+// (With all warps doing everything in step, one barrier per k-block, a k-block took 1750 cycles.)
+constexpr int kW4Producers = 4, kW4Unpackers = 8, kW4Readers = 8;
+constexpr int kW4UmmaThreads = 32 * (kW4Unpackers + kW4Readers + 1 + kW4Producers);
+constexpr int kW4UmmaDepth = 5;
+constexpr uint32_t kW4UmmaABytes = 128 * 256;
+__host__ __device__ constexpr uint32_t w4_umma_smem(int rpad, int G) {
+    return 1024u + 2u * kW4UmmaABytes + (uint32_t)kW4UmmaDepth * ((uint32_t)rpad * 256u + 8u * (uint32_t)w4_slot_bytes(G, 1)) + 192u;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// RPAD: rows of X of the product, 32 or 64 (rows past the last one are zeros or another part's; their sums are not stored).
+template <int RPAD, int G, bool GATED>
+__global__ void __launch_bounds__(kW4UmmaThreads, 1)
+w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
+{
+    extern __shared__ __align__(128) uint8_t w4_smem[];
+    constexpr int NG = 128 / G, BLOCK = w4_slot_bytes(G, 1), COLS = RPAD / 2;              // rows of X per reader
+    constexpr uint32_t X_BYTES = RPAD * 256, CODE_BYTES = 8 * BLOCK, TMEM_COLS = 2 * NG * RPAD;
+    constexpr int KERNEL_ID = 20, DEPTH = kW4UmmaDepth;
+    const uint32_t raw = ptx::smem_addr(w4_smem), base = (raw + 1023u) & ~1023u;           // the same in every CTA of a cluster
+    uint8_t* base_ptr = w4_smem + (base - raw);
+    // two buffers of A, a ring of X (all on 1024-byte boundaries: the swizzle goes by address), a ring of eight tiles' codes
+    const uint32_t x_ring = base + 2 * kW4UmmaABytes, code_ring = x_ring + DEPTH * X_BYTES;
+    uint8_t* code_ptr = base_ptr + 2 * kW4UmmaABytes + DEPTH * X_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(code_ptr + DEPTH * CODE_BYTES);
+    const uint32_t full0 = ptx::smem_addr(bars);                             // [DEPTH] a stage's copies have landed
+    const uint32_t empty0 = full0 + 8 * DEPTH;                               // [DEPTH] its sums have been read: it is free
+    const uint32_t a_full0 = empty0 + 8 * DEPTH;                             // [2] A is unpacked
+    const uint32_t done0 = a_full0 + 16;                                     // [2] the products have ended
+    const uint32_t d_empty0 = done0 + 16;                                    // [2] their sums have been read
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * DEPTH + 6);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int C = p.cluster, rank = C > 1 ? (int)ptx::cluster_ctarank() : 0, group = (int)blockIdx.x / C;
+    const int kb0 = (int)((int64_t)p.KB * rank / C), steps = (int)((int64_t)p.KB * (rank + 1) / C) - kb0;
+    const int m0 = (int)blockIdx.y * p.m_cta, M = min(p.m_cta, p.M - m0);
+    const bool has_zeros = p.w[0].zeros != nullptr;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < DEPTH; ++i) {
+            ptx::mbar_init(full0 + 8 * i, kW4Producers);
+            ptx::mbar_init(empty0 + 8 * i, kW4Readers);
+        }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(a_full0 + 8 * i, kW4Unpackers);
+            ptx::mbar_init(done0 + 8 * i, 1);
+            ptx::mbar_init(d_empty0 + 8 * i, kW4Readers);
+        }
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::fence_proxy_async_smem();
+        ptx::prefetch_tensormap(&tmX);
+    }
+    __syncthreads();
+    // TMEM is taken after the kernel before has ended and before the next one may start: neither is kept from its own by a kernel that
+    // waits for it.  The codes may be on their way before that.
+    const int issuer = kW4Unpackers + kW4Readers;
+    const bool producer = warp > issuer;
+    // producer: tiles 2 pw and 2 pw + 1 and, for pw < 2 * terms, a box of X (bit 0: half of the k-block, bit 1: lo rows).  A tile past the
+    // last column reads the last tile again; its sums are not stored.  Two terms: hi rows from row 0, lo rows from row RPAD / 2.
+    const int pw = warp - issuer - 1, x_rows = RPAD / p.terms;
+    const uint32_t my_tx = 2u * (1024u + 32u * NG + (has_zeros ? 16u * NG : 0u)) + (pw < 2 * p.terms ? (uint32_t)x_rows * 128u : 0u);
+    auto ask_codes = [&](int s, int slot) {
+        const uint32_t full = full0 + 8 * slot;
+        ptx::mbar_arrive_expect_tx(full, my_tx);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = 2 * pw + j, tile = min(GATED ? group * 4 + (i & 3) : group * 8 + i, p.n16 - 1);
+            const bool up = GATED && i >= 4;
+            const int64_t block = (int64_t)tile * p.KB + kb0 + s;
+            const uint32_t to = code_ring + slot * CODE_BYTES + i * BLOCK;
+            bulk_load(to, (up ? p.w[1].codes : p.w[0].codes) + block * 1024, 1024, full);
+            bulk_load(to + 1024, reinterpret_cast<const uint8_t*>(up ? p.w[1].scales : p.w[0].scales) + block * (32 * NG), 32 * NG, full);
+            if (has_zeros) bulk_load(to + 1024 + 32 * NG, (up ? p.w[1].zeros : p.w[0].zeros) + block * (16 * NG), 16 * NG, full);
+        }
+    };
+    auto ask_x = [&](int s, int slot) {
+        if (pw < 2 * p.terms)
+            ptx::tma_load_2d(x_ring + slot * X_BYTES + (pw & 1) * (RPAD * 128) + (pw >> 1) * (x_rows * 128), &tmX,
+                             (kb0 + s) * 128 + 64 * (pw & 1), (pw >> 1) * p.M + m0, full0 + 8 * slot);
+    };
+    const int ahead = min(DEPTH, steps);
+    if (!p.early) ptx::grid_dependency_wait();
+    if (producer && lane == 0)
+        for (int s = 0; s < ahead; ++s) ask_codes(s, s);
+    __syncwarp();
+    if (p.early) ptx::grid_dependency_wait();
+    if (producer && lane == 0)
+        for (int s = 0; s < ahead; ++s) ask_x(s, s);
+    __syncwarp();
+    if (warp == issuer) {
+        ptx::tmem_alloc(ptx::smem_addr(tmem_slot), TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    ptx::launch_dependents();
+    const uint32_t tmem = *tmem_slot;
+
+    // A wait that runs out leaves its mark in abort_flag and the device status; every loop below then runs on without waiting, so that
+    // all warps meet again at its end.
+    float y[COLS];
+    const int quarter = warp & 3, my_row = quarter * 32 + lane, my_col = (warp >= kW4Unpackers + 4 ? 1 : 0) * COLS;
+    if (producer) {
+        if (lane == 0)
+            for (int s = DEPTH, slot = 0, phase = 0; s < steps; ++s) {
+                (void)wait_bounded(empty0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 1);
+                ask_codes(s, slot);
+                ask_x(s, slot);
+                if (++slot == DEPTH) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
+        __syncwarp();
+    } else if (warp == issuer) {
+        const bool leader = ptx::elect_one();
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(RPAD >> 3) << 17) | ((128u >> 4) << 24);
+        for (int s = 0, slot = 0; s < steps; ++s) {
+            const int b = s & 1;
+            (void)__all_sync(0xFFFFFFFFu, wait_bounded(a_full0 + 8 * b, (uint32_t)(s >> 1) & 1u, abort_flag, KERNEL_ID, 2));
+            if (s >= 2) (void)__all_sync(0xFFFFFFFFu, wait_bounded(d_empty0 + 8 * b, (uint32_t)((s >> 1) - 1) & 1u, abort_flag, KERNEL_ID, 3));
+            ptx::tc_fence_after_sync();
+            const uint32_t a0 = base + b * kW4UmmaABytes, b0 = x_ring + slot * X_BYTES;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {            // 16 rows of K each
+                const uint64_t ad = ptx::make_smem_desc_sw128(a0 + (k >> 2) * (128 * 128) + (k & 3) * 32, 16, 1024);
+                const uint64_t bd = ptx::make_smem_desc_sw128(b0 + (k >> 2) * (RPAD * 128) + (k & 3) * 32, 16, 1024);
+                if (leader) ptx::umma_bf16(tmem + (uint32_t)(b * NG + k * 16 / G) * RPAD, ad, bd, idesc, (k * 16) % G == 0 ? 0u : 1u);
+            }
+            if (leader) ptx::umma_commit(done0 + 8 * b);
+            __syncwarp();
+            if (++slot == DEPTH) slot = 0;
+        }
+    } else if (warp < kW4Unpackers) {
+        const uint32_t a_at = base + (warp * 16 + g) * 128;                  // rows g and g + 8 of the tile; row & 7 is g
+        for (int s = 0, slot = 0, phase = 0; s < steps; ++s) {
+            const int b = s & 1;
+            (void)wait_bounded(full0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 4);
+            __syncwarp();
+            const uint8_t* block = code_ptr + slot * CODE_BYTES + warp * BLOCK;
+            uint32_t c[2][4], z[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4 v = *reinterpret_cast<const uint4*>(block + h * 512 + lane * 16);
+                c[h][0] = v.x; c[h][1] = v.y; c[h][2] = v.z; c[h][3] = v.w;
+                z[h] = kW4NoZeros;
+                if (has_zeros) {
+                    const uint8_t* zp = block + 1024 + 32 * NG + (g + 8 * h) * NG;
+                    if constexpr (G == 32) z[h] = *reinterpret_cast<const uint32_t*>(zp);
+                    else if constexpr (G == 64) z[h] = *reinterpret_cast<const uint16_t*>(zp);
+                    else z[h] = *zp;
+                }
+            }
+            if (s >= 2) {                            // the products that read this buffer of A have ended
+                (void)wait_bounded(done0 + 8 * b, (uint32_t)((s >> 1) - 1) & 1u, abort_flag, KERNEL_ID, 5);
+                __syncwarp();
+            }
+            const uint32_t to = a_at + b * kW4UmmaABytes;
+            auto unpack = [&](auto jc) {             // k = 32 J + 8 t .. + 7: chunk 4 (J & 1) + t of its half of K
+                constexpr int J = decltype(jc)::value;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t zc = __byte_perm(z[h], 0xC1C1C1C1u, 0x4040u | (J * 32 / G) | ((J * 32 / G) << 8));
+                    uint32_t v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u] = bf16x2_add(w4_codes_plus_16<J>(c[h][u]), zc);
+                    const uint32_t at = to + h * (8 * 128) + (J >> 1) * (128 * 128) + ((((J & 1) * 4 + t) ^ g) * 16);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                }
+            };
+            unpack(std::integral_constant<int, 0>{});
+            unpack(std::integral_constant<int, 1>{});
+            unpack(std::integral_constant<int, 2>{});
+            unpack(std::integral_constant<int, 3>{});
+            ptx::fence_proxy_async_smem();           // this thread's part of A, before the tensor core reads it
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(a_full0 + 8 * b);
+            if (++slot == DEPTH) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+    } else {
+        const uint32_t tmem_mine = tmem + ((uint32_t)(quarter * 32) << 16) + my_col;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) y[c] = 0.0f;
+        for (int s = 0, slot = 0, phase = 0; s < steps; ++s) {
+            const int b = s & 1;
+            (void)wait_bounded(full0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 6);       // the scales, too
+            __syncwarp();
+            const bf16* sp = reinterpret_cast<const bf16*>(code_ptr + slot * CODE_BYTES + (my_row >> 4) * BLOCK + 1024) + (my_row & 15) * NG;
+            float scale[NG];
+#pragma unroll
+            for (int gi = 0; gi < NG; ++gi) scale[gi] = __bfloat162float(sp[gi]);
+            (void)wait_bounded(done0 + 8 * b, (uint32_t)(s >> 1) & 1u, abort_flag, KERNEL_ID, 7);
+            ptx::tc_fence_after_sync();
+            __syncwarp();
+#pragma unroll
+            for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+                for (int c0 = 0; c0 < COLS; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_ld_32x16(tmem_mine + (uint32_t)((b * NG + gi) * RPAD + c0), v);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) y[c0 + c] = fmaf(scale[gi], __uint_as_float(v[c]), y[c0 + c]);
+                }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::mbar_arrive(d_empty0 + 8 * b);
+                ptx::mbar_arrive(empty0 + 8 * slot);
+            }
+            if (++slot == DEPTH) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == issuer) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, TMEM_COLS);
+    }
+
+    // sums of the cluster's CTAs, in a fixed order
+    constexpr int S = RPAD + 1;
+    float* red = reinterpret_cast<float*>(base_ptr);                         // [128][S], in place of A
+    if (warp >= kW4Unpackers && warp < issuer) {
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) red[my_row * S + my_col + c] = y[c];
+    }
+    __syncthreads();
+    if (C > 1) ptx::cluster_sync();
+    auto sum = [&](int row, int m) {
+        if (C == 1) return p.terms == 2 ? red[row * S + m] + red[row * S + RPAD / 2 + m] : red[row * S + m];
+        const uint32_t at = base + (uint32_t)(row * S + m) * 4u;
+        float hi[8], lo[8], v = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < C) {
+                const uint32_t peer = ptx::map_to_cta(at, (uint32_t)r);
+                hi[r] = ld_cluster_f32(peer);
+                lo[r] = p.terms == 2 ? ld_cluster_f32(peer + (RPAD / 2) * 4u) : 0.0f;
+            }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < C) v += hi[r] + lo[r];
+        return v;
+    };
+    constexpr int OUT_LOG2 = GATED ? 6 : 7;
+    const int outputs = M << OUT_LOG2, first = (int)((int64_t)outputs * rank / C), last = (int)((int64_t)outputs * (rank + 1) / C);
+    for (int i = first + threadIdx.x; i < last; i += kW4UmmaThreads) {
+        const int r = i & ((1 << OUT_LOG2) - 1), m = i >> OUT_LOG2, n = (group << OUT_LOG2) + r;
+        if (n >= p.N) continue;
+        const int64_t at = (int64_t)(m0 + m) * p.N + n;
+        if constexpr (GATED) w4_store_terms(p.out, at, (int64_t)p.M * p.N, gate_act_f32(sum(r, m), p.act) * sum(r + 64, m));
+        else p.out[at] = __float2bfloat16_rn(sum(r, m));
     }
     __syncwarp();
     if (C > 1) ptx::cluster_sync();                  // the peers may still be reading this CTA's sums

@@ -832,9 +832,9 @@ def w4_matmul(X, W4: W4Matrix, Y=None, stream=None, checked: bool = False) -> to
 
 
 def w4_plan(M: int, K: int, N: int, group: int = 128, terms: int = 1, gated: bool = False, sm_count: int = 0):
-    """gmlp_w4_plan: (persistent kernel, columns of eight rows, warps of a team, column groups per CTA, CTAs per cluster, parts,
-    CTAs per part, bytes of shared memory) of one product."""
-    out = (ctypes.c_int32 * 8)()
+    """gmlp_w4_plan: (kernel, padded rows per CTA, warps of a team or column groups per CTA, CTAs per cluster, parts, CTAs per
+    part, bytes of shared memory) of one product."""
+    out = (ctypes.c_int32 * 7)()
     rc = lib().gmlp_w4_plan(M, terms, K, N, int(gated), group, sm_count, out)
     if rc != OK:
         raise GmlpError(rc)

@@ -120,19 +120,25 @@ def test_w4_plan_of_every_size(lib, terms, gated, G):
     for M in range(1, gmlp.W4_MAX_M + 1):
         for K in (128, 256, 1024, 2048 + 128, 4096, 4096 + 128, 8192, 11008, 14336, 28672, 1 << 20):
             for N in (1, 16, 20, 33, 48, 64, 100, 256, 1000, 4096, 14336, 28672, 1 << 20):
-                stream, nt, gw, wr, c, parts, ctas, smem = gmlp.w4_plan(M, K, N, G, terms, gated, 148)
+                kind, rpad, gw, c, parts, ctas, smem = gmlp.w4_plan(M, K, N, G, terms, gated, 148)
                 kb, tiles, m_cta = -(-K // 256) * 2, -(-N // 16), -(-M // parts)
                 rows = m_cta * terms
-                assert 8 * nt >= rows > 8 * (nt - 1) and (parts - 1) * m_cta < M and smem <= 227 * 1024
-                if stream:                                       # per warp: its sums and a ring of three; all of X
-                    assert rows <= 16 and parts == 1 and c == 1 and gw in (2, 4, 8, 16) and ctas == min(tiles, 148)
-                    assert smem >= 16 * (512 + (3 if nt == 1 else 2) * 2 * block) + kb * 128 // G * nt * 32 + rows * (kb * 256 + 64)
-                    continue
-                wk = 8 // wr
-                assert rows <= 32 and wr in (1, 2, 4, 8) and gw == 0 and 1 <= c <= 8 and (c == 1 or kb >= 2 * wk * c)
-                assert smem >= 3 * (rows * (wk * 256 + 64) + 16 * block) and smem >= 8 * 32 * 8 * (nt | 1) * 4
-                assert ctas == c * -(-(-(-N // (16 if gated else 32))) // wr) and 1 <= parts <= 4
-    out = (ctypes.c_int32 * 8)()
+                assert rpad >= rows and (parts - 1) * m_cta < M and smem <= 227 * 1024 and 1 <= c <= 4
+                if kind == 0:                                    # per warp: its sums and a ring of two or three; sums of X, all of X
+                    assert rpad in (8, 16) and rows > rpad - 8 and parts == 1 and c == 1 and gw in (2, 4, 8, 16) and ctas == min(tiles, 148)
+                    assert smem >= 16 * (512 + (3 if rpad == 8 else 2) * 2 * block) + kb * 128 // G * rpad * 4 + rows * (kb * 256 + 64)
+                elif kind == 1:                                  # three stages of X and codes, then the sums of eight warps
+                    wk = 8 // gw
+                    assert rows <= 32 and rows > rpad - 8 and gw in (1, 2, 4, 8) and (c == 1 or kb >= 2 * wk * c) and parts <= 4
+                    assert smem >= 3 * (rows * (wk * 256 + 64) + 16 * block) and smem >= 8 * 32 * 8 * (rpad // 8 | 1) * 4
+                    assert ctas == c * -(-(-(-N // (16 if gated else 32))) // gw)
+                else:
+                    assert kind == 2 and M * terms > 16 and rpad in (32, 64) and (c == 1 or kb >= 8 * c) and 1 <= parts <= 2
+                    assert ctas == c * -(-tiles // (4 if gated else 8)) and (c == 1 or ctas * parts <= 148)
+                    # two buffers of A, five stages of X and codes, the sums in place of A, sixteen barriers
+                    assert smem >= 1024 + 2 * 32768 + 5 * (rpad * 256 + 8 * block) + 17 * 8 and 2 * 32768 >= 128 * (rpad + 1) * 4
+                    assert 2 * (128 // G) * rpad <= 512              # columns of TMEM
+    out = (ctypes.c_int32 * 7)()
     for bad in ((65, 1, 128, 16, 0, 128), (0, 1, 128, 16, 0, 128), (1, 3, 128, 16, 0, 128), (1, 1, 0, 16, 0, 128), (1, 1, 128, 16, 0, 48)):
         assert lib.gmlp_w4_plan(*bad, 148, out) == gmlp.ERR_SHAPE
     assert lib.gmlp_w4_plan(1, 1, 128, 16, 0, 128, 148, None) == gmlp.ERR_NULL

@@ -46,7 +46,7 @@ W4Plan w4_plan(int M, int terms, int KB, int n16, bool gated, int G, int sms) {
         while (p.cluster < 4 && groups128 * p.m_parts <= cluster_capacity_estimate(p.cluster + 1, sms) && KB >= 8 * (p.cluster + 1)) ++p.cluster;
         p.ctas = groups128 * p.cluster;
         p.threads = gmlp::kW4UmmaThreads;
-        p.smem = gmlp::w4_umma_smem(8 * p.nt, G);
+        p.smem = gmlp::w4_umma_smem(8 * p.nt);
         return p;
     }
     p.nt = (rows_cta + 7) / 8;

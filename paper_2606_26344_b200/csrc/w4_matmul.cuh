@@ -620,20 +620,20 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_tile_kernel(const W4GemmArgs
 // ------------------------------------------------------------------ more than 16 rows of X: tcgen05
 // One CTA per 128 columns of W (gated: 64 gate and the same 64 up columns) and up to 64 rows of X (blockIdx.y: further rows), K over a
 // cluster of C CTAs that add their sums in distributed shared memory.  Four kinds of warps pass k-blocks of 128 on:
-//   4 producers   bulk copies of two tiles' codes and parameters each, TMA boxes of X (the B operand: K-major, 128-byte swizzle);
-//                 a bulk copy costs its thread some 90 cycles, so one thread for all would set the pace;
+//   4 producers   bulk copies of two tiles' codes each, TMA boxes of X (the B operand: K-major, 128-byte swizzle); a bulk copy takes
+//                 some 90 cycles however small it is, so the parameters are read a k-block ahead by the warps that need them;
 //   8 unpackers   a tile each: codes to q - z, exact in bf16, straight into the same layout as the A operand (a lane's eight
-//                 neighbouring k of a column are one 16-byte store; two buffers);
+//                 neighbouring k of a column are one 16-byte store; three buffers: with two, unpacking and products took turns);
 //   1 issuer      the tcgen05.mma of each group of G rows of K, into columns of TMEM of its own (two buffers);
 //   8 readers     tcgen05.ld of the sums (a lane per column of W, half of the rows of X per warp), scaled in fp32 and added in
 //                 registers: no weight is rounded here either.
 // (With all warps doing everything in step, one barrier per k-block, a k-block took 1750 cycles.)
 constexpr int kW4Producers = 4, kW4Unpackers = 8, kW4Readers = 8;
 constexpr int kW4UmmaThreads = 32 * (kW4Unpackers + kW4Readers + 1 + kW4Producers);
-constexpr int kW4UmmaDepth = 5;
+constexpr int kW4UmmaDepth = 4, kW4ABuffers = 3;
 constexpr uint32_t kW4UmmaABytes = 128 * 256;
-__host__ __device__ constexpr uint32_t w4_umma_smem(int rpad, int G) {
-    return 1024u + 2u * kW4UmmaABytes + (uint32_t)kW4UmmaDepth * ((uint32_t)rpad * 256u + 8u * (uint32_t)w4_slot_bytes(G, 1)) + 192u;
+__host__ __device__ constexpr uint32_t w4_umma_smem(int rpad) {
+    return 1024u + (uint32_t)kW4ABuffers * kW4UmmaABytes + (uint32_t)kW4UmmaDepth * ((uint32_t)rpad * 256u + 8u * 1024u) + 192u;
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -646,21 +646,22 @@ __global__ void __launch_bounds__(kW4UmmaThreads, 1)
 w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
 {
     extern __shared__ __align__(128) uint8_t w4_smem[];
-    constexpr int NG = 128 / G, BLOCK = w4_slot_bytes(G, 1), COLS = RPAD / 2;              // rows of X per reader
-    constexpr uint32_t X_BYTES = RPAD * 256, CODE_BYTES = 8 * BLOCK, TMEM_COLS = 2 * NG * RPAD;
+    constexpr int NG = 128 / G, COLS = RPAD / 2;     // COLS: rows of X per reader
+    constexpr uint32_t X_BYTES = RPAD * 256, CODE_BYTES = 8 * 1024, TMEM_COLS = 2 * NG * RPAD;
     constexpr int KERNEL_ID = 20, DEPTH = kW4UmmaDepth;
     const uint32_t raw = ptx::smem_addr(w4_smem), base = (raw + 1023u) & ~1023u;           // the same in every CTA of a cluster
     uint8_t* base_ptr = w4_smem + (base - raw);
-    // two buffers of A, a ring of X (all on 1024-byte boundaries: the swizzle goes by address), a ring of eight tiles' codes
-    const uint32_t x_ring = base + 2 * kW4UmmaABytes, code_ring = x_ring + DEPTH * X_BYTES;
-    uint8_t* code_ptr = base_ptr + 2 * kW4UmmaABytes + DEPTH * X_BYTES;
+    // buffers of A, a ring of X (all on 1024-byte boundaries: the swizzle goes by address), a ring of eight tiles' codes
+    const uint32_t x_ring = base + kW4ABuffers * kW4UmmaABytes, code_ring = x_ring + DEPTH * X_BYTES;
+    uint8_t* code_ptr = base_ptr + kW4ABuffers * kW4UmmaABytes + DEPTH * X_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(code_ptr + DEPTH * CODE_BYTES);
     const uint32_t full0 = ptx::smem_addr(bars);                             // [DEPTH] a stage's copies have landed
     const uint32_t empty0 = full0 + 8 * DEPTH;                               // [DEPTH] its sums have been read: it is free
-    const uint32_t a_full0 = empty0 + 8 * DEPTH;                             // [2] A is unpacked
-    const uint32_t done0 = a_full0 + 16;                                     // [2] the products have ended
-    const uint32_t d_empty0 = done0 + 16;                                    // [2] their sums have been read
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * DEPTH + 6);
+    const uint32_t a_full0 = empty0 + 8 * DEPTH;                             // [3] A is unpacked
+    const uint32_t a_empty0 = a_full0 + 8 * kW4ABuffers;                     // [3] the products that read it have ended
+    const uint32_t done0 = a_empty0 + 8 * kW4ABuffers;                       // [2] the products have ended: their sums
+    const uint32_t d_empty0 = done0 + 16;                                    // [2] have been read
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * DEPTH + 2 * kW4ABuffers + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int C = p.cluster, rank = C > 1 ? (int)ptx::cluster_ctarank() : 0, group = (int)blockIdx.x / C;
@@ -673,8 +674,11 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
             ptx::mbar_init(full0 + 8 * i, kW4Producers);
             ptx::mbar_init(empty0 + 8 * i, kW4Readers);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kW4ABuffers; ++i) {
             ptx::mbar_init(a_full0 + 8 * i, kW4Unpackers);
+            ptx::mbar_init(a_empty0 + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(done0 + 8 * i, 1);
             ptx::mbar_init(d_empty0 + 8 * i, kW4Readers);
         }
@@ -691,19 +695,16 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
     // producer: tiles 2 pw and 2 pw + 1 and, for pw < 2 * terms, a box of X (bit 0: half of the k-block, bit 1: lo rows).  A tile past the
     // last column reads the last tile again; its sums are not stored.  Two terms: hi rows from row 0, lo rows from row RPAD / 2.
     const int pw = warp - issuer - 1, x_rows = RPAD / p.terms;
-    const uint32_t my_tx = 2u * (1024u + 32u * NG + (has_zeros ? 16u * NG : 0u)) + (pw < 2 * p.terms ? (uint32_t)x_rows * 128u : 0u);
+    const uint32_t my_tx = 2048u + (pw < 2 * p.terms ? (uint32_t)x_rows * 128u : 0u);
+    auto tile_of = [&](int i) { return min(GATED ? group * 4 + (i & 3) : group * 8 + i, p.n16 - 1); };
     auto ask_codes = [&](int s, int slot) {
         const uint32_t full = full0 + 8 * slot;
         ptx::mbar_arrive_expect_tx(full, my_tx);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int i = 2 * pw + j, tile = min(GATED ? group * 4 + (i & 3) : group * 8 + i, p.n16 - 1);
-            const bool up = GATED && i >= 4;
-            const int64_t block = (int64_t)tile * p.KB + kb0 + s;
-            const uint32_t to = code_ring + slot * CODE_BYTES + i * BLOCK;
-            bulk_load(to, (up ? p.w[1].codes : p.w[0].codes) + block * 1024, 1024, full);
-            bulk_load(to + 1024, reinterpret_cast<const uint8_t*>(up ? p.w[1].scales : p.w[0].scales) + block * (32 * NG), 32 * NG, full);
-            if (has_zeros) bulk_load(to + 1024 + 32 * NG, (up ? p.w[1].zeros : p.w[0].zeros) + block * (16 * NG), 16 * NG, full);
+            const int i = 2 * pw + j;
+            bulk_load(code_ring + slot * CODE_BYTES + i * 1024,
+                      (GATED && i >= 4 ? p.w[1].codes : p.w[0].codes) + ((int64_t)tile_of(i) * p.KB + kb0 + s) * 1024, 1024, full);
         }
     };
     auto ask_x = [&](int s, int slot) {
@@ -749,47 +750,65 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
     } else if (warp == issuer) {
         const bool leader = ptx::elect_one();
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(RPAD >> 3) << 17) | ((128u >> 4) << 24);
-        for (int s = 0, slot = 0; s < steps; ++s) {
+        const uint32_t desc_hi = (uint32_t)(ptx::make_smem_desc_sw128(0, 0, 1024) >> 32);
+        const uint32_t a_lo0 = (uint32_t)ptx::make_smem_desc_sw128(base, 16, 1024), x_lo0 = (uint32_t)ptx::make_smem_desc_sw128(x_ring, 16, 1024);
+        for (int s = 0, slot = 0, ab = 0, a_phase = 0; s < steps; ++s) {
             const int b = s & 1;
-            (void)__all_sync(0xFFFFFFFFu, wait_bounded(a_full0 + 8 * b, (uint32_t)(s >> 1) & 1u, abort_flag, KERNEL_ID, 2));
+            (void)__all_sync(0xFFFFFFFFu, wait_bounded(a_full0 + 8 * ab, (uint32_t)a_phase, abort_flag, KERNEL_ID, 2));
             if (s >= 2) (void)__all_sync(0xFFFFFFFFu, wait_bounded(d_empty0 + 8 * b, (uint32_t)((s >> 1) - 1) & 1u, abort_flag, KERNEL_ID, 3));
             ptx::tc_fence_after_sync();
-            const uint32_t a0 = base + b * kW4UmmaABytes, b0 = x_ring + slot * X_BYTES;
+            const uint32_t a_lo = a_lo0 + ab * (kW4UmmaABytes / 16), x_lo = x_lo0 + slot * (X_BYTES / 16), d = tmem + (uint32_t)(b * NG) * RPAD;
+            if (leader) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {            // 16 rows of K each
-                const uint64_t ad = ptx::make_smem_desc_sw128(a0 + (k >> 2) * (128 * 128) + (k & 3) * 32, 16, 1024);
-                const uint64_t bd = ptx::make_smem_desc_sw128(b0 + (k >> 2) * (RPAD * 128) + (k & 3) * 32, 16, 1024);
-                if (leader) ptx::umma_bf16(tmem + (uint32_t)(b * NG + k * 16 / G) * RPAD, ad, bd, idesc, (k * 16) % G == 0 ? 0u : 1u);
+                for (int k = 0; k < 8; ++k)          // 16 rows of K each: 32 bytes on in a 64-wide half, halves 128 (RPAD) rows apart
+                    ptx::umma_bf16_halves(d + (uint32_t)(k * 16 / G) * RPAD, a_lo + (k >> 2) * 1024 + (k & 3) * 2,
+                                          x_lo + (k >> 2) * (RPAD * 8) + (k & 3) * 2, desc_hi, idesc, (k * 16) % G == 0 ? 0u : 1u);
             }
-            if (leader) ptx::umma_commit(done0 + 8 * b);
+            if (leader) {
+                ptx::umma_commit(done0 + 8 * b);
+                ptx::umma_commit(a_empty0 + 8 * ab);
+            }
             __syncwarp();
             if (++slot == DEPTH) slot = 0;
+            if (++ab == kW4ABuffers) {
+                ab = 0;
+                a_phase ^= 1;
+            }
         }
+        // the last arrival that the tensor core owes this CTA's shared memory
+        (void)__all_sync(0xFFFFFFFFu, wait_bounded(a_empty0 + 8 * ((steps - 1) % kW4ABuffers), (uint32_t)((steps - 1) / kW4ABuffers) & 1u,
+                                                   abort_flag, KERNEL_ID, 8));
     } else if (warp < kW4Unpackers) {
         const uint32_t a_at = base + (warp * 16 + g) * 128;                  // rows g and g + 8 of the tile; row & 7 is g
-        for (int s = 0, slot = 0, phase = 0; s < steps; ++s) {
-            const int b = s & 1;
+        const uint8_t* zp = has_zeros ? (GATED && warp >= 4 ? p.w[1].zeros : p.w[0].zeros) + (((int64_t)tile_of(warp) * p.KB + kb0) * 16 + g) * NG : nullptr;
+        auto read_zeros = [&](uint32_t (&z)[2], int s) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t* from = zp + ((int64_t)s * 16 + 8 * h) * NG;
+                if constexpr (G == 32) z[h] = ld_4B(from);
+                else if constexpr (G == 64) z[h] = ld_2B(from);
+                else z[h] = ld_1B(from);
+            }
+        };
+        uint32_t z[2] = {kW4NoZeros, kW4NoZeros}, z_next[2] = {kW4NoZeros, kW4NoZeros};
+        if (has_zeros) read_zeros(z_next, 0);
+        for (int s = 0, slot = 0, phase = 0, ab = 0, a_phase = 1; s < steps; ++s) {
             (void)wait_bounded(full0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 4);
             __syncwarp();
-            const uint8_t* block = code_ptr + slot * CODE_BYTES + warp * BLOCK;
-            uint32_t c[2][4], z[2];
+            const uint8_t* block = code_ptr + slot * CODE_BYTES + warp * 1024;
+            uint32_t c[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint4 v = *reinterpret_cast<const uint4*>(block + h * 512 + lane * 16);
                 c[h][0] = v.x; c[h][1] = v.y; c[h][2] = v.z; c[h][3] = v.w;
-                z[h] = kW4NoZeros;
-                if (has_zeros) {
-                    const uint8_t* zp = block + 1024 + 32 * NG + (g + 8 * h) * NG;
-                    if constexpr (G == 32) z[h] = *reinterpret_cast<const uint32_t*>(zp);
-                    else if constexpr (G == 64) z[h] = *reinterpret_cast<const uint16_t*>(zp);
-                    else z[h] = *zp;
-                }
+                z[h] = z_next[h];
             }
-            if (s >= 2) {                            // the products that read this buffer of A have ended
-                (void)wait_bounded(done0 + 8 * b, (uint32_t)((s >> 1) - 1) & 1u, abort_flag, KERNEL_ID, 5);
+            if (has_zeros && s + 1 < steps) read_zeros(z_next, s + 1);
+            if (s >= kW4ABuffers) {                  // the products that read this buffer of A have ended
+                (void)wait_bounded(a_empty0 + 8 * ab, (uint32_t)a_phase, abort_flag, KERNEL_ID, 5);
                 __syncwarp();
             }
-            const uint32_t to = a_at + b * kW4UmmaABytes;
+            const uint32_t to = a_at + ab * kW4UmmaABytes;
             auto unpack = [&](auto jc) {             // k = 32 J + 8 t .. + 7: chunk 4 (J & 1) + t of its half of K
                 constexpr int J = decltype(jc)::value;
 #pragma unroll
@@ -808,7 +827,11 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
             unpack(std::integral_constant<int, 3>{});
             ptx::fence_proxy_async_smem();           // this thread's part of A, before the tensor core reads it
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(a_full0 + 8 * b);
+            if (lane == 0) ptx::mbar_arrive(a_full0 + 8 * ab);
+            if (++ab == kW4ABuffers) {
+                ab = 0;
+                a_phase ^= 1;
+            }
             if (++slot == DEPTH) {
                 slot = 0;
                 phase ^= 1;
@@ -818,14 +841,27 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
         const uint32_t tmem_mine = tmem + ((uint32_t)(quarter * 32) << 16) + my_col;
 #pragma unroll
         for (int c = 0; c < COLS; ++c) y[c] = 0.0f;
-        for (int s = 0, slot = 0, phase = 0; s < steps; ++s) {
+        const int i = my_row >> 4;
+        const bf16* sp = (GATED && i >= 4 ? p.w[1].scales : p.w[0].scales) + (((int64_t)tile_of(i) * p.KB + kb0) * 16 + (my_row & 15)) * NG;
+        uint32_t next[G == 32 ? 2 : 1];              // the next k-block's scales
+        auto read_scales = [&](int s) {
+            const bf16* from = sp + (int64_t)s * 16 * NG;
+            if constexpr (G == 32) {
+                const uint2 v = ld_8B(from);
+                next[0] = v.x; next[1] = v.y;
+            } else if constexpr (G == 64) {
+                next[0] = ld_4B(from);
+            } else {
+                next[0] = ld_2B(from);
+            }
+        };
+        read_scales(0);
+        for (int s = 0, slot = 0; s < steps; ++s) {
             const int b = s & 1;
-            (void)wait_bounded(full0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 6);       // the scales, too
-            __syncwarp();
-            const bf16* sp = reinterpret_cast<const bf16*>(code_ptr + slot * CODE_BYTES + (my_row >> 4) * BLOCK + 1024) + (my_row & 15) * NG;
             float scale[NG];
 #pragma unroll
-            for (int gi = 0; gi < NG; ++gi) scale[gi] = __bfloat162float(sp[gi]);
+            for (int gi = 0; gi < NG; ++gi) scale[gi] = (gi & 1) ? bf16_hi(next[gi >> 1]) : bf16_lo(next[gi >> 1]);
+            if (s + 1 < steps) read_scales(s + 1);
             (void)wait_bounded(done0 + 8 * b, (uint32_t)(s >> 1) & 1u, abort_flag, KERNEL_ID, 7);
             ptx::tc_fence_after_sync();
             __syncwarp();
@@ -845,10 +881,7 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
                 ptx::mbar_arrive(d_empty0 + 8 * b);
                 ptx::mbar_arrive(empty0 + 8 * slot);
             }
-            if (++slot == DEPTH) {
-                slot = 0;
-                phase ^= 1;
-            }
+            if (++slot == DEPTH) slot = 0;
         }
     }
     ptx::tc_fence_before_sync();

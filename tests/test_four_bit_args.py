@@ -135,8 +135,8 @@ def test_w4_plan_of_every_size(lib, terms, gated, G):
                 else:
                     assert kind == 2 and M * terms > 16 and rpad in (32, 64) and (c == 1 or kb >= 8 * c) and 1 <= parts <= 2
                     assert ctas == c * -(-tiles // (4 if gated else 8)) and (c == 1 or ctas * parts <= 148)
-                    # two buffers of A, five stages of X and codes, the sums in place of A, sixteen barriers
-                    assert smem >= 1024 + 2 * 32768 + 5 * (rpad * 256 + 8 * block) + 17 * 8 and 2 * 32768 >= 128 * (rpad + 1) * 4
+                    # three buffers of A, four stages of X and codes, the sums in place of A, eighteen barriers
+                    assert smem >= 1024 + 3 * 32768 + 4 * (rpad * 256 + 8 * 1024) + 19 * 8 and 3 * 32768 >= 128 * (rpad + 1) * 4
                     assert 2 * (128 // G) * rpad <= 512              # columns of TMEM
     out = (ctypes.c_int32 * 7)()
     for bad in ((65, 1, 128, 16, 0, 128), (0, 1, 128, 16, 0, 128), (1, 3, 128, 16, 0, 128), (1, 1, 0, 16, 0, 128), (1, 1, 128, 16, 0, 48)):

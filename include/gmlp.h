@@ -419,8 +419,8 @@ int gmlp_kv4_gather(const gmlp_kv4_rows_args* args);
  * Q, O [B * q_len, n_q_heads * head_dim] bf16, position by position; request b's key j is in slot
  * block_table[b][j / page_size] * page_size + j % page_size.  lengths[b] counts the keys, the new positions' included (append them
  * first).  A position that sees no key (L = 0, or L < q_len) gets zeros.  What the pages hold past a request's end, and table entries
- * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value is rounded to bf16 for the
- * second product; O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table are reported as above;
+ * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value enters the second
+ * product with 16 bits of significand (two bf16 terms); O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table are reported as above;
  * their keys are left out.
  * workspace: gmlp_kv4_workspace_bytes(); may be NULL where that is 0; no state is kept in it between calls.
  */

@@ -164,14 +164,18 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 // ------------------------------------------------------------------------------------------------ attention
 // T new positions per request (the last T of its sequence), O = softmax(scale * Q K^T) V over the keys up to each position's
 // own.  A CTA takes one request, one key/value head, up to 8 NT of its T * (query heads per key/value head) query rows and a range
-// of the keys; its four warps take 16-token tiles in turn.  Per tile and warp (flash-style, running maximum and sum in fp32):
+// of the keys; its four warps take 16-token tiles in turn.  Per tile and warp (running maximum and sum in fp32):
 //   S^T = K Q^T   tokens are the 16 mma rows, query rows the 8 columns, 16 + q exact in bf16; (16 + z) times the query row's sum
 //                 over the group comes off, and the token's scale (times the softmax scale) is a factor, both in fp32;
-//   P'  = exp2(S - m) * s_v, rounded to bf16 once as the operand of the second product; transposed in registers (movmatrix);
-//   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same
-//                 rounded P' and taken off at the end (a warp sums a few hundred tokens before that: the part that cancels costs
-//                 some 2^-12 of a quantiser's step).
-// Bound by HBM and by the issue slots of the unpacking (about two instructions per value); the tensor pipe idles.
+//   P'  = exp2(S - m) * s_v as two bf16 terms (hi + lo: rounded to one, the output was 1.4 times as far off as its own rounding
+//                 leaves it), transposed in registers (movmatrix);
+//   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same two
+//                 terms and taken off at the end and every 64 tiles: the accumulator sees that part of at most 1024 tokens, and its
+//                 rounding costs some 2^-13 of a quantiser's step, however long the request.
+// Bound by the issue slots and the half-rate integer pipe of the unpacking, then by HBM: 64 requests of 1..8192 keys, 32 / 8 heads of
+// 128, groups of 64: 129 us (2.8 TB/s, 0.43 of the measured copy rate); one request of 131071 keys, 64 / 8 heads, groups of 128: 55 us
+// (2.6 TB/s).  With one term for P' 115 and 51 us; so, but with loads into registers instead of the rings 146 and 67; with the maximum
+// followed at every tile and q - z formed before the products 126 and 53.
 // Each warp has a ring of three tiles in shared memory that asynchronous copies fill, two tiles ahead; the page-table entry is read
 // one tile earlier still.  Row g of a tile's products is token g ^ (g >> 1) of its eight (and so for the second eight), and for
 // D = 128 the 16-byte chunks of rows 2, 3, 6, 7, ... swap places by two: so the keys' reads (a row by four lanes) and the values' (a
@@ -317,6 +321,26 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             for (int e = 0; e < 4; ++e) o[i][n][e] = 0.0f;
     }
 
+    auto take_off = [&]() {                          // o -= the sum of P' (16 + z), which every lane holds a part of
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int gi = 0; gi < NG; ++gi) {
+                    float z = zsum[gi][n][e];
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, x);
+#pragma unroll
+                    for (int j = gi * PER; j < (gi + 1) * PER; ++j)
+#pragma unroll
+                        for (int hw = 0; hw < 2; ++hw) {
+                            o[j * 2 + hw][n][e] -= z;
+                            o[j * 2 + hw][n][2 + e] -= z;
+                        }
+                    zsum[gi][n][e] = 0.0f;
+                }
+    };
     const int32_t* table = p.table + (int64_t)b * p.width;
     // Places of this warp's tiles, stepped without divisions: page-table entry `entry`, token `place` of its page.
     const int stride = kKv4Warps * kKv4Tile, page_step = stride / p.c.page_size, place_step = stride % p.c.page_size;
@@ -369,7 +393,9 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
     const int gray = g ^ (g >> 1);                   // the token of row g
     const int swap = D == 128 ? ((gray >> 1) & 1) << 1 : 0;
     const uint8_t* slot = ring;
+    int tiles = 0;
     for (int token = first + warp * kKv4Tile; token < last; token += stride) {
+        if ((tiles++ & 63) == 63) take_off();
         cp_async_wait_but<kKv4Depth - 2>();          // this tile has landed,
         __syncwarp();                                // for every lane, and the slot of the tile before is free
         ask(kKv4Depth - 1);
@@ -497,7 +523,7 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
         // second product, group by group
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi) {
-            uint32_t pb[NT][2];
+            uint32_t pb[NT][2], pl[NT][2];           // P' as two terms
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -510,9 +536,11 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                     }
                     const uint32_t w = pack_bf16x2(a, c);
                     const float z = bf16_hi(cur.vp[h][gi]) + 16.0f;
-                    zsum[gi][n][0] = fmaf(bf16_lo(w), z, zsum[gi][n][0]);
-                    zsum[gi][n][1] = fmaf(bf16_hi(w), z, zsum[gi][n][1]);
+                    const uint32_t r = pack_bf16x2(a - bf16_lo(w), c - bf16_hi(w));
+                    zsum[gi][n][0] = fmaf(bf16_lo(w) + bf16_lo(r), z, zsum[gi][n][0]);     // of what the product sees
+                    zsum[gi][n][1] = fmaf(bf16_hi(w) + bf16_hi(r), z, zsum[gi][n][1]);
                     pb[n][h] = movmatrix_trans(w);
+                    pl[n][h] = movmatrix_trans(r);
                 }
 #pragma unroll
             for (int hw = 0; hw < 2; ++hw) {
@@ -535,7 +563,10 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                     const uint32_t a0 = kv4_codes_plus_16(lo01, 4 * j), a2 = kv4_codes_plus_16(lo89, 4 * j);
                     const uint32_t a1 = kv4_codes_plus_16(hi01, 4 * j), a3 = kv4_codes_plus_16(hi89, 4 * j);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                    for (int n = 0; n < NT; ++n) {
+                        mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                        mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pl[n][0], pl[n][1]);
+                    }
                 }
             }
         }
@@ -544,16 +575,13 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
     __syncthreads();                                 // the rings are done with: the results take their place
 
     // sums over the lanes that share a column, then the warps' results side by side
+    take_off();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) {
-                l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], x);
-#pragma unroll
-                for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] += __shfl_xor_sync(0xFFFFFFFFu, zsum[gi][n][e], x);
-            }
+            for (int x = 4; x < 32; x <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], x);
             const int c = n * 8 + 2 * t + e;
             if (g == 0) {
                 s_m[warp][c] = m[n][e];
@@ -563,10 +591,9 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
                 for (int hw = 0; hw < 2; ++hw) {
-                    const float z = zsum[j / PER][n][e];
                     float* at = &s_o[warp][c][32 * j + 4 * g + 2 * hw];
-                    at[0] = o[j * 2 + hw][n][e] - z;
-                    at[1] = o[j * 2 + hw][n][2 + e] - z;
+                    at[0] = o[j * 2 + hw][n][e];
+                    at[1] = o[j * 2 + hw][n][2 + e];
                 }
         }
     __syncthreads();

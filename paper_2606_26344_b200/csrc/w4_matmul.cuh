@@ -66,8 +66,8 @@ __device__ __forceinline__ uint32_t bf16x2_add(uint32_t a, uint32_t b) {
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0x3F803F80u), "r"(b));
     return d;
 }
-// (w & mask) | bits in one instruction (left to itself the compiler splits the and-or of two constants in two, and these run at half
-// rate: a third of the kernel's issue slots).
+// (w & mask) | bits in one instruction (left to itself the compiler splits the and-or of two constants in two, on the
+// half-rate integer pipe: 8192 x 28672 at M = 1 took 38.4 us so, 32.7 us as one).
 __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
     uint32_t d;
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(bits));
@@ -271,9 +271,12 @@ __device__ __forceinline__ void w4_store_terms(bf16* out, int64_t at, int64_t te
 // ------------------------------------------------------------------ up to 16 rows of X: a persistent stream
 // One CTA of 16 warps per SM.  A team of GW warps walks over column tiles; its warps deal out the pairs of k-blocks of a tile (gated:
 // half of them those of the gate tile, half those of the up tile), each with a ring of its own in shared memory that asynchronous
-// copies fill, across tiles too, so that the stream of codes does not pause at a tile's end.  (Held in registers instead, the loads of
-// several stages shared the few scoreboards of a warp.)  X stays in shared memory for the whole kernel, with its sums over the groups;
+// copies fill, across tiles too, so that the stream of codes does not pause at a tile's end.  X stays in shared memory for the whole kernel, with its sums over the groups;
 // only the sums of a tile cross the warps of a team.
+// Bound by the issue slots and the half-rate integer pipe (about 70 integer instructions per kilobyte of codes and warp), then by HBM:
+// 8192 x 28672, groups of 32 with zero points, M = 1: 36 us (3.9 TB/s, 0.60 of the measured copy rate); 4096 x 14336, groups of 128,
+// M = 8: 11 us.  Loads into registers instead of the rings: 46.9 against 42.0 us (8192 x 28672, groups of 128); 32 or 24 warps with
+// shorter rings, 30 us like these 16; without the rotations, which is not a result, 24 us.
 constexpr int kW4StreamWarps = 16;
 __host__ __device__ constexpr int w4_ring_depth(int nt) { return nt == 1 ? 3 : 2; }      // slots; two columns of eight need the room for X
 constexpr int kW4StreamThreads = 32 * kW4StreamWarps;
@@ -628,6 +631,8 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_tile_kernel(const W4GemmArgs
 //   8 readers     tcgen05.ld of the sums (a lane per column of W, half of the rows of X per warp), scaled in fp32 and added in
 //                 registers: no weight is rounded here either.
 // (With all warps doing everything in step, one barrier per k-block, a k-block took 1750 cycles.)
+// Bound by the hand-over from one kind of warps to the next, some 1000 cycles a k-block: 4096 x 14336 at M = 64 25 us (48 with tiles), 8B
+// layer at M = 33 94 us (158 with tiles).
 constexpr int kW4Producers = 4, kW4Unpackers = 8, kW4Readers = 8;
 constexpr int kW4UmmaThreads = 32 * (kW4Unpackers + kW4Readers + 1 + kW4Producers);
 constexpr int kW4UmmaDepth = 4, kW4ABuffers = 3;

@@ -325,8 +325,10 @@ int gmlp_w4_dequantize(const gmlp_w4_layout_args* args);
 
 /*
  * Y = X W for a 4-bit W: X [M, K], Y [M, N] row-major bf16, M at most GMLP_W4_MAX_M.  Codes are used exactly, group sums and their
- * scaling are fp32, Y is rounded once.  Beyond GMLP_W4_MAX_M tokens the product is no longer bound by the weights' bytes:
- * dequantise and use the bf16 operators (GMLP_ERR_SHAPE).  Everything is read in stream order (the weights too).
+ * scaling are fp32, Y is rounded once.  From
+ * some twenty tokens on the products, not the weights' bytes, set the time, and the bf16 operators on dequantised weights are faster
+ * where there is memory for those; more than GMLP_W4_MAX_M tokens are refused (GMLP_ERR_SHAPE).  Everything is read in stream order
+ * (the weights too).
  */
 #define GMLP_W4_MAX_M 64
 typedef struct gmlp_w4_matmul_args {

@@ -15,6 +15,7 @@ W4Plan w4_plan(int M, int terms, int KB, int n16, bool gated, int G, int sms) {
     W4Plan p{};
     const int rows = M * terms;
     // The persistent kernel, where all of X fits beside the rings.
+    if (rows <= 16) {
         const uint64_t smem = gmlp::w4_stream_bytes(rows, KB, G);
         if (smem <= kW4SmemMost) {
             p.kind = kW4Stream;

@@ -437,7 +437,7 @@ typedef struct gmlp_kv4_attention_args {
     const void* lengths;      /* device, [B] int32 */
     int64_t B, table_width;   /* B at most 65535, table_width * page_size at most 2^30 */
     int32_t n_q_heads, q_len;
-    float scale;              /* e.g. 1 / sqrt(head_dim); any finite number */
+    float scale;              /* e.g. 1 / sqrt(head_dim); any number up to 2e38 */
     int32_t reserved;         /* must be 0 */
     void* stream;             /* cudaStream_t */
     void* workspace;          /* 256-byte aligned */

@@ -60,8 +60,7 @@ Kv4Plan kv4_plan(int64_t B, int T, int ratio, int n_kv_heads, int head_dim, int6
     p.nt = cols <= 8 ? 1 : 2;
     p.col_tiles = (int)((cols + 8 * p.nt - 1) / (8 * p.nt));
     const int64_t ctas = B * n_kv_heads * p.col_tiles;
-    int64_t target = (int64_t)sms * 4;
-    int64_t long_keys = 2048;
+    const int64_t target = (int64_t)sms * 4, long_keys = 2048;
     int64_t splits = (target + ctas - 1) / ctas;
     const int64_t by_length = (most_keys + long_keys - 1) / long_keys, most = (most_keys + 127) / 128;
     if (splits < by_length && ctas * by_length <= 1 << 20) splits = by_length;
@@ -89,7 +88,8 @@ int kv4_attention_impl(const gmlp_kv4_attention_args* a) {
     if (rc != GMLP_OK) return rc;
     rc = check_kv4_attention(a->B, a->q_len, a->n_q_heads, a->cache.n_kv_heads, a->table_width, a->cache.page_size);
     if (rc != GMLP_OK) return rc;
-    if (!(a->scale - a->scale == 0.0f)) return GMLP_ERR_FLAGS;
+    const float scale_log2 = a->scale * 1.4426950408889634f;                 // exponentials are powers of two
+    if (!(scale_log2 - scale_log2 == 0.0f)) return GMLP_ERR_FLAGS;
     if (a->B == 0) return GMLP_OK;
     if (!a->Q || !a->O || !a->block_table || !a->lengths) return GMLP_ERR_NULL;
     if (!aligned16(a->Q) || !aligned16(a->O) || (reinterpret_cast<uintptr_t>(a->block_table) & 3u) ||
@@ -119,7 +119,7 @@ int kv4_attention_impl(const gmlp_kv4_attention_args* a) {
     k.width = (int)a->table_width;
     k.splits = plan.splits;
     k.col_tiles = plan.col_tiles;
-    k.scale_log2 = a->scale * 1.4426950408889634f;
+    k.scale_log2 = scale_log2;
     const dim3 grid((unsigned)plan.splits, (unsigned)(k.c.n_kv_heads * plan.col_tiles), (unsigned)a->B);
     if (grid.y > 65535u) return GMLP_ERR_SHAPE;
     prof_begin(st);

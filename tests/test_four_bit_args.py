@@ -291,3 +291,12 @@ def test_plain_quantiser_properties():
     assert bool(((v - x.double()).abs()[ok] <= (1.0 + 15 * 2.0 ** -8) * step[ok]).all())
     q, s, z = F.quantize(x[4:], 32, zero_points=False)
     assert bool((z == 8).all()) and int(q.min()) >= 1
+
+
+def test_a_scale_that_overflows_in_powers_of_two_is_refused():
+    """The kernel multiplies scores by scale * log2(e): 3e38 is a float, 4.3e38 is not, and inf * 0 would be NaN."""
+    a = attention_args()
+    a.scale = 3e38
+    assert gmlp.lib().gmlp_kv4_attention(ctypes.byref(a)) == gmlp.ERR_FLAGS
+    a.scale, a.B = 2e38, 0
+    assert gmlp.lib().gmlp_kv4_attention(ctypes.byref(a)) == gmlp.OK

@@ -74,7 +74,8 @@ typedef enum gmlp_status {
     GMLP_ERR_UNSUPPORTED = -9,/* the forced variant cannot run this shape (SKINNY: M <= 128, or <= 256 on layers whose
                                  two GEMMs both have its cluster form) */
     GMLP_ERR_STATIC_LIMIT = -10,/* gmlp_forward_static: the shape needs more than its fixed built-in scratch */
-    GMLP_ERR_INDEX = -11      /* with GMLP_FLAG_CHECKED: a cache slot, page or length on the device was out of range */
+    GMLP_ERR_INDEX = -11      /* with GMLP_FLAG_CHECKED: a cache slot, page or length on the device was out of range, in this call or
+                                 in one before it that was not checked */
 } gmlp_status;
 
 enum {
@@ -325,10 +326,9 @@ int gmlp_w4_dequantize(const gmlp_w4_layout_args* args);
 
 /*
  * Y = X W for a 4-bit W: X [M, K], Y [M, N] row-major bf16, M at most GMLP_W4_MAX_M.  Codes are used exactly, group sums and their
- * scaling are fp32, Y is rounded once.  From
- * some twenty tokens on the products, not the weights' bytes, set the time, and the bf16 operators on dequantised weights are faster
- * where there is memory for those; more than GMLP_W4_MAX_M tokens are refused (GMLP_ERR_SHAPE).  Everything is read in stream order
- * (the weights too).
+ * scaling are fp32, Y is rounded once.  From some twenty tokens on the products, not the weights' bytes, set the time, and the bf16
+ * operators on dequantised weights are faster where there is memory for those; more than GMLP_W4_MAX_M tokens are refused
+ * (GMLP_ERR_SHAPE).  Everything is read in stream order (the weights too).
  */
 #define GMLP_W4_MAX_M 64
 typedef struct gmlp_w4_matmul_args {
@@ -380,7 +380,7 @@ uint64_t gmlp_w4_workspace_bytes(int64_t M, int64_t d_model, int64_t d_ff, uint3
  * or 128, at most head_dim), quantised as gmlp_w4_quantize does with zero points:
  *     codes   [n_pages][n_kv_heads][page_size][head_dim / 2] bytes: 32 units of head_dim / 32 nibbles, channel c in nibble c / 32
  *             (the lowest bits are nibble 0) of unit c % 32,
- *     params  [n_pages][n_kv_heads][page_size][head_dim / group][2] bf16: scale, zero point,
+ *     params  [n_pages][n_kv_heads][page_size][head_dim / group][2] bf16: scale, zero point (0 to 15),
  * one such pair for K and one for V.  n_pages * page_size must fit 31 bits; byte offsets may pass 32.
  */
 typedef struct gmlp_kv4_cache {
@@ -421,9 +421,9 @@ int gmlp_kv4_gather(const gmlp_kv4_rows_args* args);
  * Q, O [B * q_len, n_q_heads * head_dim] bf16, position by position; request b's key j is in slot
  * block_table[b][j / page_size] * page_size + j % page_size.  lengths[b] counts the keys, the new positions' included (append them
  * first).  A position that sees no key (L = 0, or L < q_len) gets zeros.  What the pages hold past a request's end, and table entries
- * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value enters the second
- * product with 16 bits of significand (two bf16 terms); O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table are reported as above;
- * their keys are left out.
+ * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value enters the second product with 16
+ * bits of significand (two bf16 terms); O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table
+ * are reported as above; their keys are left out.
  * workspace: gmlp_kv4_workspace_bytes(); may be NULL where that is 0; no state is kept in it between calls.
  */
 #define GMLP_KV4_MAX_QUERIES 16

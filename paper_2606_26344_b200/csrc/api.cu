@@ -1322,6 +1322,8 @@ int read_device_status() {
     }
     return v;
 }
+// the error that a non-zero result of read_device_status stands for, whichever call left the word behind
+int status_error(int s) { return s < 0 ? s : ((s >> 16) == gmlp::kIndexStatus ? GMLP_ERR_INDEX : GMLP_ERR_TIMEOUT); }
 
 int forward_impl(const gmlp_args* a) {
     if (a == nullptr) return GMLP_ERR_NULL;
@@ -1445,8 +1447,7 @@ int forward_impl(const gmlp_args* a) {
         if (cudaStreamSynchronize(st) != cudaSuccess) { forget_counters(dev); return GMLP_ERR_LAUNCH; }
         const int s = read_device_status();
         if (s != 0) forget_counters(dev);
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -1591,8 +1592,7 @@ int gate_up_impl(const gmlp_args* a) {
         if (cudaStreamSynchronize(st) != cudaSuccess) { forget_counters(dev); return GMLP_ERR_LAUNCH; }
         const int s = read_device_status();
         if (s != 0) forget_counters(dev);
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -1681,8 +1681,7 @@ int rmsnorm_matmul_impl(const gmlp_rmsmm_args* a) {
     if (a->flags & GMLP_FLAG_CHECKED) {
         if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
         const int s = read_device_status();
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -1792,8 +1791,7 @@ int matmul_add_rmsnorm_impl(const gmlp_mmaddnorm_args* a) {
     if (a->flags & GMLP_FLAG_CHECKED) {
         if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
         const int s = read_device_status();
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -1889,8 +1887,7 @@ int qkv_proj_impl(const gmlp_qkv_args* a) {
     if (a->flags & GMLP_FLAG_CHECKED) {
         if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
         const int s = read_device_status();
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -1946,8 +1943,7 @@ int gqa_attention_impl(const gmlp_gqa_args* a) {
     if (a->flags & GMLP_FLAG_CHECKED) {
         if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
         const int s = read_device_status();
-        if (s < 0) return s;
-        if (s != 0) return GMLP_ERR_TIMEOUT;
+        if (s != 0) return status_error(s);
     }
     return GMLP_OK;
 }
@@ -2014,8 +2010,7 @@ int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* b
     }
     if (rc == GMLP_OK) {
         const int s = read_device_status();
-        if (s < 0) rc = s;
-        else if (s != 0) rc = GMLP_ERR_TIMEOUT;
+        if (s != 0) rc = status_error(s);
     }
     int best = -1;
     for (int c = 0; c < 5; ++c)
@@ -2090,8 +2085,7 @@ int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* b
         }
         if (rc == GMLP_OK) {
             const int s2 = read_device_status();
-            if (s2 < 0) rc = s2;
-            else if (s2 != 0) rc = GMLP_ERR_TIMEOUT;
+            if (s2 != 0) rc = status_error(s2);
         }
         if (rc != GMLP_OK) { (void)0; }
     }
@@ -2134,8 +2128,7 @@ int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* b
         t_force_skinny_fused = t_force_skinny_ring = 0;
         if (rc == GMLP_OK) {
             const int s3 = read_device_status();
-            if (s3 < 0) rc = s3;
-            else if (s3 != 0) rc = GMLP_ERR_TIMEOUT;
+            if (s3 != 0) rc = status_error(s3);
         }
         if (rc == GMLP_OK && n_forms > 1 && form_fits[0]) {
             int bf = 0;

@@ -45,7 +45,7 @@ int kv4_rows_impl(const gmlp_kv4_rows_args* a, bool append) {
     rc = append ? GMLP_KV4_DISPATCH(c, GMLP_KV4_APPEND) : GMLP_KV4_DISPATCH(c, GMLP_KV4_GATHER);
     if (rc != GMLP_OK) return rc;
     prof_mark(append ? "kv4_append" : "kv4_gather", st);
-    return finish_checked(a->flags, st);
+    return finish_checked(dev, a->flags, st);
 }
 
 struct Kv4Plan {
@@ -139,5 +139,5 @@ int kv4_attention_impl(const gmlp_kv4_attention_args* a) {
         if (rc != GMLP_OK) return rc;
         prof_mark("kv4_join", st);
     }
-    return finish_checked(a->flags, st);
+    return finish_checked(dev, a->flags, st);
 }

@@ -169,13 +169,13 @@ int launch_w4_gemm(DeviceState* dev, const gmlp_w4_matrix& w0, const gmlp_w4_mat
     return launch_chained(umma, grid, (unsigned)p.threads, p.smem, p.cluster, st, a, tmX);
 }
 
-int finish_checked(uint32_t flags, cudaStream_t st) {
+int finish_checked(DeviceState* dev, uint32_t flags, cudaStream_t st) {
     if (!(flags & GMLP_FLAG_CHECKED)) return GMLP_OK;
     if (cudaStreamSynchronize(st) != cudaSuccess) return GMLP_ERR_LAUNCH;
     const int s = read_device_status();
-    if (s < 0) return s;
-    if ((s >> 16) == gmlp::kIndexStatus) return GMLP_ERR_INDEX;
-    return s != 0 ? GMLP_ERR_TIMEOUT : GMLP_OK;
+    if (s == 0) return GMLP_OK;
+    forget_counters(dev);                            // the word may be an earlier gmlp_forward's, cut short by a time-out
+    return status_error(s);
 }
 
 int w4_matmul_impl(const gmlp_w4_matmul_args* a) {
@@ -194,7 +194,7 @@ int w4_matmul_impl(const gmlp_w4_matmul_args* a) {
     rc = launch_w4_gemm(dev, a->W, nullptr, static_cast<const bf16*>(a->X), 1, static_cast<bf16*>(a->Y), a->M, kSilu, false, st);
     if (rc != GMLP_OK) return rc;
     prof_mark("w4_matmul", st);
-    return finish_checked(a->flags, st);
+    return finish_checked(dev, a->flags, st);
 }
 
 uint64_t w4_forward_workspace(int64_t M, int64_t d_model, int64_t d_ff, uint32_t flags) {
@@ -246,7 +246,7 @@ int w4_forward_impl(const gmlp_w4_args* a) {
     rc = launch_w4_gemm(dev, a->Wd, nullptr, H, 2, static_cast<bf16*>(a->Y), a->M, kSilu, true, st);
     if (rc != GMLP_OK) return rc;
     prof_mark("w4_down", st);
-    return finish_checked(a->flags, st);
+    return finish_checked(dev, a->flags, st);
 }
 
 // kind: gmlp::kW4From* to pack, -1 to unpack
@@ -276,5 +276,5 @@ int w4_layout_impl(const gmlp_w4_layout_args* a, int kind) {
     else
         rc = launch_chained(gmlp::w4_pack_kernel<gmlp::kW4FromBf16Zeros>, grid, 128, 0, 1, st, a->W, out_in, s_in, z_in, codes, scales, zeros, K, N, G);
     if (rc != GMLP_OK) return rc;
-    return finish_checked(a->flags, st);
+    return finish_checked(dev, a->flags, st);
 }

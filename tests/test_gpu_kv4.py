@@ -303,3 +303,18 @@ def test_binding_refusals():
     gmlp.kv4_append(K[:0], K[:0], c, torch.zeros(0, dtype=torch.int64, device=DEV))
     torch.cuda.synchronize()
     assert gmlp.device_status() == 0
+
+
+def test_an_unchecked_call_s_bad_slot_is_an_index_error_for_the_next_checked_call_of_any_operator():
+    c = gmlp.kv4_cache(2, 2, 128, 16, 64)
+    K = bf16(gen(1), 3, 256)
+    slots = torch.tensor([5, 32, 7], device=DEV)
+    X, W = bf16(gen(2), 4, 256), bf16(gen(3), 256, 256)
+    W4 = gmlp.w4_quantize(W, 64, checked=True)
+    for call in (lambda: gmlp.forward(X, W, W, W, checked=True), lambda: gmlp.w4_matmul(X, W4, checked=True)):
+        want = call()
+        gmlp.kv4_append(K, K, c, slots)
+        with pytest.raises(gmlp.GmlpError) as e:
+            call()
+        assert e.value.status == gmlp.ERR_INDEX and gmlp.device_status() == 0
+        assert torch.equal(call(), want)

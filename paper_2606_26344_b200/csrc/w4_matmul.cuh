@@ -736,14 +736,14 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
     ptx::launch_dependents();
     const uint32_t tmem = *tmem_slot;
 
-    // A wait that runs out leaves its mark in abort_flag and the device status; every loop below then runs on without waiting, so that
-    // all warps meet again at its end.
+    // A wait that runs out leaves its mark in abort_flag and the device status; nothing more is asked for, every loop below runs on without
+    // waiting, so that all warps meet again at its end, and what is in flight gets a millisecond to land.
     float y[COLS];
     const int quarter = warp & 3, my_row = quarter * 32 + lane, my_col = (warp >= kW4Unpackers + 4 ? 1 : 0) * COLS;
     if (producer) {
         if (lane == 0)
             for (int s = DEPTH, slot = 0, phase = 0; s < steps; ++s) {
-                (void)wait_bounded(empty0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 1);
+                if (!wait_bounded(empty0 + 8 * slot, (uint32_t)phase, abort_flag, KERNEL_ID, 1)) break;
                 ask_codes(s, slot);
                 ask_x(s, slot);
                 if (++slot == DEPTH) {
@@ -888,6 +888,9 @@ w4_umma_kernel(const W4GemmArgs p, const __grid_constant__ CUtensorMap tmX)
             }
             if (++slot == DEPTH) slot = 0;
         }
+    }
+    if (*abort_flag) {
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
     ptx::tc_fence_before_sync();
     __syncthreads();

@@ -632,7 +632,8 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_tile_kernel(const W4GemmArgs
 //                 registers: no weight is rounded here either.
 // (With all warps doing everything in step, one barrier per k-block, a k-block took 1750 cycles.)
 // Bound by the hand-over from one kind of warps to the next, some 1000 cycles a k-block: 4096 x 14336 at M = 64 25 us (48 with tiles), 8B
-// layer at M = 33 94 us (158 with tiles).
+// layer at M = 33 without a norm 94 us (158 with tiles).  Two CTAs per SM for 32 rows, with two buffers each and 40 registers, lost: 8B layer
+// with the norm at M = 16 89 against 76 us.
 constexpr int kW4Producers = 4, kW4Unpackers = 8, kW4Readers = 8;
 constexpr int kW4UmmaThreads = 32 * (kW4Unpackers + kW4Readers + 1 + kW4Producers);
 constexpr int kW4UmmaDepth = 4, kW4ABuffers = 3;

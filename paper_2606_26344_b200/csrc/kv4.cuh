@@ -170,8 +170,7 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 //   P'  = exp2(S - m) * s_v as two bf16 terms (hi + lo: rounded to one, the output was 1.4 times as far off as its own rounding
 //                 leaves it), transposed in registers (movmatrix);
 //   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same two
-//                 terms and taken off at the end and every 64 tiles: the accumulator sees that part of at most 1024 tokens, and its
-//                 rounding costs some 2^-13 of a quantiser's step, however long the request.
+//                 terms and taken off at the end and every few tiles (kv4_tiles_between).
 // Bound by the issue slots and the half-rate integer pipe of the unpacking, then by HBM: 64 requests of 1..8192 keys, 32 / 8 heads of
 // 128, groups of 64: 129 us (2.8 TB/s, 0.43 of the measured copy rate); one request of 131071 keys, 64 / 8 heads, groups of 128: 55 us
 // (2.6 TB/s).  With one term for P' 115 and 51 us; so, but with loads into registers instead of the rings 146 and 67; with the maximum
@@ -183,6 +182,13 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 constexpr int kKv4Warps = 4;
 constexpr int kKv4Threads = 32 * kKv4Warps;
 constexpr int kKv4Tile = 16;
+// Tiles of a warp between two returns of the offset (a power of two).  A product's additions may round toward zero, and while the
+// accumulators hold the offset too, all of them, in all warps, lose to the same side; the output that is left shrinks with the root
+// of the length.  Error of the output over that of its own rounding alone, and time, with 64, 8, 4 and 1 tiles in between:
+//   64 requests of 1..8192 keys      1.0020, 1.0003, 1.0001, 1.0000      130.2, 131.4, 132.5, 138.6 us
+//   131071 keys, 64 / 8 heads         1.175,  1.016,  1.007,  1.001       54.6,  55.0,  56.0,  57.6 us
+//   1200000 keys, 4 / 1 heads of 64     4.4,   1.12,   1.06,   1.01       54.6,  55.6,  56.1,  57.8 us
+__device__ __forceinline__ int kv4_tiles_between(int len) { return len <= 16384 ? 8 : (len <= 262144 ? 4 : 1); }
 
 struct Kv4AttnArgs {
     const bf16* Q;             // [B * T][Hq * D]
@@ -393,9 +399,10 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
     const int gray = g ^ (g >> 1);                   // the token of row g
     const int swap = D == 128 ? ((gray >> 1) & 1) << 1 : 0;
     const uint8_t* slot = ring;
+    const int between = kv4_tiles_between(len) - 1;
     int tiles = 0;
     for (int token = first + warp * kKv4Tile; token < last; token += stride) {
-        if ((tiles++ & 63) == 63) take_off();
+        if ((tiles++ & between) == between) take_off();
         cp_async_wait_but<kKv4Depth - 2>();          // this tile has landed,
         __syncwarp();                                // for every lane, and the slot of the tile before is free
         ask(kKv4Depth - 1);

@@ -7,6 +7,8 @@
 // and one and-or per pair, the A operands of the score product, a lane that reads 4 units of a value those of the output product,
 // and each nibble position holds channels of one block of 32, so that every mma stays inside one group of G >= 32 channels.
 #pragma once
+#include <cfloat>
+
 #include "common.cuh"
 #include "ptx.cuh"
 #include "w4_matmul.cuh"
@@ -343,8 +345,11 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             ++entry;
         }
     };
-    // The warp's tiles from the first to the last; false where a sum is no number.  CAREFUL: a masked token's zero point is kept out of
-    // the sums whatever it is (ordinary ones cost nothing there: their probability is 0).
+    // The warp's tiles from the first to the last; false where a sum is no number or came near the end of float's range (2^100: the warps
+    // and splits are still to be added).  CAREFUL, the second try: a masked token's zero point is kept out of the sums whatever it is
+    // (ordinary ones cost nothing there: their probability is 0), and the base of the exponentials counts in what a value's scale has
+    // above 2^60, so that no sum of P' (16 + q) passes 2^96; the base is common to the sum of the probabilities, and the quotient
+    // stays what it is.
     auto pass = [&](auto with_care) -> bool {
         constexpr bool CAREFUL = decltype(with_care)::value;
 #pragma unroll
@@ -489,18 +494,28 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             }
             // The base of the exponentials follows the maximum of a column only once a score is more than 8 (in powers of two) above it:
             // sums of up to 2^8 are as good as sums of up to 1, and most tiles need no reduction over the lanes.
-            bool above = false;
+            bool above = CAREFUL;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) above = above || fmaxf(s[n][e], s[n][2 + e]) > m[n][e] + 8.0f;
             if (__any_sync(0xFFFFFFFFu, above)) {
+                float lift[2] = {0.0f, 0.0f};        // of the lane's two tokens
+                if constexpr (CAREFUL) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float step = 0.0f;
+#pragma unroll
+                        for (int gi = 0; gi < NG; ++gi) step = fmaxf(step, fabsf(bf16_lo(cur.vp[h][gi])));
+                        lift[h] = fmaxf(log2f(fminf(step, FLT_MAX)) - 60.0f, 0.0f);
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     float alpha[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(s[n][e], s[n][2 + e]);
+                        float top = CAREFUL ? fmaxf(s[n][e] + lift[0], s[n][2 + e] + lift[1]) : fmaxf(s[n][e], s[n][2 + e]);
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
@@ -596,7 +611,7 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) size += fabsf(o[i][n][e]);
-        return __all_sync(0xFFFFFFFFu, size - size == 0.0f);                     // the lanes are done with the ring, too
+        return __all_sync(0xFFFFFFFFu, size < 1.2676506e30f);                    // the lanes are done with the ring, too
     };
     if (!pass(std::false_type{})) (void)pass(std::true_type{});
     __syncthreads();                                 // the rings are done with: the results take their place

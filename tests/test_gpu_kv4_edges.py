@@ -24,3 +24,58 @@ def test_zero_points_that_are_no_numbers_stay_behind_the_mask(D, G, bad):
     want, A, E = F.attention(Q.double(), k, v, [n], Hq, T, D ** -0.5)
     bound = F.attention_bound(want, A, E, 68, 62 * float(v[0].abs().max()) / 7)
     assert bool(((O.double() - want).abs()[:2] <= bound[:2]).all()) and bool(torch.isnan(O[2]).all())
+
+
+def check(Q, K_rows, V_rows, Hq, T=1, page=64, G=64, D=128):
+    """Attention of one request with these keys and values against the 64-bit result on what the cache holds of them."""
+    n, Hkv = K_rows.shape[0], K_rows.shape[1] // D
+    n_pages = -(-n // page)
+    c = gmlp.kv4_cache(n_pages, Hkv, D, page, G)
+    slots = torch.arange(n, device=DEV)
+    gmlp.kv4_append(K_rows, V_rows, c, slots, checked=True)
+    k, v = (K.rows_of(codes, params, slots, page, D, G) for codes, params in ((c.k_codes, c.k_params), (c.v_codes, c.v_params)))
+    table = torch.arange(n_pages, dtype=torch.int32, device=DEV)[None]
+    O = gmlp.kv4_attention(Q, c, table, torch.tensor([n], dtype=torch.int32, device=DEV), Hq, q_len=T, checked=True)
+    want, _, E = F.attention(Q.double(), [k], [v], [n], Hq, T, D ** -0.5)
+    largest = v.abs().unflatten(-1, (-1, G)).amax(-1).repeat_interleave(G, -1)       # of its group, whose step is at most 1 / 7 of it
+    return O, want, F.attention(Q.double(), [k], [largest], [n], Hq, T, D ** -0.5)[0], E
+
+
+# The bound, relative to A = sum(p * largest value of the group): P' has 16 bits, 2^-17 of each term.  An accumulator holds 16 + q, at most
+# 31 / 7 of the largest, of up to 8 tiles with two products each, every one of which may drop 2^-23 of it: 2^-16.8 in all.  exp2 is
+# good to 2^-21, the sums of warps and splits to less; 2^-15 covers them.  Scores are off by E.
+def check_close(O, want, A, E):
+    assert bool(torch.isfinite(O.float()).all())
+    assert bool(((O.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -15 + 2 * E) * A).all())
+
+
+@pytest.mark.parametrize("n,T", [(900, 1), (70, 4)])
+@pytest.mark.parametrize("exponent", [40, 59, 61, 80, 110, 122])
+def test_values_of_any_size(exponent, n, T):
+    # exact powers of two move every value and every result alike
+    g = K.gen(exponent)
+    Q, k, v = K.bf16(g, T, 8 * 128), K.bf16(g, n, 256), K.bf16(g, n, 256)
+    small = check(Q, k, v, 8, T)
+    large = check(Q, k, (v.float() * 2.0 ** exponent).to(torch.bfloat16), 8, T)
+    check_close(*small)
+    check_close(*large)
+    assert torch.equal(large[1], small[1] * 2.0 ** exponent)
+
+
+@pytest.mark.parametrize("at", [0, 333, 899])
+@pytest.mark.parametrize("size", [2.0 ** 70, 2.0 ** 100, 2.0 ** 127])
+def test_one_large_value_among_ordinary_ones(at, size):
+    g = K.gen(at)
+    Q, k, v = K.bf16(g, 1, 8 * 128), K.bf16(g, 900, 256), K.bf16(g, 900, 256)
+    v[at, 5], v[at, 200] = size, -size
+    check_close(*check(Q, k, v, 8))
+
+
+def test_a_large_value_that_the_softmax_leaves_out():
+    # its probability is 0: what the others say comes through
+    g = K.gen(3)
+    Q, k, v = torch.ones(1, 128, dtype=torch.bfloat16, device=DEV), K.bf16(g, 500, 128), K.bf16(g, 500, 128)
+    k[7], v[7] = -1000.0, 1e38
+    O, want, A, E = check(Q, k, v, 1)
+    assert float(want.abs().max()) < 1.0
+    check_close(O, want, A, E)

@@ -168,7 +168,7 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 // own.  A CTA takes one request, one key/value head, up to 8 NT of its T * (query heads per key/value head) query rows and a range
 // of the keys; its four warps take 16-token tiles in turn.  Per tile and warp (running maximum and sum in fp32):
 //   S^T = K Q^T   tokens are the 16 mma rows, query rows the 8 columns, 16 + q exact in bf16; (16 + z) times the query row's sum
-//                 over the group comes off, and the token's scale (times the softmax scale) is a factor, both in fp32;
+//                 over the group comes off, the token's scale is a factor, and the softmax scale one of the sum, all in fp32;
 //   P'  = exp2(S - m) * s_v as two bf16 terms (hi + lo: rounded to one, the output was 1.4 times as far off as its own rounding
 //                 leaves it), transposed in registers (movmatrix);
 //   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same two
@@ -200,7 +200,8 @@ struct Kv4AttnArgs {
     const int32_t* lengths;    // [B]
     float* part;               // [B * Hkv * col_tiles][splits][8 NT][D + 2]: O, then maximum and sum; unused for one split
     int B, T, Hq, ratio, width, splits, col_tiles;
-    float scale_log2;
+    uint32_t q_scale;          // bf16, twice: a power of two that the queries are taken times, and what the scores are then multiplied with
+    float s_scale;
 };
 
 // Keys per split of a request with `len` keys: the same formula in both kernels.
@@ -287,6 +288,8 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                 q[n][j][2] = __byte_perm(x.z, x.w, 0x5410);
                 q[n][j][3] = __byte_perm(x.z, x.w, 0x7632);
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[n][j][u] = bf16x2_fma(q[n][j][u], p.q_scale, 0x80008000u);       // - 0: a product, exact
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                         mma_bf16_16816(acc[n], a[4], a[5], a[6], a[7], q[n][j][2], q[n][j][3]);
                     }
                 }
-                const float s0 = bf16_lo(cur.kp[0][gi]) * p.scale_log2, s1 = bf16_lo(cur.kp[1][gi]) * p.scale_log2;
+                const float s0 = bf16_lo(cur.kp[0][gi]), s1 = bf16_lo(cur.kp[1][gi]);
                 const float z0 = bf16_hi(cur.kp[0][gi]) + 16.0f, z1 = bf16_hi(cur.kp[1][gi]) + 16.0f;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -475,6 +478,10 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
                     s[n][3] = fmaf(fmaf(-z1, qsum[n][gi][1], acc[n][3]), s1, s[n][3]);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= p.s_scale;
             // Masks, where a tile needs them: a masked score is -inf whatever its token holds.
             const bool full = page_ok && token + kKv4Tile <= full_limit;         // of the whole warp
             const int t0 = page_ok ? token + gray : INT_MAX - 16;

@@ -119,7 +119,10 @@ int kv4_attention_impl(const gmlp_kv4_attention_args* a) {
     k.width = (int)a->table_width;
     k.splits = plan.splits;
     k.col_tiles = plan.col_tiles;
-    k.scale_log2 = scale_log2;
+    // 31 steps of a query, summed over 128 channels, are 2^12 of it: times 2^-14 they have a float wherever the query has one
+    const bool scaled = std::fabs(scale_log2) < 0x1p113f;
+    k.q_scale = scaled ? 0x38803880u : 0x3F803F80u;
+    k.s_scale = scaled ? scale_log2 * 0x1p14f : scale_log2;
     const dim3 grid((unsigned)plan.splits, (unsigned)(k.c.n_kv_heads * plan.col_tiles), (unsigned)a->B);
     if (grid.y > 65535u) return GMLP_ERR_SHAPE;
     prof_begin(st);

@@ -60,12 +60,13 @@ __device__ __forceinline__ void mma_bf16_16816_first(float (&c)[4], uint32_t a0,
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
-// a + b in both halves.
-__device__ __forceinline__ uint32_t bf16x2_add(uint32_t a, uint32_t b) {
+// a * b + c in both halves.
+__device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0x3F803F80u), "r"(b));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
+__device__ __forceinline__ uint32_t bf16x2_add(uint32_t a, uint32_t b) { return bf16x2_fma(a, 0x3F803F80u, b); }
 // (w & mask) | bits in one instruction (left to itself the compiler splits the and-or of two constants in two, on the
 // half-rate integer pipe: 8192 x 28672 at M = 1 took 38.4 us so, 32.7 us as one).
 __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {

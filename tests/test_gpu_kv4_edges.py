@@ -79,3 +79,29 @@ def test_a_large_value_that_the_softmax_leaves_out():
     O, want, A, E = check(Q, k, v, 1)
     assert float(want.abs().max()) < 1.0
     check_close(O, want, A, E)
+
+
+@pytest.mark.parametrize("D,G", K.SHAPES)
+@pytest.mark.parametrize("T", [1, 5])
+@pytest.mark.parametrize("exponent", [60, 66, 100, 120])
+def test_queries_of_any_size(exponent, T, D, G):
+    # keys as much smaller: powers of two leave every score as it is, up to where a query times 31 steps of a key has no float
+    g, n = K.gen(exponent), 300
+    Q, k, v = K.bf16(g, T, 8 * D), K.bf16(g, n, 2 * D), K.bf16(g, n, 2 * D)
+    plain = check(Q, k, v, 8, T, G=G, D=D)
+    large = check((Q.float() * 2.0 ** exponent).to(torch.bfloat16), (k.float() * 2.0 ** -exponent).to(torch.bfloat16), v, 8, T, G=G, D=D)
+    check_close(*plain)
+    check_close(*large)
+    assert torch.equal(large[1], plain[1])
+
+
+def test_queries_near_the_largest_bf16_choose_one_key():
+    # scores of 1e38: the softmax is 1 at one key, another for each head, and 0 elsewhere; ordinary heads beside them stay ordinary
+    g, n = K.gen(9), 300
+    Q, k, v = K.bf16(g, 1, 8 * 128), K.bf16(g, n, 256), K.bf16(g, n, 256)
+    Q[:, :4 * 128] *= 2.0 ** 124
+    O, want, A, E = check(Q, k, v, 8)
+    chosen = want[:, :512].view(4, 128)
+    assert len({tuple(r.tolist()) for r in chosen}) > 1
+    assert bool(((O.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15 * A)[:, :512].all())
+    check_close(O[:, 512:], want[:, 512:], A[:, 512:], E[:, 512:])

@@ -445,7 +445,7 @@ typedef struct gmlp_kv4_attention_args {
     uint64_t workspace_bytes;
 } gmlp_kv4_attention_args;
 int gmlp_kv4_attention(const gmlp_kv4_attention_args* args);
-/* On a device with `sm_count` SMs (0: the current device, 148 if there is none); 0 bytes too for invalid sizes. */
+/* On a device with `sm_count` SMs (0: the current device, 148 if there is none); at most 256 MB; 0 bytes too for invalid sizes. */
 uint64_t gmlp_kv4_workspace_bytes(int64_t B, int32_t q_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                   int64_t table_width, int32_t page_size, int32_t sm_count);
 

@@ -53,7 +53,9 @@ struct Kv4Plan {
     uint64_t workspace;
 };
 // How the keys of a request are split over CTAs.  The host knows the width of the page table, not the lengths: the kernel
-// divides each request's own length by `splits`.
+// divides each request's own length by `splits`.  They are enough to fill the GPU and, for requests much longer than the others, one per
+// 2048 keys that the table has room for, as far as the partial results of all of them fit kKv4PartialBytes.
+constexpr uint64_t kKv4PartialBytes = (uint64_t)256 << 20;
 Kv4Plan kv4_plan(int64_t B, int T, int ratio, int n_kv_heads, int head_dim, int64_t most_keys, int sms) {
     Kv4Plan p{};
     const int64_t cols = (int64_t)T * ratio;
@@ -62,13 +64,15 @@ Kv4Plan kv4_plan(int64_t B, int T, int ratio, int n_kv_heads, int head_dim, int6
     const int64_t ctas = B * n_kv_heads * p.col_tiles;
     const int64_t target = (int64_t)sms * 4, long_keys = 2048;
     int64_t splits = (target + ctas - 1) / ctas;
-    const int64_t by_length = (most_keys + long_keys - 1) / long_keys, most = (most_keys + 127) / 128;
-    if (splits < by_length && ctas * by_length <= 1 << 20) splits = by_length;
+    int64_t by_length = (most_keys + long_keys - 1) / long_keys;
+    const int64_t most = (most_keys + 127) / 128, split_bytes = ctas * 8 * p.nt * (head_dim + 4) * 4;
+    if (by_length > (int64_t)kKv4PartialBytes / split_bytes) by_length = (int64_t)kKv4PartialBytes / split_bytes;
+    if (splits < by_length) splits = by_length;
     if (splits > most) splits = most;
     if (splits > gmlp::kKv4MaxSplits) splits = gmlp::kKv4MaxSplits;
     if (splits < 1) splits = 1;
     p.splits = (int)splits;
-    p.workspace = splits > 1 ? (uint64_t)ctas * splits * 8 * p.nt * (head_dim + 4) * 4 : 0;
+    p.workspace = splits > 1 ? (uint64_t)(split_bytes * splits) : 0;
     return p;
 }
 

@@ -105,3 +105,21 @@ def test_queries_near_the_largest_bf16_choose_one_key():
     assert len({tuple(r.tolist()) for r in chosen}) > 1
     assert bool(((O.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15 * A)[:, :512].all())
     check_close(O[:, 512:], want[:, 512:], A[:, 512:], E[:, 512:])
+
+
+@pytest.mark.parametrize("B,width", [(520, 4096), (3000, 1024)])
+def test_many_requests_over_a_table_for_very_long_ones(B, width):
+    # fewer splits than one per 2048 keys, and a workspace that stays small: short requests, two long ones, pages shared among all
+    Hq = Hkv = 4
+    D, G, page, n = 64, 32, 64, 9000
+    c, table, _, k, v = K.filled([n], Hkv, D, page, G, 6)
+    wide = torch.full((B, width), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    lengths = [(11 * i) % 90 for i in range(B)]
+    lengths[1], lengths[B - 1] = n, n - 77
+    assert gmlp.kv4_workspace_bytes(B, 1, Hq, Hkv, D, width, page) <= 256 << 20
+    Q = K.bf16(K.gen(7), B, Hq * D)
+    O = gmlp.kv4_attention(Q, c, wide, torch.tensor(lengths, dtype=torch.int32, device=DEV), Hq, checked=True)
+    want, A, E = F.attention(Q.double(), [k[0][:m] for m in lengths], [v[0][:m] for m in lengths], lengths, Hq, 1, D ** -0.5)
+    bound = F.attention_bound(want, A, E, 128, 62 * float(v[0].abs().max()) / 7)
+    assert bool(((O.double() - want).abs() <= bound).all())

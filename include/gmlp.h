@@ -298,7 +298,8 @@ int gmlp_gqa_attention(const gmlp_gqa_args* args);
  *     gmlp_w4_pack      from codes (one byte each, low four bits), scales and zero points that some other tool made.
  * Their order is the library's own (tiles of 16 columns by 128 rows, K padded to 256); gmlp_w4_dequantize writes the bf16 matrix back, e.g. for a
  * prompt's gmlp_forward (rounded once; pass GMLP_FLAG_WEIGHTS_IN_STREAM_ORDER to a gmlp_forward that follows on the stream).
- * K must be a multiple of `group`; N is any positive number; both at most 2^20.
+ * K must be a multiple of `group`; N is any positive number; both at most 2^20.  The buffers of a gmlp_w4_matrix are 16-byte aligned;
+ * the plain matrix, scales and zero points of these three calls need the alignment of their elements only.
  */
 typedef struct gmlp_w4_matrix {
     const void* codes;        /* device, gmlp_w4_code_bytes(K, N) bytes */

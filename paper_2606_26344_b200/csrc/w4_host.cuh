@@ -257,6 +257,10 @@ int w4_layout_impl(const gmlp_w4_layout_args* a, int kind) {
     int rc = check_w4_matrix(a->m);
     if (rc != GMLP_OK) return rc;
     if (!a->W || (kind == gmlp::kW4FromCodes && (!a->scales || (a->zeros == nullptr) != (a->m.zeros == nullptr)))) return GMLP_ERR_NULL;
+    // read and written element by element, bf16 but for the codes that pack reads
+    if ((kind != gmlp::kW4FromCodes && (reinterpret_cast<uintptr_t>(a->W) & 1u)) ||
+        (kind == gmlp::kW4FromCodes && (reinterpret_cast<uintptr_t>(a->scales) & 1u)))
+        return GMLP_ERR_ALIGN;
     DeviceState* dev = current_device(&rc);
     if (dev == nullptr) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(a->stream);

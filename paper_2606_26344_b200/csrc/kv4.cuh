@@ -198,7 +198,7 @@ struct Kv4AttnArgs {
     Kv4Cache c;
     const int32_t* table;      // [B][width]
     const int32_t* lengths;    // [B]
-    float* part;               // [B * Hkv * col_tiles][splits][8 NT][D + 2]: O, then maximum and sum; unused for one split
+    float* part;               // [B * Hkv * col_tiles][splits][8 NT][D + 4]: O, maximum, sum, two unused; nothing for one split
     int B, T, Hq, ratio, width, splits, col_tiles;
     uint32_t q_scale;          // bf16, twice: a power of two that the queries are taken times, and what the scores are then multiplied with
     float s_scale;
@@ -247,26 +247,26 @@ __device__ __forceinline__ void lds_words(uint32_t (&d)[N], const uint8_t* p) {
     }
 }
 
-template <int D, int G, int NT>
-__global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_kernel(const Kv4AttnArgs p)
+// What a warp has of its query rows: the sums of P' V, one row per lane and block of channels, the base and the sum of P.
+template <int D, int NT>
+struct Kv4Sums {
+    float o[D / 16][NT][4], m[NT][2], l[NT][2];
+};
+// The warp's tiles from the first to the last; false where a sum is no number or came near the end of float's range (2^100: the warps
+// and splits are still to be added).  CAREFUL, the second try: a masked token's zero point is kept out of the sums whatever it is
+// (ordinary ones cost nothing there: their probability is 0), and the base of the exponentials counts in what a value's scale has
+// above 2^60, so that no sum of P' (16 + q) passes 2^96; the base is common to the sum of the probabilities, and the quotient
+// stays what it is.
+template <int D, int G, int NT, bool CAREFUL>
+__device__ __forceinline__ bool kv4_warp_sums(const Kv4AttnArgs& p, Kv4Sums<D, NT>& sums)
 {
     constexpr int NJ = D / 32, NG = D / G, PER = G / 32, MT = D / 16;        // blocks of 32, groups, output tiles
-    constexpr int COLS = 8 * NT;
-    constexpr int SLOT = kv4_slot_bytes(D, G);
+    constexpr int COLS = 8 * NT, SLOT = kv4_slot_bytes(D, G);
     extern __shared__ __align__(128) uint8_t kv4_smem[];
-    float (*s_o)[COLS][D + 4] = reinterpret_cast<float (*)[COLS][D + 4]>(kv4_smem);        // [warp][column][channel]
-    __shared__ float s_m[kKv4Warps][COLS], s_l[kKv4Warps][COLS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = blockIdx.x, head = (int)blockIdx.y / p.col_tiles, ct = (int)blockIdx.y % p.col_tiles, b = blockIdx.z;
     const int cols_all = p.T * p.ratio, col0 = ct * COLS;
-
-    ptx::grid_dependency_wait();
-    ptx::launch_dependents();
-    const int len = kv4_length(p, b);
-    const int keys = kv4_split_keys(len, p.splits);
-    const int first = split * keys, last = min(first + keys, len);
-    if (split > 0 && first >= len) return;           // the joining kernel uses the same formula and does not look here
-    if (split == 0 && ct == 0 && head == 0 && threadIdx.x == 0 && (p.lengths[b] < 0 || p.lengths[b] > len)) report_index(3);
+    const int len = kv4_length(p, b), keys = kv4_split_keys(len, p.splits), first = split * keys, last = min(first + keys, len);
 
     // query operands: column n = query row col0 + n of this head, channels 32 j + 8 t + 0..7
     uint32_t q[NT][NJ][4];
@@ -316,7 +316,9 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
         }
     const int full_limit = min(last, len - p.T + 1 + col0 / p.ratio);       // below it every column sees every key
 
-    float o[MT][NT][4], m[NT][2], l[NT][2], zsum[NG][NT][2];
+    auto &o = sums.o;
+    auto &m = sums.m, &l = sums.l;
+    float zsum[NG][NT][2];
     auto take_off = [&]() {                          // o -= the sum of P' (16 + z), which every lane holds a part of
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -348,279 +350,305 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
             ++entry;
         }
     };
-    // The warp's tiles from the first to the last; false where a sum is no number or came near the end of float's range (2^100: the warps
-    // and splits are still to be added).  CAREFUL, the second try: a masked token's zero point is kept out of the sums whatever it is
-    // (ordinary ones cost nothing there: their probability is 0), and the base of the exponentials counts in what a value's scale has
-    // above 2^60, so that no sum of P' (16 + q) passes 2^96; the base is common to the sum of the probabilities, and the quotient
-    // stays what it is.
-    auto pass = [&](auto with_care) -> bool {
-        constexpr bool CAREFUL = decltype(with_care)::value;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m[n][e] = -INFINITY;
-                l[n][e] = 0.0f;
+        for (int e = 0; e < 2; ++e) {
+            m[n][e] = -INFINITY;
+            l[n][e] = 0.0f;
 #pragma unroll
-                for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][n][e] = 0.0f;
+            for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] = 0.0f;
         }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][n][e] = 0.0f;
+    }
 
-        // Asks for the warp's next tile, one commit group per call; a page outside of the cache is not read.  Tokens past the end of a
-        // request may hold anything.  Bit i of `ok`: the i-th tile from the current one lies in the cache.
-        uint8_t* ring = kv4_smem + warp * (kKv4Depth * SLOT);
-        const int lane_code = D == 128 ? (lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 3) & 1) << 1)) * 16) : lane * 16;
-        const bool lane_param = (lane & 15) < 4 * NG;
-        const int lane_param_to = 16 * D + (lane >> 4) * (64 * NG) + (lane & 15) * 16;
-        const uint8_t* param_base = reinterpret_cast<const uint8_t*>(lane >> 4 ? p.c.params[1] : p.c.params[0]) + (lane & 15) * 16;
-        int ask_token = first + warp * kKv4Tile, entry = ask_token / p.c.page_size, place = ask_token - entry * p.c.page_size;
-        int page = ask_token < last ? (int)ld_4B(table + entry) : -1;
-        uint32_t ok = 0, ask_to = ptx::smem_addr(ring);
-        const uint32_t ring_end = ask_to + kKv4Depth * SLOT;
-        auto ask = [&](int bit) {
-            if (ask_token < last) {
-                if ((uint32_t)page < (uint32_t)p.c.n_pages) {
-                    const int64_t row = ((int64_t)page * p.c.n_kv_heads + head) * p.c.page_size + place;
-                    const uint8_t* k = p.c.codes[0] + row * (D / 2) + lane * 16;
-                    const uint8_t* v = p.c.codes[1] + row * (D / 2) + lane * 16;
-                    const uint32_t to = ask_to + lane_code;
-                    cp_async_16(to, k);
-                    cp_async_16(to + 8 * D, v);
-                    if constexpr (D == 128) {
-                        cp_async_16(to + 512, k + 512);
-                        cp_async_16(to + 8 * D + 512, v + 512);
-                    }
-                    if (lane_param) cp_async_16(ask_to + lane_param_to, param_base + row * (4 * NG));
-                    ok |= 1u << bit;
+    // Asks for the warp's next tile, one commit group per call; a page outside of the cache is not read.  Tokens past the end of a
+    // request may hold anything.  Bit i of `ok`: the i-th tile from the current one lies in the cache.
+    uint8_t* ring = kv4_smem + warp * (kKv4Depth * SLOT);
+    const int lane_code = D == 128 ? (lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 3) & 1) << 1)) * 16) : lane * 16;
+    const bool lane_param = (lane & 15) < 4 * NG;
+    const int lane_param_to = 16 * D + (lane >> 4) * (64 * NG) + (lane & 15) * 16;
+    const uint8_t* param_base = reinterpret_cast<const uint8_t*>(lane >> 4 ? p.c.params[1] : p.c.params[0]) + (lane & 15) * 16;
+    int ask_token = first + warp * kKv4Tile, entry = ask_token / p.c.page_size, place = ask_token - entry * p.c.page_size;
+    int page = ask_token < last ? (int)ld_4B(table + entry) : -1;
+    uint32_t ok = 0, ask_to = ptx::smem_addr(ring);
+    const uint32_t ring_end = ask_to + kKv4Depth * SLOT;
+    auto ask = [&](int bit) {
+        if (ask_token < last) {
+            if ((uint32_t)page < (uint32_t)p.c.n_pages) {
+                const int64_t row = ((int64_t)page * p.c.n_kv_heads + head) * p.c.page_size + place;
+                const uint8_t* k = p.c.codes[0] + row * (D / 2) + lane * 16;
+                const uint8_t* v = p.c.codes[1] + row * (D / 2) + lane * 16;
+                const uint32_t to = ask_to + lane_code;
+                cp_async_16(to, k);
+                cp_async_16(to + 8 * D, v);
+                if constexpr (D == 128) {
+                    cp_async_16(to + 512, k + 512);
+                    cp_async_16(to + 8 * D + 512, v + 512);
                 }
-                ask_token += stride;
-                advance(entry, place);
-                if (ask_token < last) page = (int)ld_4B(table + entry);
+                if (lane_param) cp_async_16(ask_to + lane_param_to, param_base + row * (4 * NG));
+                ok |= 1u << bit;
             }
-            ask_to += SLOT;
-            if (ask_to == ring_end) ask_to -= kKv4Depth * SLOT;
-            cp_async_commit();
-        };
+            ask_token += stride;
+            advance(entry, place);
+            if (ask_token < last) page = (int)ld_4B(table + entry);
+        }
+        ask_to += SLOT;
+        if (ask_to == ring_end) ask_to -= kKv4Depth * SLOT;
+        cp_async_commit();
+    };
 #pragma unroll
-        for (int i = 0; i < kKv4Depth - 1; ++i) ask(i);
+    for (int i = 0; i < kKv4Depth - 1; ++i) ask(i);
 
-        const int gray = g ^ (g >> 1);                   // the token of row g
-        const int swap = D == 128 ? ((gray >> 1) & 1) << 1 : 0;
-        const uint8_t* slot = ring;
-        const int between = kv4_tiles_between(len) - 1;
-        int tiles = 0;
-        for (int token = first + warp * kKv4Tile; token < last; token += stride) {
-            if ((tiles++ & between) == between) take_off();
-            cp_async_wait_but<kKv4Depth - 2>();          // this tile has landed,
-            __syncwarp();                                // for every lane, and the slot of the tile before is free
-            ask(kKv4Depth - 1);
-            const bool page_ok = ok & 1;
-            ok >>= 1;
-            if (!page_ok && lane == 0) report_index(4);
-            struct {
-                uint32_t k[2][D / 32];                   // rows g and g + 8: units 8 t .. 8 t + 7
-                uint32_t v[4][D / 64];                   // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9: units 4 g .. 4 g + 3
-                uint32_t kp[2][NG], vp[2][NG];
-            } cur;
+    const int gray = g ^ (g >> 1);                   // the token of row g
+    const int swap = D == 128 ? ((gray >> 1) & 1) << 1 : 0;
+    const uint8_t* slot = ring;
+    const int between = kv4_tiles_between(len) - 1;
+    int tiles = 0;
+    for (int token = first + warp * kKv4Tile; token < last; token += stride) {
+        if ((tiles++ & between) == between) take_off();
+        cp_async_wait_but<kKv4Depth - 2>();          // this tile has landed,
+        __syncwarp();                                // for every lane, and the slot of the tile before is free
+        ask(kKv4Depth - 1);
+        const bool page_ok = ok & 1;
+        ok >>= 1;
+        if (!page_ok && lane == 0) report_index(4);
+        struct {
+            uint32_t k[2][D / 32];                   // rows g and g + 8: units 8 t .. 8 t + 7
+            uint32_t v[4][D / 64];                   // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9: units 4 g .. 4 g + 3
+            uint32_t kp[2][NG], vp[2][NG];
+        } cur;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = gray + 8 * h;
-                lds_words<D / 32>(cur.k[h], slot + row * (D / 2) + (t ^ swap) * (D / 8));
-                lds_words<NG>(cur.kp[h], slot + 16 * D + row * (4 * NG));
-                lds_words<NG>(cur.vp[h], slot + 16 * D + 64 * NG + row * (4 * NG));
+        for (int h = 0; h < 2; ++h) {
+            const int row = gray + 8 * h;
+            lds_words<D / 32>(cur.k[h], slot + row * (D / 2) + (t ^ swap) * (D / 8));
+            lds_words<NG>(cur.kp[h], slot + 16 * D + row * (4 * NG));
+            lds_words<NG>(cur.vp[h], slot + 16 * D + 64 * NG + row * (4 * NG));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 2 * t + i, tok = (r ^ (r >> 1)) + 8 * h;
-                    const int chunk = D == 128 ? (((g >> 1) ^ (((tok >> 1) & 1) << 1)) * 16 + (g & 1) * 8) : g * 4;
-                    lds_words<D / 64>(cur.v[2 * h + i], slot + 8 * D + tok * (D / 2) + chunk);
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int r = 2 * t + i, tok = (r ^ (r >> 1)) + 8 * h;
+                const int chunk = D == 128 ? (((g >> 1) ^ (((tok >> 1) & 1) << 1)) * 16 + (g & 1) * 8) : g * 4;
+                lds_words<D / 64>(cur.v[2 * h + i], slot + 8 * D + tok * (D / 2) + chunk);
             }
-            slot += SLOT;
-            if (slot == ring + kKv4Depth * SLOT) slot = ring;
+        }
+        slot += SLOT;
+        if (slot == ring + kKv4Depth * SLOT) slot = ring;
 
-            // scores of tokens (rows) g and g + 8, columns 2 t and 2 t + 1
-            float s[NT][4];
+        // scores of tokens (rows) g and g + 8, columns 2 t and 2 t + 1
+        float s[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
 #pragma unroll
-            for (int gi = 0; gi < NG; ++gi) {
-                float acc[NT][4];
+        for (int gi = 0; gi < NG; ++gi) {
+            float acc[NT][4];
 #pragma unroll
-                for (int jj = 0; jj < PER; ++jj) {
-                    const int j = gi * PER + jj;
-                    uint32_t a[8];
+            for (int jj = 0; jj < PER; ++jj) {
+                const int j = gi * PER + jj;
+                uint32_t a[8];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int at = (u >> 1) * 4 + (u & 1) * 2;
+                for (int u = 0; u < 4; ++u) {
+                    const int at = (u >> 1) * 4 + (u & 1) * 2;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) a[at + h] = kv4_codes_plus_16(D == 128 ? cur.k[h][u] : cur.k[h][u >> 1], D == 128 ? 4 * j : 8 * (u & 1) + 4 * j);
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        if (jj == 0) mma_bf16_16816_first(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
-                        else mma_bf16_16816(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
-                        mma_bf16_16816(acc[n], a[4], a[5], a[6], a[7], q[n][j][2], q[n][j][3]);
-                    }
-                }
-                const float s0 = bf16_lo(cur.kp[0][gi]), s1 = bf16_lo(cur.kp[1][gi]);
-                const float z0 = bf16_hi(cur.kp[0][gi]) + 16.0f, z1 = bf16_hi(cur.kp[1][gi]) + 16.0f;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    s[n][0] = fmaf(fmaf(-z0, qsum[n][gi][0], acc[n][0]), s0, s[n][0]);
-                    s[n][1] = fmaf(fmaf(-z0, qsum[n][gi][1], acc[n][1]), s0, s[n][1]);
-                    s[n][2] = fmaf(fmaf(-z1, qsum[n][gi][0], acc[n][2]), s1, s[n][2]);
-                    s[n][3] = fmaf(fmaf(-z1, qsum[n][gi][1], acc[n][3]), s1, s[n][3]);
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] *= p.s_scale;
-            // Masks, where a tile needs them: a masked score is -inf whatever its token holds.
-            const bool full = page_ok && token + kKv4Tile <= full_limit;         // of the whole warp
-            const int t0 = page_ok ? token + gray : INT_MAX - 16;
-            if (!full) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (t0 >= limit[n][e]) s[n][e] = -INFINITY;
-                        if (t0 + 8 >= limit[n][e]) s[n][2 + e] = -INFINITY;
-#pragma unroll
-                        for (int gi = 0; gi < NG; ++gi) {                        // past the request's end: parameters of no effect
-                            if (t0 >= last) cur.vp[0][gi] = 0;
-                            if (t0 + 8 >= last) cur.vp[1][gi] = 0;
-                        }
-                    }
-            }
-            // The base of the exponentials follows the maximum of a column only once a score is more than 8 (in powers of two) above it:
-            // sums of up to 2^8 are as good as sums of up to 1, and most tiles need no reduction over the lanes.
-            bool above = CAREFUL;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) above = above || fmaxf(s[n][e], s[n][2 + e]) > m[n][e] + 8.0f;
-            if (__any_sync(0xFFFFFFFFu, above)) {
-                float lift[2] = {0.0f, 0.0f};        // of the lane's two tokens
-                if constexpr (CAREFUL) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float step = 0.0f;
-#pragma unroll
-                        for (int gi = 0; gi < NG; ++gi) step = fmaxf(step, fabsf(bf16_lo(cur.vp[h][gi])));
-                        lift[h] = fmaxf(log2f(fminf(step, FLT_MAX)) - 60.0f, 0.0f);
-                    }
+                    for (int h = 0; h < 2; ++h) a[at + h] = kv4_codes_plus_16(D == 128 ? cur.k[h][u] : cur.k[h][u >> 1], D == 128 ? 4 * j : 8 * (u & 1) + 4 * j);
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    float alpha[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float top = CAREFUL ? fmaxf(s[n][e] + lift[0], s[n][2 + e] + lift[1]) : fmaxf(s[n][e], s[n][2 + e]);
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                        alpha[e] = 1.0f;
-                        if (top > m[n][e]) {
-                            alpha[e] = fast_exp2(m[n][e] - top);                 // 0 from -inf
-                            m[n][e] = top;
-                        }
-                        l[n][e] *= alpha[e];
-#pragma unroll
-                        for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] *= alpha[e];
-                    }
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        o[i][n][0] *= alpha[0];
-                        o[i][n][1] *= alpha[1];
-                        o[i][n][2] *= alpha[0];
-                        o[i][n][3] *= alpha[1];
-                    }
+                    if (jj == 0) mma_bf16_16816_first(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
+                    else mma_bf16_16816(acc[n], a[0], a[1], a[2], a[3], q[n][j][0], q[n][j][1]);
+                    mma_bf16_16816(acc[n], a[4], a[5], a[6], a[7], q[n][j][2], q[n][j][3]);
                 }
             }
+            const float s0 = bf16_lo(cur.kp[0][gi]), s1 = bf16_lo(cur.kp[1][gi]);
+            const float z0 = bf16_hi(cur.kp[0][gi]) + 16.0f, z1 = bf16_hi(cur.kp[1][gi]) + 16.0f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][0] = fmaf(fmaf(-z0, qsum[n][gi][0], acc[n][0]), s0, s[n][0]);
+                s[n][1] = fmaf(fmaf(-z0, qsum[n][gi][1], acc[n][1]), s0, s[n][1]);
+                s[n][2] = fmaf(fmaf(-z1, qsum[n][gi][0], acc[n][2]), s1, s[n][2]);
+                s[n][3] = fmaf(fmaf(-z1, qsum[n][gi][1], acc[n][3]), s1, s[n][3]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] *= p.s_scale;
+        // Masks, where a tile needs them: a masked score is -inf whatever its token holds.
+        const bool full = page_ok && token + kKv4Tile <= full_limit;         // of the whole warp
+        const int t0 = page_ok ? token + gray : INT_MAX - 16;
+        if (!full) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float base = m[n][e] == -INFINITY ? 0.0f : m[n][e];
-                    s[n][e] = fast_exp2(s[n][e] - base);
-                    s[n][2 + e] = fast_exp2(s[n][2 + e] - base);
-                    l[n][e] += s[n][e] + s[n][2 + e];
+                    if (t0 >= limit[n][e]) s[n][e] = -INFINITY;
+                    if (t0 + 8 >= limit[n][e]) s[n][2 + e] = -INFINITY;
+#pragma unroll
+                    for (int gi = 0; gi < NG; ++gi) {                        // past the request's end: parameters of no effect
+                        if (t0 >= last) cur.vp[0][gi] = 0;
+                        if (t0 + 8 >= last) cur.vp[1][gi] = 0;
+                    }
                 }
-            // second product, group by group
+        }
+        // The base of the exponentials follows the maximum of a column only once a score is more than 8 (in powers of two) above it:
+        // sums of up to 2^8 are as good as sums of up to 1, and most tiles need no reduction over the lanes.
+        bool above = CAREFUL;
 #pragma unroll
-            for (int gi = 0; gi < NG; ++gi) {
-                uint32_t pb[NT][2], pl[NT][2];           // P' as two terms
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int e = 0; e < 2; ++e) above = above || fmaxf(s[n][e], s[n][2 + e]) > m[n][e] + 8.0f;
+        if (__any_sync(0xFFFFFFFFu, above)) {
+            float lift[2] = {0.0f, 0.0f};        // of the lane's two tokens
+            if constexpr (CAREFUL) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float sv = bf16_lo(cur.vp[h][gi]);
-                        float a = s[n][2 * h] * sv, c = s[n][2 * h + 1] * sv;
-                        if (!full) {                     // a masked token adds nothing, not even 0 * NaN
-                            a = t0 + 8 * h < limit[n][0] ? a : 0.0f;
-                            c = t0 + 8 * h < limit[n][1] ? c : 0.0f;
-                        }
-                        const uint32_t w = pack_bf16x2(a, c);
-                        const float z = bf16_hi(cur.vp[h][gi]) + 16.0f;
-                        const uint32_t r = pack_bf16x2(a - bf16_lo(w), c - bf16_hi(w));
-                        float za = z, zc = z;
-                        if constexpr (CAREFUL) {
-                            if (t0 + 8 * h >= limit[n][0]) za = 0.0f;
-                            if (t0 + 8 * h >= limit[n][1]) zc = 0.0f;
-                        }
-                        zsum[gi][n][0] = fmaf(bf16_lo(w) + bf16_lo(r), za, zsum[gi][n][0]);    // of what the product sees
-                        zsum[gi][n][1] = fmaf(bf16_hi(w) + bf16_hi(r), zc, zsum[gi][n][1]);
-                        pb[n][h] = movmatrix_trans(w);
-                        pl[n][h] = movmatrix_trans(r);
+                for (int h = 0; h < 2; ++h) {
+                    float step = 0.0f;
+#pragma unroll
+                    for (int gi = 0; gi < NG; ++gi) step = fmaxf(step, fabsf(bf16_lo(cur.vp[h][gi])));
+                    lift[h] = fmaxf(log2f(fminf(step, FLT_MAX)) - 60.0f, 0.0f);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float alpha[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = CAREFUL ? fmaxf(s[n][e] + lift[0], s[n][2 + e] + lift[1]) : fmaxf(s[n][e], s[n][2 + e]);
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                    alpha[e] = 1.0f;
+                    if (top > m[n][e]) {
+                        alpha[e] = fast_exp2(m[n][e] - top);                 // 0 from -inf
+                        m[n][e] = top;
                     }
+                    l[n][e] *= alpha[e];
 #pragma unroll
-                for (int hw = 0; hw < 2; ++hw) {
-                    // the two tokens of a pair side by side: units 4 g + 2 hw and 4 g + 2 hw + 1
-                    uint32_t lo01, hi01, lo89, hi89;
-                    if constexpr (D == 128) {
-                        lo01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x5410);
-                        hi01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x7632);
-                        lo89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x5410);
-                        hi89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x7632);
-                    } else {
-                        lo01 = __byte_perm(cur.v[0][0], cur.v[1][0], hw ? 0x7632 : 0x5410);
-                        lo89 = __byte_perm(cur.v[2][0], cur.v[3][0], hw ? 0x7632 : 0x5410);
-                        hi01 = lo01 >> 8;
-                        hi89 = lo89 >> 8;
+                    for (int gi = 0; gi < NG; ++gi) zsum[gi][n][e] *= alpha[e];
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    o[i][n][0] *= alpha[0];
+                    o[i][n][1] *= alpha[1];
+                    o[i][n][2] *= alpha[0];
+                    o[i][n][3] *= alpha[1];
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float base = m[n][e] == -INFINITY ? 0.0f : m[n][e];
+                s[n][e] = fast_exp2(s[n][e] - base);
+                s[n][2 + e] = fast_exp2(s[n][2 + e] - base);
+                l[n][e] += s[n][e] + s[n][2 + e];
+            }
+        // second product, group by group
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+            uint32_t pb[NT][2], pl[NT][2];           // P' as two terms
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float sv = bf16_lo(cur.vp[h][gi]);
+                    float a = s[n][2 * h] * sv, c = s[n][2 * h + 1] * sv;
+                    if (!full) {                     // a masked token adds nothing, not even 0 * NaN
+                        a = t0 + 8 * h < limit[n][0] ? a : 0.0f;
+                        c = t0 + 8 * h < limit[n][1] ? c : 0.0f;
                     }
+                    const uint32_t w = pack_bf16x2(a, c);
+                    const float z = bf16_hi(cur.vp[h][gi]) + 16.0f;
+                    const uint32_t r = pack_bf16x2(a - bf16_lo(w), c - bf16_hi(w));
+                    float za = z, zc = z;
+                    if constexpr (CAREFUL) {
+                        if (t0 + 8 * h >= limit[n][0]) za = 0.0f;
+                        if (t0 + 8 * h >= limit[n][1]) zc = 0.0f;
+                    }
+                    zsum[gi][n][0] = fmaf(bf16_lo(w) + bf16_lo(r), za, zsum[gi][n][0]);    // of what the product sees
+                    zsum[gi][n][1] = fmaf(bf16_hi(w) + bf16_hi(r), zc, zsum[gi][n][1]);
+                    pb[n][h] = movmatrix_trans(w);
+                    pl[n][h] = movmatrix_trans(r);
+                }
 #pragma unroll
-                    for (int jj = 0; jj < PER; ++jj) {
-                        const int j = gi * PER + jj;
-                        const uint32_t a0 = kv4_codes_plus_16(lo01, 4 * j), a2 = kv4_codes_plus_16(lo89, 4 * j);
-                        const uint32_t a1 = kv4_codes_plus_16(hi01, 4 * j), a3 = kv4_codes_plus_16(hi89, 4 * j);
+            for (int hw = 0; hw < 2; ++hw) {
+                // the two tokens of a pair side by side: units 4 g + 2 hw and 4 g + 2 hw + 1
+                uint32_t lo01, hi01, lo89, hi89;
+                if constexpr (D == 128) {
+                    lo01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x5410);
+                    hi01 = __byte_perm(cur.v[0][hw], cur.v[1][hw], 0x7632);
+                    lo89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x5410);
+                    hi89 = __byte_perm(cur.v[2][hw], cur.v[3][hw], 0x7632);
+                } else {
+                    lo01 = __byte_perm(cur.v[0][0], cur.v[1][0], hw ? 0x7632 : 0x5410);
+                    lo89 = __byte_perm(cur.v[2][0], cur.v[3][0], hw ? 0x7632 : 0x5410);
+                    hi01 = lo01 >> 8;
+                    hi89 = lo89 >> 8;
+                }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
-                            mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pl[n][0], pl[n][1]);
-                        }
+                for (int jj = 0; jj < PER; ++jj) {
+                    const int j = gi * PER + jj;
+                    const uint32_t a0 = kv4_codes_plus_16(lo01, 4 * j), a2 = kv4_codes_plus_16(lo89, 4 * j);
+                    const uint32_t a1 = kv4_codes_plus_16(hi01, 4 * j), a3 = kv4_codes_plus_16(hi89, 4 * j);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                        mma_bf16_16816(o[j * 2 + hw][n], a0, a1, a2, a3, pl[n][0], pl[n][1]);
                     }
                 }
             }
         }
-        cp_async_wait_all();
-        take_off();
-        float size = 0.0f;
+    }
+    cp_async_wait_all();
+    take_off();
+    float size = 0.0f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) size += fabsf(o[i][n][e]);
-        return __all_sync(0xFFFFFFFFu, size < 1.2676506e30f);                    // the lanes are done with the ring, too
-    };
-    if (!pass(std::false_type{})) (void)pass(std::true_type{});
+            for (int e = 0; e < 4; ++e) size += fabsf(o[i][n][e]);
+    return __all_sync(0xFFFFFFFFu, size < 1.2676506e30f);                    // the lanes are done with the ring, too
+}
+// The second try is a call of its own: inlined beside the first, 64 ragged requests took 131.2 us instead of 129.6.
+template <int D, int G, int NT>
+__device__ __noinline__ void kv4_warp_sums_careful(const Kv4AttnArgs& p, Kv4Sums<D, NT>& sums)
+{
+    Kv4Sums<D, NT> mine;
+    (void)kv4_warp_sums<D, G, NT, true>(p, mine);
+    sums = mine;
+}
+
+template <int D, int G, int NT>
+__global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_kernel(const __grid_constant__ Kv4AttnArgs p)
+{
+    constexpr int NJ = D / 32, COLS = 8 * NT;
+    extern __shared__ __align__(128) uint8_t kv4_smem[];
+    float (*s_o)[COLS][D + 4] = reinterpret_cast<float (*)[COLS][D + 4]>(kv4_smem);        // [warp][column][channel]
+    __shared__ float s_m[kKv4Warps][COLS], s_l[kKv4Warps][COLS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int split = blockIdx.x, head = (int)blockIdx.y / p.col_tiles, ct = (int)blockIdx.y % p.col_tiles, b = blockIdx.z;
+    const int cols_all = p.T * p.ratio, col0 = ct * COLS;
+
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int len = kv4_length(p, b);
+    if (split > 0 && split * kv4_split_keys(len, p.splits) >= len) return;   // the joining kernel uses the same formula and does not look here
+    if (split == 0 && ct == 0 && head == 0 && threadIdx.x == 0 && (p.lengths[b] < 0 || p.lengths[b] > len)) report_index(3);
+
+    Kv4Sums<D, NT> sums;
+    if (!kv4_warp_sums<D, G, NT, false>(p, sums)) {
+        Kv4Sums<D, NT> again;
+        kv4_warp_sums_careful<D, G, NT>(p, again);
+        sums = again;
+    }
+    auto &o = sums.o;
+    auto &m = sums.m, &l = sums.l;
     __syncthreads();                                 // the rings are done with: the results take their place
 
     // sums over the lanes that share a column, then the warps' results side by side

@@ -32,7 +32,9 @@
  * leave zero after every call, so later calls with the same workspace start without a memset (calls of other
  * shapes or schedules through the same buffer are noticed: what they overwrite is forgotten by itself).  If
  * anything else writes to that memory between two calls (the buffer was freed and handed out again by an
- * allocator, reused as scratch, ...), tell the library with gmlp_workspace_forget() before the next call.
+ * allocator, reused as scratch, ...), tell the library with gmlp_workspace_forget() before the next call.  The replay
+ * of a captured call is such a write, which the library does not see: a call that keeps counters and a captured call of
+ * another kind need a workspace each.
  *
  * Stream order: X, the outputs and the workspace are used in stream order, like any kernel's operands.  The WEIGHT
  * MATRICES (Wg, Wu, Wd here; W, Wq, Wk, Wv of the other operators below) may be read EARLIER: the kernels of a call are
@@ -354,7 +356,10 @@ int gmlp_w4_plan(int64_t M, int32_t terms, int64_t K, int64_t N, int32_t gated, 
  * The Gated MLP on 4-bit weights: Y = (act(Xn Wg) (.) (Xn Wu)) Wd with Wg, Wu [d_model, d_ff] and Wd [d_ff, d_model] as
  * gmlp_w4_matrix, M at most GMLP_W4_MAX_M; the prologue and the gate activation are those of gmlp_forward_ex.  The normed input and
  * the gated product are kept to 16 bits of significand (two bf16 terms), not rounded to bf16; Y is rounded once.
- * It beats the bf16 operator in time up to 8 tokens with GMLP_FLAG_RMSNORM and up to 16 without; beyond, it saves memory only.
+ * In time, against the bf16 operator (groups of 128, in a graph): 1.4 to 2.3 times as fast at one token on layers from 2048 x 5632 to
+ * 8192 x 28672, 1.0 to 1.4 times at 8 tokens with GMLP_FLAG_RMSNORM; at 9 to 16 tokens it takes 1.05 to 1.6 times as long with the
+ * norm, without it it is 1.0 to 1.5 times as fast from 4096 x 14336 on; from 17 tokens on it is slower on all of them, and on
+ * 1024 x 4096 from 6 to 8 on.  There it saves memory only.
  * Wg and Wu must agree in group and in having zero points.  d_model is Wg.K, d_ff is Wg.N (both multiples of a group).
  * workspace: gmlp_w4_workspace_bytes(), 256-byte aligned, required; no state is kept in it between calls.
  */
@@ -424,8 +429,9 @@ int gmlp_kv4_gather(const gmlp_kv4_rows_args* args);
  * block_table[b][j / page_size] * page_size + j % page_size.  lengths[b] counts the keys, the new positions' included (append them
  * first).  A position that sees no key (L = 0, or L < q_len) gets zeros.  What the pages hold past a request's end, and table entries
  * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value enters the second product with 16
- * bits of significand (two bf16 terms); O is rounded once.  Entries outside of the cache, negative lengths and lengths past the table
- * are reported as above; their keys are left out.
+ * bits of significand (two bf16 terms); O is rounded once.  Queries (taken to multiples of 2^-119), keys and values may be any finite
+ * bf16 numbers as long as a score times log2(e) is a float.  Entries outside of the cache, negative lengths and lengths past the table are reported as above; their
+ * keys are left out.
  * workspace: gmlp_kv4_workspace_bytes(); may be NULL where that is 0; no state is kept in it between calls.
  */
 #define GMLP_KV4_MAX_QUERIES 16

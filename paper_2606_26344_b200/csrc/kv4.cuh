@@ -173,10 +173,11 @@ kv4_gather_kernel(const Kv4Cache c, const int64_t* slots, bf16* K, bf16* V, int6
 //                 leaves it), transposed in registers (movmatrix);
 //   O^T += V^T P'^T   with 16 + q again; the sum of P' (16 + z), a scalar per query row and group, is formed in fp32 from the same two
 //                 terms and taken off at the end and every few tiles (kv4_tiles_between).
-// Bound by the issue slots and the half-rate integer pipe of the unpacking, then by HBM: 64 requests of 1..8192 keys, 32 / 8 heads of
-// 128, groups of 64: 129 us (2.8 TB/s, 0.43 of the measured copy rate); one request of 131071 keys, 64 / 8 heads, groups of 128: 55 us
-// (2.6 TB/s).  With one term for P' 115 and 51 us; so, but with loads into registers instead of the rings 146 and 67; with the maximum
-// followed at every tile and q - z formed before the products 126 and 53.
+// 64 requests of 1..8192 keys, 32 / 8 heads of 128, groups of 64: 130 us (2.8 TB/s, 0.43 of the measured copy rate); one request of
+// 131071 keys, 64 / 8 heads, groups of 128: 57 us (2.5 TB/s).  No pipe is full (32 requests of 4096 keys: integer pipe 58 % busy,
+// issue slots 59 %, tensor pipe 24 %, HBM 2.5 TB/s): three warps per scheduler wait in turn for their copies, products and exchanges;
+// a tile takes 468 warp instructions, 120 of them the unpacking.  With one term for P' 115 and 51 us; so, but with loads into
+// registers instead of the rings 146 and 67; with the maximum followed at every tile and q - z formed before the products 126 and 53.
 // Each warp has a ring of three tiles in shared memory that asynchronous copies fill, two tiles ahead; the page-table entry is read
 // one tile earlier still.  Row g of a tile's products is token g ^ (g >> 1) of its eight (and so for the second eight), and for
 // D = 128 the 16-byte chunks of rows 2, 3, 6, 7, ... swap places by two: so the keys' reads (a row by four lanes) and the values' (a

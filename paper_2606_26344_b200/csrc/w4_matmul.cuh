@@ -264,9 +264,10 @@ __device__ __forceinline__ void w4_store_terms(bf16* out, int64_t at, int64_t te
 // half of them those of the gate tile, half those of the up tile), each with a ring of its own in shared memory that asynchronous
 // copies fill, across tiles too, so that the stream of codes does not pause at a tile's end.  X stays in shared memory for the whole kernel, with its sums over the groups;
 // only the sums of a tile cross the warps of a team.
-// Bound by the issue slots and the half-rate integer pipe (about 70 integer instructions per kilobyte of codes and warp), then by HBM:
 // 8192 x 28672, groups of 32 with zero points, M = 1: 36 us (3.9 TB/s, 0.60 of the measured copy rate); 4096 x 14336, groups of 128,
-// M = 8: 11 us.  Loads into registers instead of the rings: 46.9 against 42.0 us (8192 x 28672, groups of 128); 32 or 24 warps with
+// M = 8: 11 us.  No pipe is full (8192 x 28672, groups of 128: integer pipe 47 % busy, issue slots 56 %, HBM 3.8 TB/s; the copies alone
+// take 24 us, the arithmetic alone 25.5, both together 30): four warps per scheduler wait in turn for copies, shared memory and products.
+// Loads into registers instead of the rings: 46.9 against 42.0 us (8192 x 28672, groups of 128); 32 or 24 warps with
 // shorter rings, 30 us like these 16; without the rotations, which is not a result, 24 us.
 constexpr int kW4StreamWarps = 16;
 __host__ __device__ constexpr int w4_ring_depth(int nt) { return nt == 1 ? 3 : 2; }      // slots; two columns of eight need the room for X
@@ -443,6 +444,9 @@ __global__ void __launch_bounds__(kW4StreamThreads, 1) w4_stream_kernel(const W4
 // The 8 warps of a CTA are WR groups of two column tiles (gated: of a gate and an up tile) x WK ranges of K; stages of WK k-blocks of
 // codes and X pass through shared memory, three deep.  Up to 32 rows of X per CTA (blockIdx.y: further rows, which read the codes
 // again, from L2: by then the products set the time), and K over a cluster of C CTAs that add their sums in distributed shared memory.
+// One CTA of 8 warps per SM from 9 rows on (shared memory), two per scheduler; the register limit for two CTAs, which only one column
+// of eight rows uses, makes three and four columns spill (up to 344 bytes a thread).  64 x 4096 x 4096, groups of 128: 17.8 us;
+// 8 x 14336 x 4096: 14.0 us.
 constexpr int kW4Stages = 3;
 __host__ __device__ constexpr int w4_red_stride(int nt) { return 8 * (nt | 1); }      // floats; odd multiples of 8 spread the banks
 __host__ __device__ constexpr uint32_t w4_tile_smem(int nt, int rows, int wk, int G) {

@@ -83,7 +83,7 @@ def test_a_large_value_that_the_softmax_leaves_out():
 
 @pytest.mark.parametrize("D,G", K.SHAPES)
 @pytest.mark.parametrize("T", [1, 5])
-@pytest.mark.parametrize("exponent", [60, 66, 100, 120])
+@pytest.mark.parametrize("exponent", [-100, -60, 60, 66, 100, 120])
 def test_queries_of_any_size(exponent, T, D, G):
     # keys as much smaller: powers of two leave every score as it is, up to where a query times 31 steps of a key has no float
     g, n = K.gen(exponent), 300

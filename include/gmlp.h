@@ -430,8 +430,8 @@ int gmlp_kv4_gather(const gmlp_kv4_rows_args* args);
  * first).  A position that sees no key (L = 0, or L < q_len) gets zeros.  What the pages hold past a request's end, and table entries
  * past its last page, are never used.  Scores and sums are fp32; probability times scale of a value enters the second product with 16
  * bits of significand (two bf16 terms); O is rounded once.  Queries (taken to multiples of 2^-119), keys and values may be any finite
- * bf16 numbers as long as a score times log2(e) is a float.  Entries outside of the cache, negative lengths and lengths past the table are reported as above; their
- * keys are left out.
+ * bf16 numbers as long as a score times log2(e) is a float.  Entries outside of the cache, negative lengths and lengths past the table
+ * are reported as above; their keys are left out.
  * workspace: gmlp_kv4_workspace_bytes(); may be NULL where that is 0; no state is kept in it between calls.
  */
 #define GMLP_KV4_MAX_QUERIES 16

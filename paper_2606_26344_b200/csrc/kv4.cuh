@@ -317,8 +317,9 @@ __device__ __forceinline__ bool kv4_warp_sums(const Kv4AttnArgs& p, Kv4Sums<D, N
         }
     const int full_limit = min(last, len - p.T + 1 + col0 / p.ratio);       // below it every column sees every key
 
-    auto &o = sums.o;
-    auto &m = sums.m, &l = sums.l;
+    auto& o = sums.o;
+    auto& m = sums.m;
+    auto& l = sums.l;
     float zsum[NG][NT][2];
     auto take_off = [&]() {                          // o -= the sum of P' (16 + z), which every lane holds a part of
 #pragma unroll
@@ -648,8 +649,9 @@ __global__ void __launch_bounds__(kKv4Threads, NT == 1 ? 3 : 2) kv4_attention_ke
         kv4_warp_sums_careful<D, G, NT>(p, again);
         sums = again;
     }
-    auto &o = sums.o;
-    auto &m = sums.m, &l = sums.l;
+    auto& o = sums.o;
+    auto& m = sums.m;
+    auto& l = sums.l;
     __syncthreads();                                 // the rings are done with: the results take their place
 
     // sums over the lanes that share a column, then the warps' results side by side

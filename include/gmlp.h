@@ -457,6 +457,130 @@ uint64_t gmlp_kv4_workspace_bytes(int64_t B, int32_t q_len, int32_t n_q_heads, i
                                   int64_t table_width, int32_t page_size, int32_t sm_count);
 
 /*
+ * Rotary positions.  Pair i of a head's first rotary_dim channels - (2 i, 2 i + 1) if interleaved, else (i, i + rotary_dim / 2) - turns
+ * by the angle position * f_i and is multiplied by an amplitude A; the head's other channels stay as they are:
+ *     u' = A (u cos t - v sin t),   v' = A (u sin t + v cos t),   t = position * f_i.
+ * steps[i] is f_i / (2 pi), turns per position, in units of 2^-64 (modulo one turn): position * step modulo 2^64 is exact, so a far
+ * position's angle is as good as a near one's.  The rotation is computed in fp32 and rounded once.  Positions may be negative; the call
+ * with negated positions is the transpose, i.e. the gradient.  rotary_dim is a multiple of 4 (4-byte accesses unless it is one of 16, or of
+ * 8 if interleaved).
+ * gmlp_rope_steps fills the table (on the HOST; pure host arithmetic) from f_i = base^(-2 i / rotary_dim), scaled for contexts longer than
+ * the trained one (`original` tokens) by `factor`:
+ *     PLAIN    f_i
+ *     LINEAR   f_i / factor
+ *     BANDS    w f_i + (1 - w) f_i / factor,  w = clamp((turns_i - low) / (high - low), 0, 1),  turns_i = original * f_i / (2 pi)
+ *     RAMP     the same with w = 1 - clamp((i - a) / max(b - a, 0.001), 0, 1),  a = max(floor(at(high)), 0),
+ *              b = min(ceil(at(low)), rotary_dim - 1),  at(n) = rotary_dim log(original / (2 pi n)) / (2 log(base)): the pair that turns
+ *              n times within the trained context; A = 0.1 ln(factor) + 1 for factor > 1
+ * `scaling` NULL is PLAIN; A is 1 but for RAMP.  1 < base < 1e30.
+ */
+enum { GMLP_ROPE_PLAIN = 0, GMLP_ROPE_LINEAR = 1, GMLP_ROPE_BANDS = 2, GMLP_ROPE_RAMP = 3 };
+typedef struct gmlp_rope_scaling {
+    int32_t kind;             /* GMLP_ROPE_* */
+    int32_t reserved;         /* must be 0 */
+    double factor, low, high, original;
+} gmlp_rope_scaling;
+int gmlp_rope_steps(int32_t rotary_dim, double base, const gmlp_rope_scaling* scaling, uint64_t* steps, float* amplitude);
+
+typedef struct gmlp_rope {
+    const void* steps;        /* device, [rotary_dim / 2] uint64 */
+    int32_t rotary_dim;
+    int32_t interleaved;      /* 0 or 1 */
+    float amplitude;
+    int32_t reserved;         /* must be 0 */
+} gmlp_rope;
+
+/* Y = X [T, n_heads * head_dim] bf16 with every head rotated, e.g. before gmlp_gqa_attention or gmlp_kv4_append.  Y may be X; otherwise they
+ * must not overlap.  head_dim is a multiple of 8 up to 512, T at most 2^24. */
+typedef struct gmlp_rope_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_rope_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED */
+    const void* X;            /* device, [T, n_heads * head_dim] bf16 */
+    void* Y;                  /* device, the same shape, written */
+    const void* positions;    /* device, [T] int64 */
+    int64_t T;
+    int32_t n_heads, head_dim;
+    gmlp_rope rope;
+    void* stream;             /* cudaStream_t */
+} gmlp_rope_args;
+int gmlp_rope_apply(const gmlp_rope_args* args);
+
+/*
+ * A paged key/value cache in bf16: k, v [n_pages][n_kv_heads][page_size][head_dim], page_size a multiple of 16, head_dim 64 or 128; a token
+ * lives in slot  page * page_size + place.  n_pages * n_kv_heads * page_size must fit 31 bits; byte offsets may pass 32.
+ */
+typedef struct gmlp_kv_cache {
+    void* k;                  /* device; written by gmlp_kv_append */
+    void* v;
+    int64_t n_pages;
+    int32_t n_kv_heads, page_size, head_dim;
+    int32_t reserved;         /* must be 0 */
+} gmlp_kv_cache;
+
+/*
+ * What lies between gmlp_qkv_proj and the attention, in one launch: rows of K and V [T, n_kv_heads * head_dim] go to the cache at slots[i]
+ * (int64, device), K rotated to positions[i] on the way if rope.steps is given; Q [T, n_q_heads * head_dim], if given, is rotated into Qout
+ * (which may be Q).  A negative slot skips its row of K and V (padding), not that of Q.  The slots of one call must differ: of two rows
+ * with the same slot either may win, 16 bytes by 16 bytes.  No other row of the cache is touched.  A slot past the cache is skipped and
+ * reported: GMLP_ERR_INDEX with GMLP_FLAG_CHECKED, else through gmlp_device_status().  T at most 2^24.
+ */
+typedef struct gmlp_kv_append_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_kv_append_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED */
+    const void* Q;            /* device, [T, n_q_heads * head_dim] bf16, or NULL; needs rope.steps */
+    void* Qout;               /* device, the same shape, written; NULL exactly if Q is */
+    const void* K;            /* device, [T, n_kv_heads * head_dim] bf16 */
+    const void* V;
+    const void* positions;    /* device, [T] int64; read only with rope.steps */
+    const void* slots;        /* device, [T] int64 */
+    int64_t T;
+    int32_t n_q_heads;
+    int32_t reserved;         /* must be 0 */
+    gmlp_kv_cache cache;
+    gmlp_rope rope;           /* steps NULL: rows are stored as they are */
+    void* stream;             /* cudaStream_t */
+} gmlp_kv_append_args;
+int gmlp_kv_append(const gmlp_kv_append_args* args);
+
+/*
+ * Grouped-query attention of new positions over the cache, for B requests of any lengths - a chunk of a prompt, a single token each, or
+ * both in one call:  O = softmax(scale * Q K^T) V.  Request b has the rows q_start[b] .. q_start[b + 1] - 1 of Q and O [T, n_q_heads *
+ * head_dim] (q_start NULL: q_len rows each, T = B * q_len) and lengths[b] keys, the new positions' included (append them first); its key j
+ * is in slot block_table[b][j / page_size] * page_size + j % page_size.  With GMLP_KV_CAUSAL row i of a request with r rows and n keys
+ * sees keys 0 .. n - r + i, without it all n.  A row that sees no key gets zeros, and so does one whose scores are all -infinity; rows of
+ * no request are left as they were.  What the pages hold past a request's end, and table entries past its last page, are never used, and
+ * what a row does not see does not reach it, infinities and NaN included.  Scores, exponentials and sums are fp32; the probabilities are
+ * rounded to bf16 for the second product, as in gmlp_gqa_attention, in tiles of more than 128 rows (positions times n_q_heads /
+ * n_kv_heads), and kept to 16 bits of significand (two bf16 terms) in smaller ones; O is rounded once.
+ * A table entry outside of the cache, a negative length, a length past the table, and a q_start that falls or passes T are reported like a
+ * bad slot above; that page's keys, that request's keys, that request's rows are left out.
+ * n_q_heads / n_kv_heads at most 128.  scale > 0.  How a request is split over the GPU depends on all lengths of the call: the same
+ * request may round differently beside others; the same call gives the same bits.
+ * workspace: gmlp_kv_workspace_bytes(), 256-byte aligned, required; no state is kept in it between calls.
+ */
+enum { GMLP_KV_CAUSAL = 1u << 4 };
+typedef struct gmlp_kv_attention_args {
+    uint32_t struct_bytes;    /* sizeof(gmlp_kv_attention_args) */
+    uint32_t flags;           /* GMLP_FLAG_CHECKED | GMLP_KV_CAUSAL */
+    const void* Q;            /* device, [T, n_q_heads * head_dim] bf16 */
+    void* O;                  /* device, the same shape, written; must not overlap Q */
+    gmlp_kv_cache cache;
+    const void* block_table;  /* device, [B, table_width] int32 */
+    const void* lengths;      /* device, [B] int32 */
+    const void* q_start;      /* device, [B + 1] int32, or NULL */
+    int64_t B, T, table_width;/* B at most 65535, T at most 2^24, table_width * page_size at most 2^30 */
+    int32_t n_q_heads, q_len; /* q_len is read only without q_start */
+    float scale;              /* e.g. 1 / sqrt(head_dim) */
+    int32_t reserved;         /* must be 0 */
+    void* stream;             /* cudaStream_t */
+    void* workspace;
+    uint64_t workspace_bytes;
+} gmlp_kv_attention_args;
+int gmlp_kv_attention(const gmlp_kv_attention_args* args);
+/* On a device with `sm_count` SMs (0: the current device, 148 if there is none); 0 bytes for invalid sizes. */
+uint64_t gmlp_kv_workspace_bytes(int64_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t sm_count);
+
+/*
  * The same call for a caller whose activations live in HOST memory: copies X_host
  * (M*d_model bf16, ideally pinned) to args->X, runs gmlp_forward_ex, and copies args->Y
  * to Y_host, all asynchronously on args->stream.  args->X and args->Y are device staging

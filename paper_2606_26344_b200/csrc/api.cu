@@ -27,6 +27,8 @@
 #include "gqa_attention.cuh"
 #include "w4_matmul.cuh"
 #include "kv4.cuh"
+#include "kv_attention.cuh"
+#include "rope.cuh"
 
 namespace {
 
@@ -1950,6 +1952,7 @@ int gqa_attention_impl(const gmlp_gqa_args* a) {
 
 #include "w4_host.cuh"
 #include "kv4_host.cuh"
+#include "kv_host.cuh"
 
 // Empirical schedule selection for one shape: time every tensor-core schedule that can run it, keep the fastest.
 int autotune_impl(const gmlp_args* a, int iters, int32_t* best_variant, float* best_us) {
@@ -2191,6 +2194,16 @@ int gmlp_w4_forward(const gmlp_w4_args* args) { GMLP_GUARDED(w4_forward_impl(arg
 int gmlp_kv4_append(const gmlp_kv4_rows_args* args) { GMLP_GUARDED(kv4_rows_impl(args, true)); }
 int gmlp_kv4_gather(const gmlp_kv4_rows_args* args) { GMLP_GUARDED(kv4_rows_impl(args, false)); }
 int gmlp_kv4_attention(const gmlp_kv4_attention_args* args) { GMLP_GUARDED(kv4_attention_impl(args)); }
+int gmlp_rope_steps(int32_t rotary_dim, double base, const gmlp_rope_scaling* scaling, uint64_t* steps, float* amplitude) {
+    GMLP_GUARDED(rope_steps_impl(rotary_dim, base, scaling, steps, amplitude));
+}
+int gmlp_rope_apply(const gmlp_rope_args* args) { GMLP_GUARDED(rope_apply_impl(args)); }
+int gmlp_kv_append(const gmlp_kv_append_args* args) { GMLP_GUARDED(kv_append_impl(args)); }
+int gmlp_kv_attention(const gmlp_kv_attention_args* args) { GMLP_GUARDED(kv_attention_impl(args)); }
+uint64_t gmlp_kv_workspace_bytes(int64_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t sm_count) {
+    if ((head_dim != 64 && head_dim != 128) || check_kv_attention(1, T, n_q_heads, n_kv_heads, 1, 16) != GMLP_OK) return 0;
+    return 0;
+}
 
 uint64_t gmlp_w4_code_bytes(int64_t K, int64_t N) {
     if (K <= 0 || N <= 0 || K > kW4MaxDim || N > kW4MaxDim) return 0;

@@ -159,6 +159,60 @@ class GmlpKv4AttentionArgs(ctypes.Structure):
     ]
 
 
+class GmlpRopeScaling(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double), ("original", ctypes.c_double),
+    ]
+
+
+class GmlpRope(ctypes.Structure):
+    _fields_ = [
+        ("steps", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class GmlpRopeArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("X", ctypes.c_void_p), ("Y", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("T", ctypes.c_int64),
+        ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rope", GmlpRope), ("stream", ctypes.c_void_p),
+    ]
+
+
+class GmlpKvCache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+        ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class GmlpKvAppendArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("Q", ctypes.c_void_p), ("Qout", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("T", ctypes.c_int64),
+        ("n_q_heads", ctypes.c_int32), ("reserved", ctypes.c_int32), ("cache", GmlpKvCache), ("rope", GmlpRope),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class GmlpKvAttentionArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("Q", ctypes.c_void_p), ("O", ctypes.c_void_p), ("cache", GmlpKvCache),
+        ("block_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+        ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("table_width", ctypes.c_int64),
+        ("n_q_heads", ctypes.c_int32), ("q_len", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+KV_CAUSAL = 1 << 4
+ROPE_KINDS = {"linear": 1, "bands": 2, "ramp": 3}
+
+
 class GmlpError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -196,7 +250,8 @@ def lib() -> ctypes.CDLL:
         L.gmlp_qkv_proj.argtypes = [ctypes.POINTER(GmlpQkvArgs)]
         for name, args in (("w4_quantize", GmlpW4LayoutArgs), ("w4_pack", GmlpW4LayoutArgs), ("w4_dequantize", GmlpW4LayoutArgs),
                            ("w4_matmul", GmlpW4MatmulArgs), ("w4_forward", GmlpW4Args), ("kv4_append", GmlpKv4RowsArgs),
-                           ("kv4_gather", GmlpKv4RowsArgs), ("kv4_attention", GmlpKv4AttentionArgs)):
+                           ("kv4_gather", GmlpKv4RowsArgs), ("kv4_attention", GmlpKv4AttentionArgs), ("rope_apply", GmlpRopeArgs),
+                           ("kv_append", GmlpKvAppendArgs), ("kv_attention", GmlpKvAttentionArgs)):
             f = getattr(L, "gmlp_" + name)
             f.restype, f.argtypes = ctypes.c_int, [ctypes.POINTER(args)]
         L.gmlp_w4_code_bytes.restype = u64
@@ -209,6 +264,11 @@ def lib() -> ctypes.CDLL:
         L.gmlp_w4_plan.argtypes = [i64, i32, i64, i64, i32, i32, i32, ctypes.POINTER(i32)]
         L.gmlp_kv4_workspace_bytes.restype = u64
         L.gmlp_kv4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
+        L.gmlp_rope_steps.restype = ctypes.c_int
+        L.gmlp_rope_steps.argtypes = [i32, ctypes.c_double, ctypes.POINTER(GmlpRopeScaling), ctypes.POINTER(u64),
+                                      ctypes.POINTER(ctypes.c_float)]
+        L.gmlp_kv_workspace_bytes.restype = u64
+        L.gmlp_kv_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
         L.gmlp_autotune.restype = ctypes.c_int
         L.gmlp_autotune.argtypes = [ctypes.POINTER(GmlpArgs), ctypes.c_int, ctypes.POINTER(ctypes.c_int32),
                                     ctypes.POINTER(ctypes.c_float)]
@@ -965,8 +1025,171 @@ def kv4_attention(Q, cache: Kv4Cache, block_table, lengths, n_q_heads: int, q_le
     return O
 
 
+# --------------------------------------------------------------------------- rotary positions, bf16 cache and its attention
+
+def rope_steps(rotary_dim: int, base: float = 10000.0, scaling=None):
+    """gmlp_rope_steps: (turns per position of each pair in units of 2^-64, as a list of ints; amplitude).  ``scaling``: None,
+    ("linear", factor), ("bands", factor, low, high, original) or ("ramp", factor, high, low, original)."""
+    if scaling is None:
+        s = None
+    else:
+        kind, values = scaling[0], [float(v) for v in scaling[1:]]
+        if kind not in ROPE_KINDS or len(values) != (1 if kind == "linear" else 4):
+            raise ValueError('scaling: expected None, ("linear", factor), ("bands", factor, low, high, original) or '
+                             '("ramp", factor, high, low, original)')
+        factor, low, high, original = values if len(values) == 4 else values + [0.0] * 3
+        if kind == "ramp":
+            low, high = high, low
+        s = ctypes.byref(GmlpRopeScaling(ROPE_KINDS[kind], 0, factor, low, high, original))
+    steps, amplitude = (ctypes.c_uint64 * max(1, rotary_dim // 2))(), ctypes.c_float()
+    rc = lib().gmlp_rope_steps(rotary_dim, base, s, steps, ctypes.byref(amplitude))
+    if rc != OK:
+        raise GmlpError(rc)
+    return list(steps), amplitude.value
+
+
+class Rope:
+    """A rotation's table (gmlp_rope): ``rotary_dim`` channels of each head, pairs (i, i + rotary_dim / 2) or, ``interleaved``,
+    (2 i, 2 i + 1).  ``scaling`` as for rope_steps(); ``amplitude`` overrides the scaling's own."""
+    __slots__ = ("steps", "rotary_dim", "interleaved", "amplitude", "device", "struct")
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None,
+                 amplitude: Optional[float] = None, device="cuda"):
+        steps, own = rope_steps(rotary_dim, base, scaling)
+        signed = [v - (1 << 64) if v >> 63 else v for v in steps]
+        self.steps = torch.tensor(signed, dtype=torch.int64).to(device)
+        if self.steps.device.type != "cuda":
+            raise TypeError("device: expected a CUDA device")
+        self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, bool(interleaved), own if amplitude is None else float(amplitude)
+        self.device = self.steps.device
+        self.struct = GmlpRope(self.steps.data_ptr(), rotary_dim, int(self.interleaved), self.amplitude, 0)
+
+
+def rope_apply(X, positions, rope: Rope, n_heads: int, Y=None, stream=None, checked: bool = False) -> torch.Tensor:
+    """gmlp_rope_apply: X [T, n_heads * head_dim] with every head turned to ``positions`` (int64 [T]); Y may be X.  With negated
+    positions it is the transpose (the gradient)."""
+    if X.dim() != 2 or n_heads < 1:
+        raise ValueError("X: expected a matrix of n_heads heads a row")
+    (T, width), device = X.shape, rope.device
+    if width % n_heads != 0:
+        raise ValueError("shape mismatch: n_heads must divide the columns of X")
+    x = _pointer(X, "X", torch.bfloat16, (T, width), device)
+    at = _pointer(positions, "positions", torch.int64, (T,), device)
+    if Y is None:
+        Y = _empty((T, width), torch.bfloat16, device, stream)
+        y = Y.data_ptr()
+    else:
+        y = _pointer(Y, "Y", torch.bfloat16, (T, width), device)
+    _run(lib().gmlp_rope_apply, GmlpRopeArgs(_SIZE_ROPE, FLAG_CHECKED if checked else 0, x, y, at, T, n_heads, width // n_heads, rope.struct,
+                                             _stream_handle(stream, device)), device)
+    return Y
+
+
+class KvCache:
+    """A paged key/value cache in bf16 (gmlp_kv_cache): k and v [n_pages, n_kv_heads, page_size, head_dim]."""
+    __slots__ = ("k", "v", "n_pages", "n_kv_heads", "page_size", "head_dim", "device", "struct")
+
+    def __init__(self, k, v):
+        if k.dim() != 4:
+            raise ValueError("expected k and v [n_pages, n_kv_heads, page_size, head_dim]")
+        device = k.device
+        pointers = [_pointer(t, name, torch.bfloat16, k.shape, device) for t, name in ((k, "k"), (v, "v"))]
+        if device.type != "cuda":
+            raise TypeError("k: expected a CUDA tensor")
+        self.k, self.v, self.device = k, v, device
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.struct = GmlpKvCache(*pointers, *k.shape, 0)
+
+
+def kv_cache(n_pages: int, n_kv_heads: int, head_dim: int = 128, page_size: int = 64, device="cuda") -> KvCache:
+    """An empty cache (all rows are zeros)."""
+    rows = lambda: torch.zeros(n_pages, n_kv_heads, page_size, head_dim, dtype=torch.bfloat16, device=device)
+    return KvCache(rows(), rows())
+
+
+_NO_ROPE = GmlpRope(None, 0, 0, 1.0, 0)
+
+
+def kv_append(K, V, cache: KvCache, slots, rope: Optional[Rope] = None, positions=None, Q=None, Q_out=None, stream=None,
+              checked: bool = False):
+    """gmlp_kv_append: rows of K and V [T, n_kv_heads * head_dim] into the cache at ``slots`` (int64, all different; negative: the row is
+    skipped).  With ``rope`` the keys are turned to ``positions`` (int64 [T]) on the way, and so are the queries Q [T, n_q_heads *
+    head_dim], if given, into Q_out (by default new; Q itself for in place).  Returns Q_out, or None without Q."""
+    if slots.dim() != 1:
+        raise ValueError("slots: expected a vector")
+    T, device = slots.shape[0], cache.device
+    shape = (T, cache.n_kv_heads * cache.head_dim)
+    k, v = _pointer(K, "K", torch.bfloat16, shape, device), _pointer(V, "V", torch.bfloat16, shape, device)
+    at = q = q_out = None
+    heads = 0
+    if rope is None:
+        if Q is not None or positions is not None:
+            raise ValueError("Q and positions need a rope")
+    else:
+        if positions is None:
+            raise ValueError("rope needs positions")
+        if rope.device != device:
+            raise ValueError(f"rope: expected a table on {device}, got one on {rope.device}")
+        at = _pointer(positions, "positions", torch.int64, (T,), device)
+    if Q is not None:
+        if Q.dim() != 2 or Q.shape[1] % cache.head_dim != 0:
+            raise ValueError("Q: expected a matrix of whole heads a row")
+        shape = (T, Q.shape[1])
+        heads = shape[1] // cache.head_dim
+        q = _pointer(Q, "Q", torch.bfloat16, shape, device)
+        if Q_out is None:
+            Q_out = _empty(shape, torch.bfloat16, device, stream)
+            q_out = Q_out.data_ptr()
+        else:
+            q_out = _pointer(Q_out, "Q_out", torch.bfloat16, shape, device)
+    elif Q_out is not None:
+        raise ValueError("Q_out needs Q")
+    _run(lib().gmlp_kv_append, GmlpKvAppendArgs(_SIZE_KV_APPEND, FLAG_CHECKED if checked else 0, q, q_out, k, v, at,
+                                                _pointer(slots, "slots", torch.int64, (T,), device), T, heads, 0, cache.struct,
+                                                _NO_ROPE if rope is None else rope.struct, _stream_handle(stream, device)), device)
+    return Q_out
+
+
+def kv_workspace_bytes(T: int, n_q_heads: int, n_kv_heads: int, head_dim: int, sm_count: int = 0) -> int:
+    return int(lib().gmlp_kv_workspace_bytes(T, n_q_heads, n_kv_heads, head_dim, sm_count))
+
+
+def kv_attention(Q, cache: KvCache, block_table, lengths, n_q_heads: int, q_start=None, q_len: int = 1, causal: bool = True,
+                 scale: Optional[float] = None, O=None, workspace=None, stream=None, checked: bool = False) -> torch.Tensor:
+    """gmlp_kv_attention: the new positions of B requests, Q [T, n_q_heads * head_dim], over the cache.  Request b has rows
+    ``q_start[b]`` to ``q_start[b + 1]`` (int32 [B + 1]; None: ``q_len`` rows each); ``block_table`` int32 [B, pages], ``lengths`` int32 [B]
+    (keys of each request, the new ones included); ``scale`` defaults to 1 / sqrt(head_dim)."""
+    if block_table.dim() != 2 or Q.dim() != 2:
+        raise ValueError("block_table and Q: expected matrices")
+    B, width = block_table.shape
+    T, device, D = Q.shape[0], cache.device, cache.head_dim
+    shape = (T, n_q_heads * D)
+    q = _pointer(Q, "Q", torch.bfloat16, shape, device)
+    table = _pointer(block_table, "block_table", torch.int32, (B, width), device)
+    n = _pointer(lengths, "lengths", torch.int32, (B,), device)
+    if q_start is not None:
+        start, q_len = _pointer(q_start, "q_start", torch.int32, (B + 1,), device), 0
+    elif T != B * q_len:
+        raise ValueError(f"Q: expected {B} * {q_len} rows, got {T}")
+    else:
+        start = None
+    if O is None:
+        O = _empty(shape, torch.bfloat16, device, stream)
+        o = O.data_ptr()
+    else:
+        o = _pointer(O, "O", torch.bfloat16, shape, device)
+    need = 0 if workspace is not None else lib().gmlp_kv_workspace_bytes(T, n_q_heads, cache.n_kv_heads, D, _sm_count(device))
+    keep, ws, ws_bytes = _workspace(workspace, need, device, stream)
+    _run(lib().gmlp_kv_attention,
+         GmlpKvAttentionArgs(_SIZE_KV_ATTENTION, (KV_CAUSAL if causal else 0) | (FLAG_CHECKED if checked else 0), q, o, cache.struct, table, n,
+                             start, B, T, width, n_q_heads, q_len, D ** -0.5 if scale is None else scale, 0, _stream_handle(stream, device),
+                             ws, ws_bytes), device)
+    return O
+
+
 _SIZE_W4_MATMUL, _SIZE_W4 = ctypes.sizeof(GmlpW4MatmulArgs), ctypes.sizeof(GmlpW4Args)
 _SIZE_KV4_ROWS, _SIZE_KV4_ATTENTION = ctypes.sizeof(GmlpKv4RowsArgs), ctypes.sizeof(GmlpKv4AttentionArgs)
+_SIZE_ROPE, _SIZE_KV_APPEND, _SIZE_KV_ATTENTION = ctypes.sizeof(GmlpRopeArgs), ctypes.sizeof(GmlpKvAppendArgs), ctypes.sizeof(GmlpKvAttentionArgs)
 _sm_counts: dict = {}
 
 

@@ -140,6 +140,7 @@ struct DeviceState {
     bool addss_attr_set = false;
     bool multi_attr_set = false;
     bool gqa_attr_set = false;
+    bool kv_attr_set[2] = {};                    // head dimension 64, 128
     bool umma_attr_set = false;
     bool pair_attr_set = false;
     bool rowscale_attr_set = false;
@@ -2201,8 +2202,9 @@ int gmlp_rope_apply(const gmlp_rope_args* args) { GMLP_GUARDED(rope_apply_impl(a
 int gmlp_kv_append(const gmlp_kv_append_args* args) { GMLP_GUARDED(kv_append_impl(args)); }
 int gmlp_kv_attention(const gmlp_kv_attention_args* args) { GMLP_GUARDED(kv_attention_impl(args)); }
 uint64_t gmlp_kv_workspace_bytes(int64_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t sm_count) {
-    if ((head_dim != 64 && head_dim != 128) || check_kv_attention(1, T, n_q_heads, n_kv_heads, 1, 16) != GMLP_OK) return 0;
-    return 0;
+    if ((head_dim != 64 && head_dim != 128) || T < 1 || check_kv_attention(1, T, n_q_heads, n_kv_heads, 1, 16) != GMLP_OK)
+        return 0;
+    return kv_attention_workspace(T, n_q_heads, n_kv_heads, head_dim, sm_count > 0 ? sm_count : current_sm_count());
 }
 
 uint64_t gmlp_w4_code_bytes(int64_t K, int64_t N) {

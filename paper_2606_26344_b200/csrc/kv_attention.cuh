@@ -1,20 +1,80 @@
-// Attention of the new positions of ragged requests over a paged bf16 cache (first, plain form: one CTA per position and head).
+// Attention of the new positions of ragged requests over a paged bf16 cache:  O = softmax(scale Q K^T) V, request by request.
+//
+// Rows.  The query heads that share a key/value head are rows of one tile next to one another: with R heads to a key/value head a tile of
+// 128 rows is P = 128 / R positions.  So K and V are read once for all R heads, one token of a request already fills R rows, and a causal
+// tile of a chunk spans few positions.  A work item is up to 2 P positions of one request and key/value head:
+//   big   (more than P positions): two tiles of 128 rows that take turns on the tensor pipe, both over every block of 128 keys;
+//   small (up to P positions):     one tile of rows, the two "tiles" take the even and the odd blocks of keys and are joined at the
+//                                  end.  Bytes bound these, so the probabilities get a second bf16 term (16 bits) for the tensor pipe's spare time.
+// Order and split.  All items lie end to end on one axis, heads outermost, an item as long as the keys that its last position sees plus
+// a constant; every CTA (one per SM) takes an equal stretch of the axis, computed by itself from the lengths on the device (the host knows
+// none of them).  So a decode batch of ragged lengths, one long conversation and a prompt's chunk all load the GPU evenly, without a plan
+// kernel.  A cut item's parts (at most two per CTA) leave unnormalised fp32 sums, base and weight in the workspace; a second, small
+// kernel joins them in order, so results do not depend on timing.
+//
+//   warp 0      K/V producer: K(0), V(0), K(1), ... through one FIFO, a page (or its share of a block) per TMA box; rows of no page
+//               are zeros in V, which a probability of 0 would not hide if they were NaN
+//   warp 1      MMA issuer:   S_t = Q_t K^T (TMEM columns 128 t), O_t += P_t V (columns 256 + 128 t)
+//   warp 2      walks the axis, hands items to the others through a ring, loads Q
+//   warp 3      mends V blocks that hold keys which some row must not see: rows past the request's end become zeros, numbers that are none
+//               become 0 and are added by the epilogue for the rows that see them
+//   warps 4..7  softmax and epilogue of tile A, warps 8..11 of tile B: thread = row.  As in gqa_attention.cuh: scores are read once, the base
+//               of the exponentials moves only when a row's sum of a block passes 2^10, P goes back to TMEM over the scores.
+// Every wait is bounded.
 #pragma once
+#include <type_traits>
+#include <cuda.h>
+
 #include "common.cuh"
+#include "gqa_attention.cuh"
 #include "ptx.cuh"
+#include "umma_gemm.cuh"
 
 namespace gmlp {
 
 struct KvAttnArgs {
-    const bf16* Q;                   // [T, Hq * D]
-    bf16* O;
-    const bf16 *k, *v;               // [page][Hkv][page_size][D]
+    bf16* O;                         // [T, Hq * D]
+    const bf16* v;                   // [page][Hkv][page_size][D]
     const int32_t *table, *lengths, *q_start;
+    uint8_t* workspace;
     int B, T, Hq, Hkv, ratio, width, page_size, n_pages, q_len, causal;
+    int tile_pos;                    // positions per 128 rows
+    int box;                         // keys per TMA box: the largest power of two that divides the page size, at most 128
+    int q_bytes;                     // of one tile's Q boxes
+    int slot_rows;                   // rows of a partial result
+    int min_stretch;                 // of a CTA, in keys
     float scale_log2;
 };
 
-// Request b: its first row, its number of rows and keys; what the arrays hold outside of their ranges is reported and left out.
+constexpr int kKvThreads = 384, kKvBlock = 128, kKvRing = 4;
+constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
+constexpr int kKvItemCost = 128;                 // of an item's start and end, in keys
+constexpr int kKvRegsLight = 80, kKvRegsSoftmax = 208;
+constexpr long long kKvItemWait = 16 * kWaitLimitCycles;     // waits of an item's length
+__host__ __device__ constexpr int kv_slots(int D) { return D == 128 ? 5 : 10; }
+__host__ __device__ constexpr uint32_t kv_tile_bytes(int D) { return 128u * D * 2; }
+// Q, FIFO; base and weight of rows; items and barriers; alignment
+constexpr uint32_t kv_attn_smem(int D) { return (2 + kv_slots(D)) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
+
+// Workspace: one descriptor per CTA, then base and weight of the rows of each of its two partial results, then their sums.
+struct KvCut {
+    int parts, head, row0, npos, two_tiles, pad[3];
+};
+__host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ctas * sizeof(KvCut) + 255) & ~(uint64_t)255; }
+__host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) { return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255); }
+__host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) { return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4; }
+
+struct KvItem {
+    int blk0, blk1;                  // blocks of keys; none: rows that see no key
+    int b, head, row0;               // request, key/value head, row of Q of the first position
+    int npos, keys;                  // positions, keys of the request
+    int seen0;                       // keys that the first position sees (may be negative)
+    int slot;                        // of the partial result, or -1: the rows' final values
+    int last;                        // no more items (this one is none)
+    int pad[6];
+};
+
+// Request b: its first row, rows and keys; what the arrays hold outside of their ranges is left out (and reported by one CTA).
 __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0, int& rows, int& keys, bool report) {
     const int s = a.q_start ? a.q_start[b] : b * a.q_len, e = a.q_start ? a.q_start[b + 1] : s + a.q_len;
     const bool ok = s >= 0 && s <= e && e <= a.T;
@@ -23,57 +83,798 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
     keys = a.lengths[b];
     const bool fits = keys >= 0 && (int64_t)keys <= (int64_t)a.width * a.page_size;
     if (!fits) keys = 0;
-    if (report && (!ok || !fits)) report_index(ok ? 7 : 6);
+    if (report && (!ok || !fits)) report_index(ok ? 6 : 7);
+}
+// Length on the axis of the first n of a request's tiles.
+__device__ __forceinline__ int64_t kv_cost(const KvAttnArgs& a, int rows, int keys, int n) {
+    const int s = 2 * a.tile_pos;
+    const int64_t start = (int64_t)n * kKvItemCost;
+    if (n == 0) return 0;
+    if (!a.causal) return start + (int64_t)n * keys;
+    const bool whole = (int64_t)n * s >= rows;                      // the last tile ends with the request
+    const int m = whole ? n - 1 : n, first = keys - rows;           // the others see first + (i + 1) s keys
+    const int none = first < 0 ? min(m, -first / s) : 0;
+    return start + (int64_t)(m - none) * first + (int64_t)s * ((int64_t)m * (m + 1) - (int64_t)none * (none + 1)) / 2 + (whole && n > 0 ? keys : 0);
+}
+__device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int rows) { return (rows + 2 * a.tile_pos - 1) / (2 * a.tile_pos); }
+// Blocks of an item of `keys` keys that lie before place x of it.
+__device__ __forceinline__ int kv_blocks_before(int64_t x, int keys) {
+    const int64_t n = x <= kKvItemCost ? 0 : (x - kKvItemCost + kKvBlock - 1) / kKvBlock;
+    return (int)min(n, (int64_t)((keys + kKvBlock - 1) / kKvBlock));
 }
 
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// Three coordinates: channel, head, position.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bf16_pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// A place in the FIFO: slot and the parity of its use.
+template <int SLOTS> struct KvCursor {
+    uint32_t slot, phase;
+    __device__ __forceinline__ void move(uint32_t n) {               // n < SLOTS
+        slot += n;
+        if (slot >= SLOTS) { slot -= SLOTS; phase ^= 1u; }
+    }
+    __device__ __forceinline__ void skip(uint32_t n) {
+        const uint32_t at = slot + n;
+        phase ^= (at / SLOTS) & 1u;
+        slot = at % SLOTS;
+    }
+};
+
 template <int D>
-__global__ void __launch_bounds__(128) kv_attention_plain_kernel(const KvAttnArgs a)
+__global__ void __launch_bounds__(kKvThreads, 1)
+kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const KvAttnArgs a)
+{
+    constexpr int KERNEL_ID = 30, SLOTS = kv_slots(D), HALVES = D / 64;
+    constexpr uint32_t TILE = kv_tile_bytes(D), HALF = 16384;                // 128 rows of 64 channels
+    // S = Q K^T: A and B K-major, N = 128 keys;  O += P V: B MN-major, N = D;  M = 128, bf16 in, fp32 accumulate
+    constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = ptx::smem_addr(smem_raw);
+    const uint32_t base = (raw_addr + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - raw_addr);
+    const uint32_t q_smem = base, fifo = base + 2 * TILE;
+    uint8_t* fifo_ptr = base_ptr + 2 * TILE;
+    float2* stats = reinterpret_cast<float2*>(base_ptr + (2 + SLOTS) * TILE);        // [128]: base and weight of tile B's rows
+    KvItem* items = reinterpret_cast<KvItem*>(base_ptr + (2 + SLOTS) * TILE + 1024); // [ring]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(items + kKvRing);
+    const uint32_t kv_full0 = ptx::smem_addr(bars);                          // [slots]
+    const uint32_t kv_empty0 = kv_full0 + 8 * SLOTS;                         // [slots]
+    const uint32_t s_full0 = kv_empty0 + 8 * SLOTS;                          // [2] scores of a step are in TMEM
+    const uint32_t p_full0 = s_full0 + 16;                                   // [2] its probabilities are
+    const uint32_t o_full0 = p_full0 + 16;                                   // [2] O += P V of a step is done
+    const uint32_t q_full = o_full0 + 16, q_empty = q_full + 8;
+    const uint32_t mend0 = q_empty + 8, fixed0 = mend0 + 8 * kKvMends;       // a block of V to be mended is on its way, has been mended: in turn
+    const uint32_t item_full0 = fixed0 + 8 * kKvMends, item_empty0 = item_full0 + 8 * kKvRing, item_fixed0 = item_empty0 + 8 * kKvRing;
+    const uint32_t stats_full = item_fixed0 + 8 * kKvRing, stats_done = stats_full + 8;
+    volatile uint32_t* hidden = reinterpret_cast<volatile uint32_t*>(bars + 2 * SLOTS + 10 + 2 * kKvMends + 3 * kKvRing);    // [ring] V held numbers that are none
+    uint32_t* tmem_slot = const_cast<uint32_t*>(hidden) + kKvRing;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    static_assert(sizeof(KvItem) * kKvRing + 8 * (2 * SLOTS + 10 + 2 * kKvMends + 3 * kKvRing) + 4 * (kKvRing + 2) <= 1024, "items and barriers");
+    // for the start only, in the same place as `stats`: sums of costs, the place within the first item, its request and tile
+    int64_t* s_scan = reinterpret_cast<int64_t*>(stats);
+    int64_t* s_rest = s_scan + kKvThreads / 32;
+    int* s_start = reinterpret_cast<int*>(s_rest + 1);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    ptx::launch_dependents();
+    if (tid == 0) {
+        auto init = [](uint32_t bar, int n, int count) { for (int i = 0; i < n; ++i) ptx::mbar_init(bar + 8 * i, count); };
+        init(kv_full0, 2 * SLOTS, 1);
+        init(s_full0, 2, 1);
+        init(p_full0, 2, 4);                                                 // one arrival per softmax warp of the tile
+        init(o_full0, 2, 1);
+        init(q_full, 2, 1);
+        init(mend0, 2 * kKvMends, 1);
+        init(item_full0, kKvRing, 1);
+        init(item_empty0, kKvRing, 11);                                      // producer, issuer, mender, eight softmax warps
+        init(item_fixed0, kKvRing, 1);
+        init(stats_full, 2, 4);
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::fence_proxy_async_smem();
+        ptx::prefetch_tensormap(&tmQ);
+        ptx::prefetch_tensormap(&tmK);
+        ptx::prefetch_tensormap(&tmV);
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_addr(tmem_slot), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::grid_dependency_wait();
+
+    // ---------------- this CTA's stretch of the axis ----------------
+    const int per = (a.B + kKvThreads - 1) / kKvThreads, b_lo = min(a.B, tid * per), b_hi = min(a.B, b_lo + per);
+    int64_t mine = 0;
+    for (int b = b_lo; b < b_hi; ++b) {
+        int row0, rows, keys;
+        kv_request(a, b, row0, rows, keys, blockIdx.x == 0);
+        mine += kv_cost(a, rows, keys, kv_tiles(a, rows));
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, w);
+        if (lane >= w) upto += v;
+    }
+    if (lane == 31) s_scan[warp] = upto;
+    __syncthreads();
+    int64_t per_head = 0;
+#pragma unroll
+    for (int w = 0; w < kKvThreads / 32; ++w) {
+        if (w < warp) upto += s_scan[w];
+        per_head += s_scan[w];
+    }
+    const int64_t total = per_head * a.Hkv;
+    const int64_t stretch = max((total + gridDim.x - 1) / gridDim.x, (int64_t)a.min_stretch);
+    const int64_t lo = stretch * blockIdx.x, hi = min(total, lo + stretch);
+    const int head_lo = lo < hi ? (int)(lo / per_head) : 0;
+    if (lo < hi) {
+        const int64_t rest = lo - head_lo * per_head;
+        if (rest >= upto - mine && rest < upto) {                            // one thread's requests hold the start
+            int64_t at = upto - mine;
+            for (int b = b_lo; b < b_hi; ++b) {
+                int row0, rows, keys;
+                kv_request(a, b, row0, rows, keys, false);
+                const int n = kv_tiles(a, rows);
+                const int64_t c = kv_cost(a, rows, keys, n);
+                if (rest < at + c) {
+                    int first = 0, last = n - 1;                             // the tile that holds it
+                    while (first < last) {
+                        const int mid = (first + last + 1) / 2;
+                        if (at + kv_cost(a, rows, keys, mid) <= rest) first = mid;
+                        else last = mid - 1;
+                    }
+                    s_start[0] = b;
+                    s_start[1] = first;
+                    *s_rest = rest - at - kv_cost(a, rows, keys, first);
+                    break;
+                }
+                at += c;
+            }
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;                                   // S_t at + 128 t, O_t at + 256 + 128 t
+
+    if (warp < 4) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kKvRegsLight));
+      // the item in ring place i; false when there is no more
+      auto next_item = [&](uint32_t i, KvItem& it) -> bool {
+          if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_full0 + 8 * (i % kKvRing), (i / kKvRing) & 1u, abort_flag, KERNEL_ID, 1, kKvItemWait))) return false;
+          it = items[i % kKvRing];
+          return it.last == 0;
+      };
+      auto item_done = [&](uint32_t i) {
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * (i % kKvRing));
+      };
+      // the first key of the item that some row of it must not see
+      auto first_hidden = [&](const KvItem& it) { return min(max(it.seen0, 0), it.keys); };
+
+      if (warp == 0) {
+        // ---------------- K/V producer ----------------
+        KvCursor<SLOTS> at = {0, 0};
+        uint32_t n_mends = 0;
+        KvItem it;
+        const int boxes = kKvBlock / a.box;
+        const uint32_t box_bytes = (uint32_t)a.box * 128u;
+        const int my = lane % boxes, half = lane / boxes;                    // this lane's box of a block and half of the channels
+        const bool copies = lane < boxes * HALVES;
+        for (uint32_t i = 0; next_item(i, it); ++i) {
+            const int32_t* table = a.table + (int64_t)it.b * a.width;
+            // the page of this lane's box in block j: -1 past the request's end, -2 outside of the cache
+            auto page_of = [&](int j, int& place) -> int {
+                const int key = j * kKvBlock + my * a.box;
+                if (j >= it.blk1 || key >= it.keys) return -1;
+                const int index = key / a.page_size;
+                place = key - index * a.page_size;
+                const int page = table[index];
+                return page >= 0 && page < a.n_pages ? page : -2;
+            };
+            const int open = first_hidden(it) / kKvBlock;                    // blocks before this one need no mending
+            int place_next = 0, page_next = page_of(it.blk0, place_next);
+            bool ok = true;
+            for (int j = it.blk0; j < it.blk1 && ok; ++j) {
+                const int page = page_next, place = place_next;
+                page_next = page_of(j + 1, place_next);                      // asked for a block ahead
+                if (page == -2 && half == 0 && copies) report_index(8);
+                const bool there = page >= 0;
+                const uint32_t bytes = __popc(__ballot_sync(0xFFFFFFFFu, there && copies)) * box_bytes;
+                const int row = (page * a.Hkv + it.head) * a.page_size + place;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(kv_empty0 + 8 * at.slot, at.phase ^ 1u, abort_flag, KERNEL_ID, 2))) { ok = false; break; }
+                    const uint32_t full = kv_full0 + 8 * at.slot, dst = fifo + at.slot * TILE + half * HALF + my * box_bytes;
+                    if (kv == 1 && __any_sync(0xFFFFFFFFu, copies && !there)) {
+                        if (copies && !there) {
+                            uint4* z = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE + half * HALF + my * box_bytes);
+                            for (uint32_t n = 0; n < box_bytes / 16; ++n) z[n] = make_uint4(0, 0, 0, 0);
+                        }
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(full, bytes);
+                    __syncwarp();
+                    if (copies && there) ptx::tma_load_2d(dst, kv == 0 ? &tmK : &tmV, 64 * half, row, full);
+                    if (kv == 1 && j >= open) {
+                        if (lane == 0) ptx::mbar_arrive(mend0 + 8 * (n_mends % kKvMends));
+                        ++n_mends;
+                    }
+                    at.move(1);
+                }
+            }
+            if (!ok) break;
+            item_done(i);
+        }
+        __syncwarp();
+      } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        // (as in gqa_attention.cuh: all lanes run the loop so that the operands are warp-uniform, one lane issues)
+        const bool leader = ptx::elect_one();
+        const uint32_t desc_hi = (uint32_t)(ptx::make_smem_desc_sw128(0, 0, 1024) >> 32);
+        const uint32_t q_lo = (uint32_t)ptx::make_smem_desc_sw128(q_smem, 16, 1024);
+        const uint32_t k_lo_base = (uint32_t)ptx::make_smem_desc_sw128(fifo, 16, 1024);
+        const uint32_t v_lo_base = (uint32_t)ptx::make_smem_desc_sw128(fifo, HALF, 1024);
+        KvCursor<SLOTS> k_at = {0, 0}, v_at = {1, 0};
+        uint32_t p_phase[2] = {0, 0}, q_phase = 0, n_fixed = 0;
+        KvItem it;
+        auto wait_all = [&](uint32_t bar, uint32_t phase, int site) -> bool {
+            const bool ok = __all_sync(0xFFFFFFFFu, wait_bounded(bar, phase, abort_flag, KERNEL_ID, site));
+            ptx::tc_fence_after_sync();
+            return ok;
+        };
+        for (uint32_t i = 0; next_item(i, it); ++i) {
+            const int blocks = it.blk1 - it.blk0;
+            if (blocks == 0) { item_done(i); continue; }
+            const bool big = it.npos > a.tile_pos;
+            const int steps = big ? 2 * blocks : blocks;
+            const int open = first_hidden(it) / kKvBlock;
+            bool ok = wait_all(q_full, q_phase, 3);
+            q_phase ^= 1u;
+            uint32_t k_slot = 0, v_slot = 0;
+            // step n: tile n & 1, block n / 2 (big) or n
+            auto scores = [&](int n) -> bool {
+                const int t = n & 1;
+                if (!big || t == 0) {
+                    if (!wait_all(kv_full0 + 8 * k_at.slot, k_at.phase, 4)) return false;
+                    k_slot = k_at.slot;
+                    k_at.move(2);
+                }
+                const uint32_t a0 = q_lo + (big && t ? TILE >> 4 : 0u), b0 = k_lo_base + k_slot * (TILE >> 4);
+                uint32_t ad[D / 16], bd[D / 16];
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    ad[k] = a0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
+                    bd[k] = b0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
+                }
+                if (leader) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        ptx::umma_bf16_halves(tmem_base + 128u * (uint32_t)t, ad[k], bd[k], desc_hi, kIdescQK, k != 0 ? 1u : 0u);
+                    ptx::umma_commit(s_full0 + 8 * t);
+                    if (!big || t == 1) ptx::umma_commit(kv_empty0 + 8 * k_slot);
+                    if (n == steps - 1) ptx::umma_commit(q_empty);
+                }
+                __syncwarp();
+                return true;
+            };
+            ok = ok && scores(0) && (steps < 2 || scores(1));
+            for (int n = 0; n < steps && ok; ++n) {
+                const int t = n & 1;
+                if (!wait_all(p_full0 + 8 * t, p_phase[t], 5)) { ok = false; break; }
+                p_phase[t] ^= 1u;
+                if (!big || t == 0) {
+                    if (!wait_all(kv_full0 + 8 * v_at.slot, v_at.phase, 6)) { ok = false; break; }
+                    v_slot = v_at.slot;
+                    v_at.move(2);
+                    if (it.blk0 + (big ? n >> 1 : n) >= open) {
+                        if (!wait_all(fixed0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, 7)) { ok = false; break; }
+                        ++n_fixed;
+                    }
+                }
+                // A = P_t from TMEM: 16 keys of a K step are 8 columns of packed pairs; small items: the second terms 64 columns on
+                const uint32_t v0 = v_lo_base + v_slot * (TILE >> 4);
+                const uint32_t d_tmem = tmem_base + 256u + 128u * (uint32_t)t, p_tmem = tmem_base + 128u * (uint32_t)t;
+                uint32_t bd[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) bd[k] = v0 + (uint32_t)(k * 128);
+                if (leader) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        umma_bf16_tmem_a_halves(d_tmem, p_tmem + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, n >= 2 || k != 0 ? 1u : 0u);
+                    if (!big) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            umma_bf16_tmem_a_halves(d_tmem, p_tmem + 64u + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, 1u);
+                    }
+                    ptx::umma_commit(o_full0 + 8 * t);
+                    if (!big || t == 1) ptx::umma_commit(kv_empty0 + 8 * v_slot);
+                }
+                __syncwarp();
+                if (n + 2 < steps) ok = scores(n + 2);
+            }
+            if (!ok) break;
+            item_done(i);
+        }
+        __syncwarp();
+      } else if (warp == 2) {
+        // ---------------- items and Q ----------------
+        KvCut* cuts = reinterpret_cast<KvCut*>(a.workspace);
+        KvCut cut = {};
+        uint32_t i = 0, loads = 0;
+        bool ok = true;
+        if (lo < hi) {
+            int head = head_lo, b = s_start[0], tile = s_start[1], window = -1;
+            int w_row0 = 0, w_rows = 0, w_keys = 0;                          // this lane's request of the window
+            int64_t x = lo - *s_rest;                                        // where the item starts
+            while (ok && x < hi) {
+                if (b >= a.B) { b = 0; ++head; tile = 0; continue; }
+                if (window != b / 32) {
+                    window = b / 32;
+                    if (window * 32 + lane < a.B) kv_request(a, window * 32 + lane, w_row0, w_rows, w_keys, false);
+                    else w_rows = 0;
+                }
+                const int rows = __shfl_sync(0xFFFFFFFFu, w_rows, b & 31), row0 = __shfl_sync(0xFFFFFFFFu, w_row0, b & 31);
+                const int keys = __shfl_sync(0xFFFFFFFFu, w_keys, b & 31);
+                const int pos0 = tile * 2 * a.tile_pos;
+                if (pos0 >= rows) {                                          // on to the next request that has rows
+                    const uint32_t some = __ballot_sync(0xFFFFFFFFu, w_rows > 0) & (0xFFFFFFFEu << (b & 31));
+                    b = some ? window * 32 + __ffs((int)some) - 1 : window * 32 + 32;
+                    tile = 0;
+                    continue;
+                }
+                const int npos = min(2 * a.tile_pos, rows - pos0);
+                const int seen_last = a.causal ? max(keys - rows + pos0 + npos, 0) : keys;
+                const int64_t cost = (int64_t)seen_last + kKvItemCost;
+                const int all = (seen_last + kKvBlock - 1) / kKvBlock;
+                const int64_t from = max(lo - x, (int64_t)0);
+                const int blk0 = kv_blocks_before(from, seen_last), blk1 = kv_blocks_before(min(hi - x, cost), seen_last);
+                if (blk1 > blk0 || (all == 0 && from == 0)) {
+                    const bool whole = blk0 == 0 && blk1 == all;
+                    if (!whole && blk0 == 0) {                               // the first part of a cut item: whose are the others
+                        cut.parts = (int)((x + kKvItemCost + (int64_t)kKvBlock * (all - 1)) / stretch) - (int)blockIdx.x + 1;
+                        cut.head = head;
+                        cut.npos = npos;
+                        cut.row0 = row0 + pos0;
+                        cut.two_tiles = npos > a.tile_pos;
+                    }
+                    const uint32_t p = i % kKvRing;
+                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, KERNEL_ID, 8, kKvItemWait))) { ok = false; break; }
+                    if (lane == 0) {
+                        KvItem it;
+                        it.blk0 = blk0;
+                        it.blk1 = blk1;
+                        it.b = b;
+                        it.head = head;
+                        it.row0 = row0 + pos0;
+                        it.npos = npos;
+                        it.keys = keys;
+                        it.seen0 = a.causal ? keys - rows + pos0 + 1 : keys;
+                        it.slot = whole ? -1 : 2 * (int)blockIdx.x + (blk0 == 0 ? 1 : 0);
+                        it.last = 0;
+                        items[p] = it;
+                        hidden[p] = 0;
+                        ptx::mbar_arrive(item_full0 + 8 * p);
+                    }
+                    __syncwarp();
+                    ++i;
+                    if (blk1 > blk0) {
+                        if (!__all_sync(0xFFFFFFFFu, wait_bounded(q_empty, (loads & 1u) ^ 1u, abort_flag, KERNEL_ID, 9, kKvItemWait))) { ok = false; break; }
+                        ++loads;
+                        if (lane == 0) {
+                            const int tiles = npos > a.tile_pos ? 2 : 1;
+                            ptx::mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * a.q_bytes));
+                            for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                                for (int h = 0; h < HALVES; ++h)
+                                    tma_load_3d(q_smem + t * TILE + h * HALF, &tmQ, 64 * h, head * a.ratio, row0 + pos0 + t * a.tile_pos, q_full);
+                        }
+                        __syncwarp();
+                    }
+                }
+                x += cost;
+                ++tile;
+            }
+        }
+        if (lane == 0) cuts[blockIdx.x] = cut;
+        const uint32_t p = i % kKvRing;
+        if (ok && __all_sync(0xFFFFFFFFu, wait_bounded(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, KERNEL_ID, 10, kKvItemWait))) {
+            if (lane == 0) {
+                items[p].last = 1;
+                ptx::mbar_arrive(item_full0 + 8 * p);
+            }
+        }
+        __syncwarp();
+      } else {
+        // ---------------- V mender ----------------
+        KvCursor<SLOTS> at = {1, 0};
+        uint32_t n_fixed = 0;
+        KvItem it;
+        for (uint32_t i = 0; next_item(i, it); ++i) {
+            const int first = first_hidden(it);
+            const int from = max(it.blk0, first / kKvBlock);
+            at.skip(2u * (uint32_t)max(0, min(from, it.blk1) - it.blk0));
+            bool ok = true, none = false;
+            for (int j = from; j < it.blk1; ++j) {
+                // (the producer has filled the slot anew: before that, its barrier's parity could be that of an older use)
+                if (!__all_sync(0xFFFFFFFFu, wait_bounded(mend0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, abort_flag, KERNEL_ID, 18, kKvItemWait) &&
+                                             wait_bounded(kv_full0 + 8 * at.slot, at.phase, abort_flag, KERNEL_ID, 11))) { ok = false; break; }
+                const int r0 = max(0, first - j * kKvBlock), end = it.keys - j * kKvBlock;       // rows from r0 on; from `end` on none
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    uint4* rows = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE + h * HALF);
+#pragma unroll 8
+                    for (int c = r0 * 8 + lane; c < kKvBlock * 8; c += 32) {
+                        if (c >= end * 8) {
+                            rows[c] = make_uint4(0, 0, 0, 0);
+                            continue;
+                        }
+                        uint4 v = rows[c];
+                        if (bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) || bf16_pair_not_finite(v.w)) {
+                            none = true;
+                            uint32_t* w = &v.x;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if ((w[k] & 0x7F80u) == 0x7F80u) w[k] &= 0xFFFF0000u;
+                                if ((w[k] & 0x7F800000u) == 0x7F800000u) w[k] &= 0x0000FFFFu;
+                            }
+                            rows[c] = v;
+                        }
+                    }
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(fixed0 + 8 * (n_fixed % kKvMends));
+                ++n_fixed;
+                at.move(2);
+            }
+            if (!ok) break;
+            none = __any_sync(0xFFFFFFFFu, none);
+            if (lane == 0) {
+                if (none) hidden[i % kKvRing] = 1;
+                ptx::mbar_arrive(item_fixed0 + 8 * (i % kKvRing));
+            }
+            item_done(i);
+        }
+        __syncwarp();
+      }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kKvRegsSoftmax));
+        // ---------------- softmax and epilogue: one group of four warps per tile, thread = row ----------------
+        const int t = (warp - 4) >> 2;
+        const int r = (warp & 3) * 32 + lane;                                // row within the tile = TMEM lane
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem_base + 128u * (uint32_t)t + lane_addr;
+        const uint32_t o_addr = tmem_base + 256u + lane_addr;                // tile A's; tile B's 128 columns on
+        const int my_pos = r / a.ratio, my_head = r - my_pos * a.ratio;
+        uint32_t s_phase = 0, o_phase = 0, joins = 0;
+        float m_use = -INFINITY, l_run = 0.0f;                               // exponent base, row sum
+        bool ok = true;
+
+        // One step: as in gqa_attention.cuh.  MASKED: some row of the warp must not see some key of the block (no cubic here: it would
+        // make 2^-125 of a masked score).  TWO: probabilities in two bf16 terms.  `bits`: of the block's groups of 16 keys those whose page exists.
+        auto step_pass = [&](auto masked_tag, auto two_tag, bool first, int valid, uint32_t bits, bool mine) {
+            constexpr bool MASKED = decltype(masked_tag)::value, TWO = decltype(two_tag)::value;
+            uint32_t v[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_addr + 32 * c, v[c]);
+            ptx::tmem_ld_wait();
+            if constexpr (MASKED) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (32 * c + i >= valid || !((bits >> (2 * c + i / 16)) & 1u)) v[c][i] = 0xFF800000u;    // -inf
+            }
+            auto exp_pass = [&]() -> float {
+                const float b0 = m_use == -INFINITY ? 0.0f : m_use;
+                const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_base2 = pack_f32x2(-b0, -b0);
+                uint64_t l_acc2 = pack_f32x2(0.0f, 0.0f);
+                auto pair = [&](int c, int i, float& p0, float& p1) {
+                    float e0, e1;
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), scale2, neg_base2), e0, e1);
+                    if (!MASKED && ((GMLP_GQA_POLY_MASK >> (i & 7)) & 1)) {
+                        ex2_poly_x2(e0, e1, p0, p1);
+                    } else {
+                        p0 = ex2_approx(e0);
+                        p1 = ex2_approx(e1);
+                    }
+                    l_acc2 = add_f32x2(l_acc2, pack_f32x2(p0, p1));
+                };
+                if constexpr (TWO) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t top[16], low[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float p0, p1;
+                            pair(c, i, p0, p1);
+                            top[i] = pack_bf16x2(p0, p1);
+                            low[i] = pack_bf16x2(p0 - bf16_lo(top[i]), p1 - bf16_hi(top[i]));
+                        }
+                        tmem_st_32x16(s_addr + 16 * c, top);
+                        tmem_st_32x16(s_addr + 64 + 16 * c, low);
+                    }
+                } else {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        uint32_t packed[32];
+#pragma unroll
+                        for (int ci = 0; ci < 32; ++ci) {
+                            float p0, p1;
+                            pair(2 * hh + (ci >> 4), ci & 15, p0, p1);
+                            packed[ci] = pack_bf16x2(p0, p1);
+                        }
+                        tmem_st_32x32(s_addr + 32 * hh, packed);
+                    }
+                }
+                float l0, l1;
+                unpack_f32x2(l_acc2, l0, l1);
+                return l0 + l1;
+            };
+            // The base moves when a row's sum says that it is far too low, and from -infinity (no key so far, or only scores of
+            // -infinity): the first keys after that may score far below 0.  A row goes by its own sum alone, so that what its neighbours
+            // see (NaN, say) does not change its rounding.
+            float l_blk = 0.0f;
+            bool moved = first;
+            if (!first) {
+                l_blk = exp_pass();
+                moved = !(l_blk <= kGqaLazySum) || m_use == -INFINITY;
+            }
+            if (__any_sync(0xFFFFFFFFu, mine && moved)) {
+                float m_raw = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        m_raw = max3_f32(m_raw, __uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1]));
+                const float m_new = moved ? fmaxf(m_use, m_raw * a.scale_log2) : m_use;      // the scale is positive
+                if (!first && __any_sync(0xFFFFFFFFu, mine && m_new != m_use)) {
+                    // O of the steps so far is complete: this step's scores were issued after their matmuls
+                    const float alpha = m_new == m_use ? 1.0f : ex2_approx(m_use - m_new);
+                    l_run *= alpha;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        ptx::tmem_ld_32x32(o_addr + 128u * (uint32_t)t + c, o);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tmem_st_32x32(o_addr + 128u * (uint32_t)t + c, o);
+                    }
+                }
+                m_use = m_new;
+                l_blk = exp_pass();
+            }
+            l_run += l_blk;
+            tmem_st_wait();
+        };
+
+        for (uint32_t i = 0;; ++i) {
+            const uint32_t ring = i % kKvRing, ring_phase = (i / kKvRing) & 1u;
+            if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_full0 + 8 * ring, ring_phase, abort_flag, KERNEL_ID, 12, kKvItemWait))) break;
+            const KvItem it = items[ring];
+            if (it.last) break;
+            const int blocks = it.blk1 - it.blk0;
+            const bool big = it.npos > a.tile_pos;
+            const int pos = my_pos + (big ? t * a.tile_pos : 0);
+            const bool mine = my_pos < a.tile_pos && pos < it.npos;          // this thread's row exists
+            const bool active = __any_sync(0xFFFFFFFFu, mine);
+            const int seen = mine ? min(max(a.causal ? it.seen0 + pos : it.keys, 0), it.keys) : 0;
+            const int n_steps = big ? blocks : (blocks + 1 - t) / 2;         // of this tile
+            // pages that the cache does not have: looked for once, at the item's start
+            const int32_t* table = a.table + (int64_t)it.b * a.width;
+            bool bad = false;
+            if (active && blocks > 0) {
+                const int p1 = (min(it.keys, it.blk1 * kKvBlock) - 1) / a.page_size;
+                for (int p = it.blk0 * kKvBlock / a.page_size + lane; p <= p1; p += 32) bad |= (uint32_t)table[p] >= (uint32_t)a.n_pages;
+                bad = __any_sync(0xFFFFFFFFu, bad);
+            }
+            m_use = -INFINITY;
+            l_run = 0.0f;
+            for (int n = 0; n < n_steps; ++n) {
+                const int key0 = (it.blk0 + (big ? n : 2 * n + t)) * kKvBlock;
+                // the scores are complete, and with them every matmul issued before them
+                if (!__all_sync(0xFFFFFFFFu, wait_bounded(s_full0 + 8 * t, s_phase, abort_flag, KERNEL_ID, 13))) { ok = false; break; }
+                s_phase ^= 1u;
+                ptx::tc_fence_after_sync();
+                if (active) {
+                    const int valid = max(0, min(kKvBlock, seen - key0));
+                    uint32_t bits = 0xFFu;
+                    if (bad) {
+                        const int key = key0 + 16 * lane;
+                        bool there = true;
+                        if (lane < 8 && key < it.keys) there = (uint32_t)table[key / a.page_size] < (uint32_t)a.n_pages;
+                        bits = __ballot_sync(0xFFFFFFFFu, there) & 0xFFu;
+                    }
+                    const bool masked = __any_sync(0xFFFFFFFFu, mine && valid < kKvBlock) || bits != 0xFFu;
+                    if (big) {
+                        if (masked) step_pass(std::true_type{}, std::false_type{}, n == 0, valid, bits, mine);
+                        else step_pass(std::false_type{}, std::false_type{}, n == 0, valid, bits, mine);
+                    } else {
+                        if (masked) step_pass(std::true_type{}, std::true_type{}, n == 0, valid, bits, mine);
+                        else step_pass(std::false_type{}, std::true_type{}, n == 0, valid, bits, mine);
+                    }
+                }
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * t);
+            }
+            if (!ok) break;
+            o_phase ^= (uint32_t)n_steps & 1u;                               // parity of the next use: one phase per step
+            // a row whose scores were all -infinity (a NaN among them stays)
+            if (m_use == -INFINITY && l_run < 1e-30f) l_run = 0.0f;
+            if (n_steps > 0) {
+                if (!__all_sync(0xFFFFFFFFu, wait_bounded(o_full0 + 8 * t, o_phase ^ 1u, abort_flag, KERNEL_ID, 14))) { ok = false; break; }
+                ptx::tc_fence_after_sync();
+            }
+            bool odd = false;                                                // numbers that are none, taken out of V
+            if (blocks > 0) {
+                if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_fixed0 + 8 * ring, ring_phase, abort_flag, KERNEL_ID, 15, kKvItemWait))) { ok = false; break; }
+                odd = hidden[ring] != 0;
+            }
+
+            // Small items of several blocks: both tiles hold sums of the same rows.  Tile B's warps hand base and weight over, tile A's (which may
+            // read the same lanes of tile B's columns) do the rest.
+            const bool both = !big && blocks > 1;
+            float f_mine = 1.0f, f_other = 0.0f;
+            if (both) {
+                if (t == 1) {
+                    stats[r] = make_float2(m_use, l_run);
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(stats_full);
+                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(stats_done, joins & 1u, abort_flag, KERNEL_ID, 16))) { ok = false; break; }
+                } else {
+                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(stats_full, joins & 1u, abort_flag, KERNEL_ID, 17))) { ok = false; break; }
+                    ptx::tc_fence_after_sync();
+                    const float2 other = stats[r];
+                    const float m_both = fmaxf(m_use, other.x), b0 = m_both == -INFINITY ? 0.0f : m_both;
+                    f_mine = ex2_approx(m_use - b0);
+                    f_other = ex2_approx(other.x - b0);
+                    l_run = l_run * f_mine + other.y * f_other;
+                    m_use = m_both;
+                }
+                ++joins;
+            }
+            if (active && (big || t == 0)) {
+                const int row_in_slot = (big ? 128 * t : 0) + r;
+                const int64_t part = (int64_t)it.slot * a.slot_rows + row_in_slot;
+                float* sums = reinterpret_cast<float*>(a.workspace + kv_ws_sums(gridDim.x, a.slot_rows)) + part * D;
+                bf16* out = a.O + ((int64_t)(it.row0 + pos) * a.Hq + (int64_t)it.head * a.ratio + my_head) * D;
+                const bool zero = l_run == 0.0f;                             // nothing was seen
+                const float inv_l = 1.0f / l_run;
+                if (it.slot >= 0 && mine) reinterpret_cast<float2*>(a.workspace + kv_ws_stats(gridDim.x))[part] = make_float2(m_use, l_run);
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    if (n_steps > 0) {
+                        ptx::tmem_ld_32x32(o_addr + 128u * (uint32_t)t + c, o);
+                        ptx::tmem_ld_wait();
+                    }
+                    if (both) {
+                        uint32_t o1[32];
+                        ptx::tmem_ld_32x32(o_addr + 128u + c, o1);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            o[k] = __float_as_uint(__uint_as_float(o[k]) * f_mine + __uint_as_float(o1[k]) * f_other);
+                    }
+                    if (odd) {
+#pragma unroll 1
+                        for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
+                            const int page = table[j / a.page_size];
+                            if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+                            const bf16* vr = a.v + (((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + c;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                const float x = __bfloat162float(vr[k]);
+                                if (!(x - x == 0.0f)) o[k] = __float_as_uint(__uint_as_float(o[k]) + x);
+                            }
+                        }
+                    }
+                    if (!mine) continue;
+                    if (it.slot < 0) {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            uint32_t pk[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                pk[k] = zero ? 0u : pack_bf16x2(__uint_as_float(o[8 * w + 2 * k]) * inv_l, __uint_as_float(o[8 * w + 2 * k + 1]) * inv_l);
+                            *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < 8; ++w)
+                            *reinterpret_cast<uint4*>(sums + c + 4 * w) = make_uint4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
+                    }
+                }
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                if (both && t == 0) ptx::mbar_arrive(stats_done);
+                ptx::mbar_arrive(item_empty0 + 8 * ring);
+            }
+        }
+    }
+
+    if (*abort_flag) {
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// The parts of cut items, added in order: CTA (c, y) takes a share of the rows of the item that was cut at the end of CTA c's stretch;
+// a warp takes a row at a time.
+constexpr int kKvJoinThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kKvJoinThreads)
+kv_join_kernel(const KvAttnArgs a, int ctas)
 {
     constexpr int C = D / 32;
-    __shared__ float sm[4], sl[4], so[4][D];
-    const int b = blockIdx.z, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    int row0, rows, keys;
-    kv_request(a, b, row0, rows, keys, threadIdx.x == 0);
-    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
-        const int64_t at = ((int64_t)(row0 + r) * a.Hq + h) * D;
-        float q[C], o[C], m = -INFINITY, l = 0.0f;
-        for (int c = 0; c < C; ++c) {
-            q[c] = __bfloat162float(a.Q[at + lane * C + c]);
-            o[c] = 0.0f;
+    const int lane = threadIdx.x & 31, warps = kKvJoinThreads / 32;
+    const KvCut cut = reinterpret_cast<const KvCut*>(a.workspace)[blockIdx.x];
+    if (cut.parts < 2) return;
+    const float2* stats = reinterpret_cast<const float2*>(a.workspace + kv_ws_stats(ctas));
+    const float* sums = reinterpret_cast<const float*>(a.workspace + kv_ws_sums(ctas, a.slot_rows));
+    for (int i = blockIdx.y * warps + (threadIdx.x >> 5); i < cut.npos * a.ratio; i += gridDim.y * warps) {
+        const int pos = i / a.ratio, head = i - pos * a.ratio;
+        const int t = cut.two_tiles && pos >= a.tile_pos ? 1 : 0;
+        const int row = 128 * t + (pos - t * a.tile_pos) * a.ratio + head;
+        auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + p)) * a.slot_rows + row; };
+        float top = -INFINITY;
+        for (int p = lane; p < cut.parts; p += 32) top = fmaxf(top, stats[part(p)].x);
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
+        const float b0 = top == -INFINITY ? 0.0f : top;
+        float o[C], l = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = 0.0f;
+#pragma unroll 4
+        for (int p = 0; p < cut.parts; ++p) {
+            const float2 s = stats[part(p)];
+            const float f = ex2_approx(s.x - b0);
+            l += s.y * f;
+            const float* x = sums + part(p) * D + lane * C;
+            float v[C];
+            if constexpr (C == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
+            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] += v[c] * f;
         }
-        const int seen = a.causal ? min(keys, keys - rows + r + 1) : keys;
-        for (int j = warp; j < seen; j += 4) {
-            const int page = a.table[(int64_t)b * a.width + j / a.page_size];
-            if (page < 0 || page >= a.n_pages) {
-                if (lane == 0) report_index(8);
-                continue;
-            }
-            const int64_t kv = (((int64_t)page * a.Hkv + h / a.ratio) * a.page_size + j % a.page_size) * D + lane * C;
-            float s = 0.0f;
-            for (int c = 0; c < C; ++c) s += q[c] * __bfloat162float(a.k[kv + c]);
-            for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, w);
-            s *= a.scale_log2;
-            const float top = fmaxf(m, s), base = top == -INFINITY ? 0.0f : top;
-            const float f = exp2f(m - base), p = exp2f(s - base);
-            l = l * f + p;
-            for (int c = 0; c < C; ++c) o[c] = o[c] * f + p * __bfloat162float(a.v[kv + c]);
-            m = top;
-        }
-        if (lane == 0) { sm[warp] = m; sl[warp] = l; }
-        for (int c = 0; c < C; ++c) so[warp][lane * C + c] = o[c];
-        __syncthreads();
-        for (int c = threadIdx.x; c < D; c += 128) {
-            float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), num = 0.0f, den = 0.0f;
-            if (top == -INFINITY) top = 0.0f;
-            for (int w = 0; w < 4; ++w) {
-                const float f = exp2f(sm[w] - top);
-                num += f * so[w][c];
-                den += f * sl[w];
-            }
-            a.O[at + c] = __float2bfloat16_rn(den == 0.0f ? 0.0f : num / den);
-        }
-        __syncthreads();
+        const float inv = 1.0f / l;
+        uint32_t pk[C / 2];
+#pragma unroll
+        for (int c = 0; c < C / 2; ++c) pk[c] = l == 0.0f ? 0u : pack_bf16x2(o[2 * c] * inv, o[2 * c + 1] * inv);
+        bf16* out = a.O + ((int64_t)(cut.row0 + pos) * a.Hq + (int64_t)cut.head * a.ratio + head) * D + lane * C;
+        if constexpr (C == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pk[0], pk[1]);
+        else *reinterpret_cast<uint32_t*>(out) = pk[0];
     }
 }
 

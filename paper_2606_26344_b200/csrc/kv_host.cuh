@@ -173,6 +173,37 @@ int check_kv_attention(int64_t B, int64_t T, int Hq, int Hkv, int64_t width, int
     return Hq / Hkv > kKvMaxRatio ? GMLP_ERR_UNSUPPORTED : GMLP_OK;
 }
 
+// Rows of a partial result: a big item's two tiles of 128, or what all rows of the call make.
+int kv_slot_rows(int64_t T, int ratio) { return T * ratio <= 128 ? (int)(T * ratio) : 256; }
+uint64_t kv_attention_workspace(int64_t T, int Hq, int Hkv, int head_dim, int sms) { return gmlp::kv_ws_bytes(sms, kv_slot_rows(T, Hq / Hkv), head_dim); }
+
+bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, int64_t T, int box_heads, int box_rows) {
+    const cuuint64_t gdim[3] = {(cuuint64_t)head_dim, (cuuint64_t)Hq, (cuuint64_t)T};
+    const cuuint64_t gstride[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)head_dim * 2 * Hq};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+    const cuuint32_t estride[3] = {1, 1, 1};
+    return g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), gdim, gstride, box, estride,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, cudaStream_t st) {
+    if (!dev->kv_attr_set[D == 128]) {
+        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
+            return GMLP_ERR_LAUNCH;
+        dev->kv_attr_set[D == 128] = true;
+    }
+    const int ctas = dev->sm_count;
+    int rc = launch_block(gmlp::kv_attention_kernel<D>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmK, tmV, k);
+    if (rc != GMLP_OK) return rc;
+    prof_mark("kv_attention", st);
+    rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)ctas, k.slot_rows > 64 ? 4 : 1), dim3(gmlp::kKvJoinThreads), 0, st, k, ctas);
+    if (rc != GMLP_OK) return rc;
+    prof_mark("kv_join", st);
+    return GMLP_OK;
+}
+
 int kv_attention_impl(const gmlp_kv_attention_args* a) {
     if (a == nullptr) return GMLP_ERR_NULL;
     if (a->struct_bytes != sizeof(gmlp_kv_attention_args) || (a->flags & ~(uint32_t)(GMLP_FLAG_CHECKED | GMLP_KV_CAUSAL)) || a->reserved != 0)
@@ -192,30 +223,43 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     DeviceState* dev = current_device(&rc);
     if (dev == nullptr) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(a->stream);
+    const int ratio = a->n_q_heads / a->cache.n_kv_heads;
+    const uint64_t need = kv_attention_workspace(a->T, a->n_q_heads, a->cache.n_kv_heads, a->cache.head_dim, dev->sm_count);
+    if (a->workspace == nullptr) return GMLP_ERR_NULL;
+    if (a->workspace_bytes < need) return GMLP_ERR_WORKSPACE;
+    claim_workspace(dev, static_cast<const uint8_t*>(a->workspace), need, nullptr, 0);
     gmlp::KvAttnArgs k{};
-    k.Q = static_cast<const bf16*>(a->Q);
     k.O = static_cast<bf16*>(a->O);
-    k.k = static_cast<const bf16*>(a->cache.k);
     k.v = static_cast<const bf16*>(a->cache.v);
     k.table = static_cast<const int32_t*>(a->block_table);
     k.lengths = static_cast<const int32_t*>(a->lengths);
     k.q_start = static_cast<const int32_t*>(a->q_start);
+    k.workspace = static_cast<uint8_t*>(a->workspace);
     k.B = (int)a->B;
     k.T = (int)a->T;
     k.Hq = a->n_q_heads;
     k.Hkv = a->cache.n_kv_heads;
-    k.ratio = k.Hq / k.Hkv;
+    k.ratio = ratio;
     k.width = (int)a->table_width;
     k.page_size = a->cache.page_size;
     k.n_pages = (int)a->cache.n_pages;
     k.q_len = a->q_len;
     k.causal = (a->flags & GMLP_KV_CAUSAL) != 0;
     k.scale_log2 = scale_log2;
+    k.tile_pos = 128 / ratio;
+    k.box = a->cache.page_size & -a->cache.page_size;
+    if (k.box > gmlp::kKvBlock) k.box = gmlp::kKvBlock;
+    const int q_pos = a->T < k.tile_pos ? (int)a->T : k.tile_pos, D = a->cache.head_dim;
+    k.q_bytes = ratio * q_pos * D * 2;
+    k.slot_rows = kv_slot_rows(a->T, ratio);
+    k.min_stretch = 384;
+    const uint64_t cache_rows = (uint64_t)a->cache.n_pages * (uint64_t)k.Hkv * (uint64_t)k.page_size;
+    CUtensorMap tmQ, tmK, tmV;
+    if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
+        !encode_2d(&tmV, a->cache.v, (uint64_t)D, cache_rows, 64, (uint32_t)k.box))
+        return GMLP_ERR_LAUNCH;
     prof_begin(st);
-    const dim3 grid((unsigned)(a->T < 1024 ? a->T : 1024), (unsigned)k.Hq, (unsigned)k.B);
-    rc = a->cache.head_dim == 128 ? launch_block(gmlp::kv_attention_plain_kernel<128>, grid, dim3(128), 0, st, k)
-                                  : launch_block(gmlp::kv_attention_plain_kernel<64>, grid, dim3(128), 0, st, k);
+    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmK, tmV, k, st) : launch_kv_attention<64>(dev, tmQ, tmK, tmV, k, st);
     if (rc != GMLP_OK) return rc;
-    prof_mark("kv_attention", st);
     return finish_checked(dev, a->flags, st);
 }

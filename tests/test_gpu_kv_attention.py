@@ -58,6 +58,10 @@ class Batch:
     def check(self, scale=None, causal=True, only=None):
         O = self.run(scale=scale, causal=causal)
         assert bool((O[self.rows:] == 7.0).all())                        # rows of no request
+        self.check_rows(O, scale, causal, only)
+        return O
+
+    def check_rows(self, O, scale=None, causal=True, only=None):
         at = 0
         for b, (r, n) in enumerate(self.reqs):
             if only is None or b in only:
@@ -67,7 +71,6 @@ class Batch:
                     worst = float(((O[at:at + r].double() - want).abs() / P.attention_bound(want, A, E, self.D, n)).nan_to_num(nan=math.inf).max())
                     assert worst <= 1.0, (b, r, n, worst)
             at += r
-        return O
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -231,7 +234,6 @@ def test_infinite_scores():
 def test_bad_pages_lengths_and_starts_are_left_out_and_reported():
     reqs = [(1, 300), (90, 400), (1, 70), (2, 40)]
     batch = Batch(reqs, 8, 2, 64, 16, behind=0)
-    clean = batch.run().clone()
     holes = {0: [3], 1: [0, 7, 24]}
     for b, pages in holes.items():
         for i, p in enumerate(pages):
@@ -242,7 +244,7 @@ def test_bad_pages_lengths_and_starts_are_left_out_and_reported():
     O = torch.full_like(batch.Q, 7.0)
     gmlp.kv_attention(batch.Q, batch.cache, batch.table, batch.lengths, 8, q_start=batch.start, O=O)
     assert gmlp.device_status() >> 16 == 200
-    assert torch.equal(O[91:], clean[91:])
+    batch.check_rows(O, only=(2, 3))
     at = 0
     for b, pages in holes.items():                                       # the other keys, each with its own place in the mask
         r, n = reqs[b]
@@ -264,7 +266,8 @@ def test_bad_pages_lengths_and_starts_are_left_out_and_reported():
         O = torch.full_like(batch.Q, 7.0)
         gmlp.kv_attention(batch.Q, batch.cache, batch.table, batch.lengths, 8, q_start=batch.start, O=O)
         assert gmlp.device_status() >> 16 == 200
-        assert bool((O[1:91] == 0).all()) and torch.equal(O[:1], clean[:1]) and torch.equal(O[91:], clean[91:])
+        assert bool((O[1:91] == 0).all())
+        batch.check_rows(O, only=(0, 2, 3))                              # (they may be split elsewhere than beside a good length)
     batch.lengths[1] = 400
     for i, bad in ((1, -3), (1, 1 << 30), (2, 95)):                      # starts that fall or pass the rows: those requests' rows are left out
         start = batch.start.clone()
@@ -278,7 +281,7 @@ def test_bad_pages_lengths_and_starts_are_left_out_and_reported():
                 covered = any(0 <= s[c] <= int(batch.start[b]) < s[c + 1] <= batch.Q.shape[0] for c in range(4))
                 assert covered or bool((O[batch.start[b]:batch.start[b + 1]] == 7.0).all())
             elif (s[b], s[b + 1]) == (int(batch.start[b]), int(batch.start[b + 1])):
-                assert torch.equal(O[s[b]:s[b + 1]], clean[s[b]:s[b + 1]])
+                batch.check_rows(O, only=(b,))
 
 
 def test_cache_past_four_gigabytes():

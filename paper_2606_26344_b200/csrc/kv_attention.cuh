@@ -5,7 +5,11 @@
 // tile of a chunk spans few positions.  A work item is up to 2 P positions of one request and key/value head:
 //   big   (more than P positions): two tiles of 128 rows that take turns on the tensor pipe, both over every block of 128 keys;
 //   small (up to P positions):     one tile of rows, the two "tiles" take the even and the odd blocks of keys and are joined at the
-//                                  end.  Bytes bound these, so the probabilities get a second bf16 term (16 bits) for the tensor pipe's spare time.
+//                                  end.  Bytes bound these, so the probabilities get a second bf16 term (16 bits) for the tensor pipe's spare time;
+//   few   (up to 16 rows, e.g. single tokens): the products are turned round, S^T = K Q^T and O^T += V^T P^T, so that the 128 keys
+//                                  of a block, not 16 rows of 128, are the threads' lanes: a block's softmax takes some 16 exponentials a thread
+//                                  instead of 128 (0.4 us instead of 1.9, two terms as well), which leaves the copies as the bound.  The items of a CTA
+//                                  go to the two tiles in turn, so that one's end and the next one's start overlap.
 // Order and split.  All items lie end to end on one axis, heads outermost, an item as long as the keys that its last position sees plus
 // a constant; every CTA (one per SM) takes an equal stretch of the axis, computed by itself from the lengths on the device (the host knows
 // none of them).  So a decode batch of ragged lengths, one long conversation and a prompt's chunk all load the GPU evenly, without a plan
@@ -16,7 +20,7 @@
 //               are zeros in V, which a probability of 0 would not hide if they were NaN
 //   warp 1      MMA issuer:   S_t = Q_t K^T (TMEM columns 128 t), O_t += P_t V (columns 256 + 128 t)
 //   warp 2      walks the axis, hands items to the others through a ring, loads Q
-//   warp 3      mends V blocks that hold keys which some row must not see: rows past the request's end become zeros, numbers that are none
+//   warp 3      looks for pages outside of the cache, and mends V blocks that hold keys which some row must not see: rows past the request's end become zeros, numbers that are none
 //               become 0 and are added by the epilogue for the rows that see them
 //   warps 4..7  softmax and epilogue of tile A, warps 8..11 of tile B: thread = row.  As in gqa_attention.cuh: scores are read once, the base
 //               of the exponentials moves only when a row's sum of a block passes 2^10, P goes back to TMEM over the scores.
@@ -40,21 +44,25 @@ struct KvAttnArgs {
     int B, T, Hq, Hkv, ratio, width, page_size, n_pages, q_len, causal;
     int tile_pos;                    // positions per 128 rows
     int box;                         // keys per TMA box: the largest power of two that divides the page size, at most 128
-    int q_bytes;                     // of one tile's Q boxes
+    int few_pos;                     // positions per 16 rows (0: more than 16 heads share a key/value head)
+    int q_bytes, q_few_bytes;        // of one tile's Q boxes
     int slot_rows;                   // rows of a partial result
     int min_stretch;                 // of a CTA, in keys
     float scale_log2;
 };
 
 constexpr int kKvThreads = 384, kKvBlock = 128, kKvRing = 4;
+constexpr int kKvFew = 16;                       // rows of an item whose products are turned round
 constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
 constexpr int kKvItemCost = 128;                 // of an item's start and end, in keys
 constexpr int kKvRegsLight = 80, kKvRegsSoftmax = 208;
-constexpr long long kKvItemWait = 16 * kWaitLimitCycles;     // waits of an item's length
+constexpr int kKvKernelId = 30;
+constexpr uint32_t kKvWaitLimit = 8;                         // some 20 s: some waits last as long as an item
 __host__ __device__ constexpr int kv_slots(int D) { return D == 128 ? 5 : 10; }
 __host__ __device__ constexpr uint32_t kv_tile_bytes(int D) { return 128u * D * 2; }
-// Q, FIFO; base and weight of rows; items and barriers; alignment
-constexpr uint32_t kv_attn_smem(int D) { return (2 + kv_slots(D)) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
+constexpr uint32_t kKvRegion = 32768;            // of a tile: Q, and in few items P^T behind it
+// the tiles' regions, FIFO; base and weight of rows; what the warps of few items exchange; items and barriers
+constexpr uint32_t kv_attn_smem(int D) { return 2 * kKvRegion + kv_slots(D) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
 
 // Workspace: one descriptor per CTA, then base and weight of the rows of each of its two partial results, then their sums.
 struct KvCut {
@@ -64,6 +72,7 @@ __host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ct
 __host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) { return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255); }
 __host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) { return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4; }
 
+enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
 struct KvItem {
     int blk0, blk1;                  // blocks of keys; none: rows that see no key
     int b, head, row0;               // request, key/value head, row of Q of the first position
@@ -71,7 +80,8 @@ struct KvItem {
     int seen0;                       // keys that the first position sees (may be negative)
     int slot;                        // of the partial result, or -1: the rows' final values
     int last;                        // no more items (this one is none)
-    int pad[6];
+    int mode, tile;                  // kKvBigItem ..; the tile of a few item
+    int pad[4];
 };
 
 // Request b: its first row, rows and keys; what the arrays hold outside of their ranges is left out (and reported by one CTA).
@@ -110,6 +120,28 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, float (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float tmem_ld_32x1(uint32_t taddr) {
+    float r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=f"(r) : "r"(taddr) : "memory");
+    return r;
+}
+// the largest of a warp's values, NaN left out
+__device__ __forceinline__ float redux_max_f32(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
 // Three coordinates: channel, head, position.
 __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap, int x, int y, int z, uint32_t bar) {
     asm volatile(
@@ -117,6 +149,30 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap,
         ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bf16_pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// A bounded wait of a whole warp.  Smaller than wait_bounded (limit in units of 2^32 cycles, reported at the kernel's end): it stands in some
+// thirty places, and the kernel's code has to stay in the instruction cache - at 298 KB, everything inline several times over, each step of
+// a short item cost microseconds.
+// The same number, which the compiler takes for another one each time: conditions on it are not moved out of a loop by doubling the loop.
+__device__ __forceinline__ int opaque(int v) {
+    asm volatile("" : "+r"(v));
+    return v;
+}
+__device__ __forceinline__ uint32_t clock_hi() {
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(t));
+    return t;
+}
+__device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
+    bool ok = ptx::mbar_try_wait(bar, parity);
+    if (!ok) {
+        const uint32_t start = clock_hi();
+#pragma unroll 1
+        while (!(ok = ptx::mbar_try_wait(bar, parity)) && *abort_flag == 0)
+            if (clock_hi() - start > kKvWaitLimit) *abort_flag = site;
+    }
+    return __all_sync(0xFFFFFFFFu, ok);                              // the outcome is the warp's
+}
 
 // A place in the FIFO: slot and the parity of its use.
 template <int SLOTS> struct KvCursor {
@@ -134,37 +190,54 @@ template <int SLOTS> struct KvCursor {
 
 template <int D>
 __global__ void __launch_bounds__(kKvThreads, 1)
-kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQfew, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const KvAttnArgs a)
 {
-    constexpr int KERNEL_ID = 30, SLOTS = kv_slots(D), HALVES = D / 64;
+    constexpr int SLOTS = kv_slots(D), HALVES = D / 64;
     constexpr uint32_t TILE = kv_tile_bytes(D), HALF = 16384;                // 128 rows of 64 channels
     // S = Q K^T: A and B K-major, N = 128 keys;  O += P V: B MN-major, N = D;  M = 128, bf16 in, fp32 accumulate
     constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw_addr = ptx::smem_addr(smem_raw);
-    const uint32_t base = (raw_addr + 1023u) & ~1023u;
-    uint8_t* base_ptr = smem_raw + (base - raw_addr);
-    const uint32_t q_smem = base, fifo = base + 2 * TILE;
-    uint8_t* fifo_ptr = base_ptr + 2 * TILE;
-    float2* stats = reinterpret_cast<float2*>(base_ptr + (2 + SLOTS) * TILE);        // [128]: base and weight of tile B's rows
-    KvItem* items = reinterpret_cast<KvItem*>(base_ptr + (2 + SLOTS) * TILE + 1024); // [ring]
+    // few items: S^T = K Q^T, M = 128 keys, N = 16;  O^T += V^T P^T: A MN-major, B K-major, M = 128 channels
+    constexpr uint32_t kIdescFewQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKvFew >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    constexpr uint32_t kIdescFewPV = kIdescFewQK | (1u << 15);
+    // P^T of a few item behind its Q: two buffers of two terms, each two blocks of 64 keys, 16 rows of 128 B
+    constexpr uint32_t P_BUF = 16384, P_AT = 4096, P_TERM = 4096, P_HALF = 2048;
+
+    // (no static shared memory: this starts the CTA's, whose first kilobyte is the system's)
+    extern __shared__ __align__(1024) uint8_t base_ptr[];
+    const uint32_t base = ptx::smem_addr(base_ptr);
+    if (base & 1023u) {                                                      // the swizzled tiles count on it
+        if (threadIdx.x == 0) report_timeout(kKvKernelId, 0);
+        return;
+    }
+    const uint32_t q_smem = base, fifo = base + 2 * kKvRegion;
+    uint8_t* fifo_ptr = base_ptr + 2 * kKvRegion;
+    uint8_t* tail_ptr = fifo_ptr + SLOTS * TILE;
+    float2* stats = reinterpret_cast<float2*>(tail_ptr);                     // [128]: base and weight of tile B's rows
+    float* exchange = reinterpret_cast<float*>(tail_ptr + 1024);             // [tile][maxima, sums][16 rows][4 warps]
+    KvItem* items = reinterpret_cast<KvItem*>(tail_ptr + 2048);              // [ring]
     uint64_t* bars = reinterpret_cast<uint64_t*>(items + kKvRing);
     const uint32_t kv_full0 = ptx::smem_addr(bars);                          // [slots]
     const uint32_t kv_empty0 = kv_full0 + 8 * SLOTS;                         // [slots]
-    const uint32_t s_full0 = kv_empty0 + 8 * SLOTS;                          // [2] scores of a step are in TMEM
-    const uint32_t p_full0 = s_full0 + 16;                                   // [2] its probabilities are
-    const uint32_t o_full0 = p_full0 + 16;                                   // [2] O += P V of a step is done
-    const uint32_t q_full = o_full0 + 16, q_empty = q_full + 8;
-    const uint32_t mend0 = q_empty + 8, fixed0 = mend0 + 8 * kKvMends;       // a block of V to be mended is on its way, has been mended: in turn
+    // [tile][buffer], the second buffer in few items only:
+    const uint32_t s_full0 = kv_empty0 + 8 * SLOTS;                          // scores of a step are in TMEM
+    const uint32_t p_full0 = s_full0 + 32;                                   // its probabilities are in place
+    const uint32_t o_full0 = p_full0 + 32;                                   // O += P V of a step is done
+    const uint32_t q_full0 = o_full0 + 32, q_empty0 = q_full0 + 16;          // [tile] its region holds Q, is free
+    const uint32_t mend0 = q_empty0 + 16, fixed0 = mend0 + 8 * kKvMends;     // a block of V to be mended is on its way, has been mended: in turn
     const uint32_t item_full0 = fixed0 + 8 * kKvMends, item_empty0 = item_full0 + 8 * kKvRing, item_fixed0 = item_empty0 + 8 * kKvRing;
-    const uint32_t stats_full = item_fixed0 + 8 * kKvRing, stats_done = stats_full + 8;
-    volatile uint32_t* hidden = reinterpret_cast<volatile uint32_t*>(bars + 2 * SLOTS + 10 + 2 * kKvMends + 3 * kKvRing);    // [ring] V held numbers that are none
-    uint32_t* tmem_slot = const_cast<uint32_t*>(hidden) + kKvRing;
+    const uint32_t item_checked0 = item_fixed0 + 8 * kKvRing;
+    const uint32_t stats_full = item_checked0 + 8 * kKvRing, stats_done = stats_full + 8;
+    const uint32_t agree0 = stats_done + 8;                                  // [tile] the warps of a few item's tile
+    constexpr int BARS = 2 * SLOTS + 20 + 2 * kKvMends + 4 * kKvRing;
+    volatile uint32_t* hidden = reinterpret_cast<volatile uint32_t*>(bars + BARS);   // [ring] V held numbers that are none
+    volatile uint32_t* odd_pages = hidden + kKvRing;                         // [ring] the table has pages outside of the cache
+    volatile uint32_t* votes = odd_pages + kKvRing;                          // [tile][parity][4 warps]
+    uint32_t* tmem_slot = const_cast<uint32_t*>(votes) + 16;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert(sizeof(KvItem) * kKvRing + 8 * (2 * SLOTS + 10 + 2 * kKvMends + 3 * kKvRing) + 4 * (kKvRing + 2) <= 1024, "items and barriers");
+    static_assert(sizeof(KvItem) * kKvRing + 8 * BARS + 4 * (2 * kKvRing + 18) <= 1024, "items and barriers");
     // for the start only, in the same place as `stats`: sums of costs, the place within the first item, its request and tile
     int64_t* s_scan = reinterpret_cast<int64_t*>(stats);
     int64_t* s_rest = s_scan + kKvThreads / 32;
@@ -176,19 +249,21 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     if (tid == 0) {
         auto init = [](uint32_t bar, int n, int count) { for (int i = 0; i < n; ++i) ptx::mbar_init(bar + 8 * i, count); };
         init(kv_full0, 2 * SLOTS, 1);
-        init(s_full0, 2, 1);
-        init(p_full0, 2, 4);                                                 // one arrival per softmax warp of the tile
-        init(o_full0, 2, 1);
-        init(q_full, 2, 1);
+        init(s_full0, 4, 1);
+        init(p_full0, 4, 4);                                                 // one arrival per softmax warp of the tile
+        init(o_full0, 4, 1);
+        init(q_full0, 4, 1);
         init(mend0, 2 * kKvMends, 1);
         init(item_full0, kKvRing, 1);
         init(item_empty0, kKvRing, 11);                                      // producer, issuer, mender, eight softmax warps
         init(item_fixed0, kKvRing, 1);
-        init(stats_full, 2, 4);
+        init(item_checked0, kKvRing, 1);
+        init(stats_full, 4, 4);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::fence_proxy_async_smem();
         ptx::prefetch_tensormap(&tmQ);
+        ptx::prefetch_tensormap(&tmQfew);
         ptx::prefetch_tensormap(&tmK);
         ptx::prefetch_tensormap(&tmV);
     }
@@ -258,7 +333,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kKvRegsLight));
       // the item in ring place i; false when there is no more
       auto next_item = [&](uint32_t i, KvItem& it) -> bool {
-          if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_full0 + 8 * (i % kKvRing), (i / kKvRing) & 1u, abort_flag, KERNEL_ID, 1, kKvItemWait))) return false;
+          if (!kv_wait(item_full0 + 8 * (i % kKvRing), (i / kKvRing) & 1u, abort_flag, 1)) return false;
           it = items[i % kKvRing];
           return it.last == 0;
       };
@@ -292,6 +367,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int open = first_hidden(it) / kKvBlock;                    // blocks before this one need no mending
             int place_next = 0, page_next = page_of(it.blk0, place_next);
             bool ok = true;
+#pragma unroll 1
             for (int j = it.blk0; j < it.blk1 && ok; ++j) {
                 const int page = page_next, place = place_next;
                 page_next = page_of(j + 1, place_next);                      // asked for a block ahead
@@ -301,10 +377,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const int row = (page * a.Hkv + it.head) * a.page_size + place;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
-                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(kv_empty0 + 8 * at.slot, at.phase ^ 1u, abort_flag, KERNEL_ID, 2))) { ok = false; break; }
+                    if (!kv_wait(kv_empty0 + 8 * at.slot, at.phase ^ 1u, abort_flag, 2)) { ok = false; break; }
                     const uint32_t full = kv_full0 + 8 * at.slot, dst = fifo + at.slot * TILE + half * HALF + my * box_bytes;
-                    if (kv == 1 && __any_sync(0xFFFFFFFFu, copies && !there)) {
-                        if (copies && !there) {
+                    if (kv == 1 && __any_sync(0xFFFFFFFFu, copies && page == -2)) {      // (past the end: the mender's)
+                        if (copies && page == -2) {
                             uint4* z = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE + half * HALF + my * box_bytes);
                             for (uint32_t n = 0; n < box_bytes / 16; ++n) z[n] = make_uint4(0, 0, 0, 0);
                         }
@@ -333,83 +409,180 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const uint32_t q_lo = (uint32_t)ptx::make_smem_desc_sw128(q_smem, 16, 1024);
         const uint32_t k_lo_base = (uint32_t)ptx::make_smem_desc_sw128(fifo, 16, 1024);
         const uint32_t v_lo_base = (uint32_t)ptx::make_smem_desc_sw128(fifo, HALF, 1024);
+        const uint32_t p_lo = (uint32_t)ptx::make_smem_desc_sw128(q_smem + P_AT, 16, 1024);
+        // V as the A operand of few items: 128 channels.  With D = 64 rows 64.. of O^T are never read: their atom may lie anywhere
+        const uint32_t v_few_base = (uint32_t)ptx::make_smem_desc_sw128(fifo, D == 128 ? HALF : 1024, 1024);
         KvCursor<SLOTS> k_at = {0, 0}, v_at = {1, 0};
-        uint32_t p_phase[2] = {0, 0}, q_phase = 0, n_fixed = 0;
+        uint32_t p_phase = 0, q_phase = 0, n_fixed = 0;                      // bits: [tile][buffer]; [tile]
         KvItem it;
         auto wait_all = [&](uint32_t bar, uint32_t phase, int site) -> bool {
-            const bool ok = __all_sync(0xFFFFFFFFu, wait_bounded(bar, phase, abort_flag, KERNEL_ID, site));
+            const bool ok = kv_wait(bar, phase, abort_flag, site);
             ptx::tc_fence_after_sync();
+            return ok;
+        };
+        auto wait_q = [&](int t) -> bool {
+            const bool ok = wait_all(q_full0 + 8 * t, (q_phase >> t) & 1u, 3);
+            q_phase ^= 1u << t;
+            return ok;
+        };
+        // the next block's keys, its values (mended where they hold keys that some row must not see)
+        auto wait_k = [&](uint32_t& slot) -> bool {
+            if (!wait_all(kv_full0 + 8 * k_at.slot, k_at.phase, 4)) return false;
+            slot = k_at.slot;
+            k_at.move(2);
+            return true;
+        };
+        auto wait_v = [&](uint32_t& slot, bool mended) -> bool {
+            if (!wait_all(kv_full0 + 8 * v_at.slot, v_at.phase, 6)) return false;
+            slot = v_at.slot;
+            v_at.move(2);
+            if (!mended) return true;
+            const bool ok = wait_all(fixed0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, 7);
+            ++n_fixed;
+            return ok;
+        };
+        auto wait_p = [&](int at) -> bool {
+            const bool ok = wait_all(p_full0 + 8 * at, (p_phase >> at) & 1u, 5);
+            p_phase ^= 1u << at;
             return ok;
         };
         for (uint32_t i = 0; next_item(i, it); ++i) {
             const int blocks = it.blk1 - it.blk0;
             if (blocks == 0) { item_done(i); continue; }
-            const bool big = it.npos > a.tile_pos;
-            const int steps = big ? 2 * blocks : blocks;
-            const int open = first_hidden(it) / kKvBlock;
-            bool ok = wait_all(q_full, q_phase, 3);
-            q_phase ^= 1u;
+            const bool big = it.mode == kKvBigItem;
+            const int open = first_hidden(it) / kKvBlock - it.blk0;          // blocks of the item before this one need no mending
             uint32_t k_slot = 0, v_slot = 0;
-            // step n: tile n & 1, block n / 2 (big) or n
-            auto scores = [&](int n) -> bool {
-                const int t = n & 1;
-                if (!big || t == 0) {
-                    if (!wait_all(kv_full0 + 8 * k_at.slot, k_at.phase, 4)) return false;
-                    k_slot = k_at.slot;
-                    k_at.move(2);
+            bool ok;
+            if (it.mode == kKvFewItem) {
+                const int t = it.tile;
+                const uint32_t q0 = q_lo + (uint32_t)t * (kKvRegion >> 4), p0 = p_lo + (uint32_t)t * (kKvRegion >> 4);
+                auto scores = [&](int n) -> bool {
+                    if (!wait_k(k_slot)) return false;
+                    const uint32_t a0 = k_lo_base + k_slot * (TILE >> 4);
+                    uint32_t ad[D / 16], bd[D / 16];
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        ad[k] = a0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
+                        bd[k] = q0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
+                    }
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            ptx::umma_bf16_halves(tmem_base + 128u * (uint32_t)t + (uint32_t)(kKvFew * (n & 1)), ad[k], bd[k], desc_hi, kIdescFewQK, k != 0 ? 1u : 0u);
+                        ptx::umma_commit(s_full0 + 8 * (2 * t + (n & 1)));
+                        ptx::umma_commit(kv_empty0 + 8 * k_slot);
+                    }
+                    __syncwarp();
+                    return true;
+                };
+                // S(0), S(1), P V(0), S(2), P V(1), ... (one place in the code for each)
+                ok = wait_q(t);
+#pragma unroll 1
+                for (int m = 0; m < blocks + 2 && ok; ++m) {
+                  if (m >= 2) {
+                    const int n = m - 2;
+                    if (!wait_p(2 * t + (n & 1)) || !wait_v(v_slot, n >= open)) { ok = false; break; }
+                    const uint32_t a0 = v_few_base + v_slot * (TILE >> 4), b0 = p0 + (uint32_t)(n & 1) * (P_BUF >> 4);
+                    uint32_t ad[8], bd[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        ad[k] = a0 + (uint32_t)(k * 128);
+                        bd[k] = b0 + (uint32_t)((k >> 2) * (P_HALF >> 4) + (k & 3) * 2);
+                    }
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)                         // both terms
+                            ptx::umma_bf16_halves(tmem_base + 256u + 128u * (uint32_t)t, ad[k & 7], bd[k & 7] + (k >= 8 ? P_TERM >> 4 : 0u), desc_hi,
+                                                  kIdescFewPV, n != 0 || k != 0 ? 1u : 0u);
+                        ptx::umma_commit(o_full0 + 8 * (2 * t + (n & 1)));
+                        ptx::umma_commit(kv_empty0 + 8 * v_slot);
+                        if (n == blocks - 1) ptx::umma_commit(q_empty0 + 8 * t);         // P lies in the region too
+                    }
+                    __syncwarp();
+                  }
+                  if (m < blocks) ok = scores(m);
                 }
-                const uint32_t a0 = q_lo + (big && t ? TILE >> 4 : 0u), b0 = k_lo_base + k_slot * (TILE >> 4);
+                if (!ok) break;
+                item_done(i);
+                continue;
+            }
+            // S_t = Q K^T with the block in k_slot; O_t += P_t V with that in v_slot: A = P_t from TMEM, 16 keys of a K step are 8 columns of
+            // packed pairs, the second terms of small items 64 columns on
+            auto scores = [&](int t, uint32_t q0, bool free_k) {
+                const uint32_t b0 = k_lo_base + k_slot * (TILE >> 4);
                 uint32_t ad[D / 16], bd[D / 16];
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    ad[k] = a0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
+                    ad[k] = q0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
                     bd[k] = b0 + (uint32_t)((k >> 2) * (HALF >> 4) + (k & 3) * 2);
                 }
                 if (leader) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
                         ptx::umma_bf16_halves(tmem_base + 128u * (uint32_t)t, ad[k], bd[k], desc_hi, kIdescQK, k != 0 ? 1u : 0u);
-                    ptx::umma_commit(s_full0 + 8 * t);
-                    if (!big || t == 1) ptx::umma_commit(kv_empty0 + 8 * k_slot);
-                    if (n == steps - 1) ptx::umma_commit(q_empty);
+                    ptx::umma_commit(s_full0 + 16 * t);
+                    if (free_k) ptx::umma_commit(kv_empty0 + 8 * k_slot);
                 }
                 __syncwarp();
-                return true;
             };
-            ok = ok && scores(0) && (steps < 2 || scores(1));
-            for (int n = 0; n < steps && ok; ++n) {
-                const int t = n & 1;
-                if (!wait_all(p_full0 + 8 * t, p_phase[t], 5)) { ok = false; break; }
-                p_phase[t] ^= 1u;
-                if (!big || t == 0) {
-                    if (!wait_all(kv_full0 + 8 * v_at.slot, v_at.phase, 6)) { ok = false; break; }
-                    v_slot = v_at.slot;
-                    v_at.move(2);
-                    if (it.blk0 + (big ? n >> 1 : n) >= open) {
-                        if (!wait_all(fixed0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, 7)) { ok = false; break; }
-                        ++n_fixed;
-                    }
-                }
-                // A = P_t from TMEM: 16 keys of a K step are 8 columns of packed pairs; small items: the second terms 64 columns on
+            auto values = [&](int t, bool more, bool two, bool free_v) {
                 const uint32_t v0 = v_lo_base + v_slot * (TILE >> 4);
                 const uint32_t d_tmem = tmem_base + 256u + 128u * (uint32_t)t, p_tmem = tmem_base + 128u * (uint32_t)t;
                 uint32_t bd[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) bd[k] = v0 + (uint32_t)(k * 128);
                 if (leader) {
+                    umma_bf16_tmem_a_halves(d_tmem, p_tmem, bd[0], desc_hi, kIdescPV, more ? 1u : 0u);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        umma_bf16_tmem_a_halves(d_tmem, p_tmem + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, n >= 2 || k != 0 ? 1u : 0u);
-                    if (!big) {
+                    for (int k = 1; k < 8; ++k) umma_bf16_tmem_a_halves(d_tmem, p_tmem + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, 1u);
+                    if (two) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            umma_bf16_tmem_a_halves(d_tmem, p_tmem + 64u + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, 1u);
+                        for (int k = 0; k < 8; ++k) umma_bf16_tmem_a_halves(d_tmem, p_tmem + 64u + 8u * (uint32_t)k, bd[k], desc_hi, kIdescPV, 1u);
                     }
-                    ptx::umma_commit(o_full0 + 8 * t);
-                    if (!big || t == 1) ptx::umma_commit(kv_empty0 + 8 * v_slot);
+                    ptx::umma_commit(o_full0 + 16 * t);
+                    if (free_v) ptx::umma_commit(kv_empty0 + 8 * v_slot);
                 }
                 __syncwarp();
-                if (n + 2 < steps) ok = scores(n + 2);
+            };
+            if (big) {
+                // both tiles over each block: S_A(0), S_B(0), then P_A V(j), S_A(j + 1), P_B V(j), S_B(j + 1)
+                ok = wait_q(0) && wait_q(1);
+#pragma unroll 1
+                for (int j = -1; j < blocks && ok; ++j) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (j >= 0) {
+                            if (!wait_p(2 * t) || (t == 0 && !wait_v(v_slot, j >= open))) { ok = false; break; }
+                            values(t, j > 0, false, t == 1);
+                        }
+                        if (j + 1 < blocks) {
+                            if (t == 0 && !wait_k(k_slot)) { ok = false; break; }
+                            scores(t, q_lo + (uint32_t)t * (kKvRegion >> 4), t == 1);
+                        }
+                    }
+                }
+                if (leader) {
+                    ptx::umma_commit(q_empty0);
+                    ptx::umma_commit(q_empty0 + 8);
+                }
+                __syncwarp();
+            } else {
+                // block n to tile n & 1: S(0), S(1), P V(0), S(2), P V(1), ...
+                ok = wait_q(0);
+#pragma unroll 1
+                for (int m = 0; m < blocks + 2 && ok; ++m) {
+                    const int t = m & 1;
+                    if (m >= 2) {
+                        if (!wait_p(2 * t) || !wait_v(v_slot, m - 2 >= open)) { ok = false; break; }
+                        values(t, m >= 4, true, true);
+                    }
+                    if (m < blocks) {
+                        if (!wait_k(k_slot)) { ok = false; break; }
+                        scores(t, q_lo, true);
+                    }
+                }
+                if (leader) ptx::umma_commit(q_empty0);
+                __syncwarp();
             }
             if (!ok) break;
             item_done(i);
@@ -419,7 +592,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         // ---------------- items and Q ----------------
         KvCut* cuts = reinterpret_cast<KvCut*>(a.workspace);
         KvCut cut = {};
-        uint32_t i = 0, loads = 0;
+        uint32_t i = 0, loads = 0, few_items = 0;                            // loads: bits, parity of [tile]'s
         bool ok = true;
         if (lo < hi) {
             int head = head_lo, b = s_start[0], tile = s_start[1], window = -1;
@@ -456,8 +629,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         cut.row0 = row0 + pos0;
                         cut.two_tiles = npos > a.tile_pos;
                     }
+                    const int mode = npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem);
+                    const int tile_of = mode == kKvFewItem ? (int)(few_items & 1u) : 0;
                     const uint32_t p = i % kKvRing;
-                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, KERNEL_ID, 8, kKvItemWait))) { ok = false; break; }
+                    if (!kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 8)) { ok = false; break; }
                     if (lane == 0) {
                         KvItem it;
                         it.blk0 = blk0;
@@ -470,25 +645,30 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         it.seen0 = a.causal ? keys - rows + pos0 + 1 : keys;
                         it.slot = whole ? -1 : 2 * (int)blockIdx.x + (blk0 == 0 ? 1 : 0);
                         it.last = 0;
+                        it.mode = mode;
+                        it.tile = tile_of;
                         items[p] = it;
                         hidden[p] = 0;
                         ptx::mbar_arrive(item_full0 + 8 * p);
                     }
                     __syncwarp();
                     ++i;
-                    if (blk1 > blk0) {
-                        if (!__all_sync(0xFFFFFFFFu, wait_bounded(q_empty, (loads & 1u) ^ 1u, abort_flag, KERNEL_ID, 9, kKvItemWait))) { ok = false; break; }
-                        ++loads;
+                    if (mode == kKvFewItem) ++few_items;
+                    for (int t = tile_of; ok && blk1 > blk0 && t < (mode == kKvBigItem ? 2 : tile_of + 1); ++t) {
+                        if (!kv_wait(q_empty0 + 8 * t, ((loads >> t) & 1u) ^ 1u, abort_flag, 9)) { ok = false; break; }
+                        loads ^= 1u << t;
                         if (lane == 0) {
-                            const int tiles = npos > a.tile_pos ? 2 : 1;
-                            ptx::mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * a.q_bytes));
-                            for (int t = 0; t < tiles; ++t)
+                            const bool few = mode == kKvFewItem;
+                            const uint32_t full = q_full0 + 8 * t;
+                            ptx::mbar_arrive_expect_tx(full, (uint32_t)(few ? a.q_few_bytes : a.q_bytes));
 #pragma unroll
-                                for (int h = 0; h < HALVES; ++h)
-                                    tma_load_3d(q_smem + t * TILE + h * HALF, &tmQ, 64 * h, head * a.ratio, row0 + pos0 + t * a.tile_pos, q_full);
+                            for (int h = 0; h < HALVES; ++h)
+                                tma_load_3d(q_smem + t * kKvRegion + h * HALF, few ? &tmQfew : &tmQ, 64 * h, head * a.ratio,
+                                            row0 + pos0 + (few ? 0 : t * a.tile_pos), full);
                         }
                         __syncwarp();
                     }
+                    if (!ok) break;
                 }
                 x += cost;
                 ++tile;
@@ -496,7 +676,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         if (lane == 0) cuts[blockIdx.x] = cut;
         const uint32_t p = i % kKvRing;
-        if (ok && __all_sync(0xFFFFFFFFu, wait_bounded(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, KERNEL_ID, 10, kKvItemWait))) {
+        if (ok && kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 10)) {
             if (lane == 0) {
                 items[p].last = 1;
                 ptx::mbar_arrive(item_full0 + 8 * p);
@@ -509,26 +689,37 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         uint32_t n_fixed = 0;
         KvItem it;
         for (uint32_t i = 0; next_item(i, it); ++i) {
+            bool pages = false;                                              // some outside of the cache
+            if (it.blk1 > it.blk0) {
+                const int32_t* table = a.table + (int64_t)it.b * a.width;
+                const int p1 = (min(it.keys, it.blk1 * kKvBlock) - 1) / a.page_size;
+#pragma unroll 4
+                for (int p = it.blk0 * kKvBlock / a.page_size + lane; p <= p1; p += 32) pages |= (uint32_t)table[p] >= (uint32_t)a.n_pages;
+                pages = __any_sync(0xFFFFFFFFu, pages);
+            }
+            if (lane == 0) {
+                odd_pages[i % kKvRing] = pages;
+                ptx::mbar_arrive(item_checked0 + 8 * (i % kKvRing));
+            }
             const int first = first_hidden(it);
             const int from = max(it.blk0, first / kKvBlock);
             at.skip(2u * (uint32_t)max(0, min(from, it.blk1) - it.blk0));
             bool ok = true, none = false;
+#pragma unroll 1
             for (int j = from; j < it.blk1; ++j) {
                 // (the producer has filled the slot anew: before that, its barrier's parity could be that of an older use)
-                if (!__all_sync(0xFFFFFFFFu, wait_bounded(mend0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, abort_flag, KERNEL_ID, 18, kKvItemWait) &&
-                                             wait_bounded(kv_full0 + 8 * at.slot, at.phase, abort_flag, KERNEL_ID, 11))) { ok = false; break; }
+                if (!kv_wait(mend0 + 8 * (n_fixed % kKvMends), (n_fixed / kKvMends) & 1u, abort_flag, 18) ||
+                    !kv_wait(kv_full0 + 8 * at.slot, at.phase, abort_flag, 11)) { ok = false; break; }
                 const int r0 = max(0, first - j * kKvBlock), end = it.keys - j * kKvBlock;       // rows from r0 on; from `end` on none
+                uint4* rows = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE);               // [half][key][16 B]
+#pragma unroll 1
+                for (int c = r0 * 8 + lane; c < kKvBlock * 8; c += 32) {
 #pragma unroll
-                for (int h = 0; h < HALVES; ++h) {
-                    uint4* rows = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE + h * HALF);
-#pragma unroll 8
-                    for (int c = r0 * 8 + lane; c < kKvBlock * 8; c += 32) {
-                        if (c >= end * 8) {
-                            rows[c] = make_uint4(0, 0, 0, 0);
-                            continue;
-                        }
-                        uint4 v = rows[c];
-                        if (bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) || bf16_pair_not_finite(v.w)) {
+                    for (int h = 0; h < HALVES; ++h) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (c < end * 8) {
+                            v = rows[h * 1024 + c];
+                            if (!(bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) || bf16_pair_not_finite(v.w))) continue;
                             none = true;
                             uint32_t* w = &v.x;
 #pragma unroll
@@ -536,8 +727,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                                 if ((w[k] & 0x7F80u) == 0x7F80u) w[k] &= 0xFFFF0000u;
                                 if ((w[k] & 0x7F800000u) == 0x7F800000u) w[k] &= 0x0000FFFFu;
                             }
-                            rows[c] = v;
                         }
+                        rows[h * 1024 + c] = v;
                     }
                 }
                 ptx::fence_proxy_async_smem();
@@ -565,170 +756,349 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const uint32_t s_addr = tmem_base + 128u * (uint32_t)t + lane_addr;
         const uint32_t o_addr = tmem_base + 256u + lane_addr;                // tile A's; tile B's 128 columns on
         const int my_pos = r / a.ratio, my_head = r - my_pos * a.ratio;
-        uint32_t s_phase = 0, o_phase = 0, joins = 0;
+        uint32_t s_phase = 0, o_phase = 0, joins = 0, agreed = 0;           // bits: [buffer]
         float m_use = -INFINITY, l_run = 0.0f;                               // exponent base, row sum
         bool ok = true;
 
-        // One step: as in gqa_attention.cuh.  MASKED: some row of the warp must not see some key of the block (no cubic here: it would
-        // make 2^-125 of a masked score).  TWO: probabilities in two bf16 terms.  `bits`: of the block's groups of 16 keys those whose page exists.
-        auto step_pass = [&](auto masked_tag, auto two_tag, bool first, int valid, uint32_t bits, bool mine) {
-            constexpr bool MASKED = decltype(masked_tag)::value, TWO = decltype(two_tag)::value;
+        // One step: as in gqa_attention.cuh.  `valid`: keys of the block that the row sees, `bits`: of the block's groups of 16 keys those whose
+        // page exists; `two`: probabilities in two bf16 terms.  (A masked score is -infinity and the cubic makes 2^-125 of it, not 0: next to nothing
+        // beside a key that counts, and a row that has none is told by its base.)
+        auto step_pass = [&](bool first, int valid, uint32_t bits, bool masked, bool two, bool mine) {
             uint32_t v[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_addr + 32 * c, v[c]);
             ptx::tmem_ld_wait();
-            if constexpr (MASKED) {
+            if (masked) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (32 * c + i >= valid || !((bits >> (2 * c + i / 16)) & 1u)) v[c][i] = 0xFF800000u;    // -inf
             }
-            auto exp_pass = [&]() -> float {
+            // The base moves when a row's sum says that it is far too low, and from -infinity (no key so far, or only scores of
+            // -infinity): the first keys after that may score far below 0.  A row goes by its own sum alone, so that what its neighbours
+            // see (NaN, say) does not change its rounding.
+            bool moved = first, again = first;
+            float l_blk;
+#pragma unroll 1
+            for (;;) {
+                if (again) {
+                    float m_raw = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            m_raw = max3_f32(m_raw, __uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1]));
+                    const float m_new = moved ? fmaxf(m_use, m_raw * a.scale_log2) : m_use;      // the scale is positive
+                    if (!first && __any_sync(0xFFFFFFFFu, mine && m_new != m_use)) {
+                        // O of the steps so far is complete: this step's scores were issued after their matmuls
+                        const float alpha = m_new == m_use ? 1.0f : ex2_approx(m_use - m_new);
+                        l_run *= alpha;
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            float o[16];
+                            uint32_t w[16];
+                            tmem_ld_32x16(o_addr + 128u * (uint32_t)t + c, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * alpha);
+                            tmem_st_32x16(o_addr + 128u * (uint32_t)t + c, w);
+                        }
+                    }
+                    m_use = m_new;
+                }
                 const float b0 = m_use == -INFINITY ? 0.0f : m_use;
                 const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_base2 = pack_f32x2(-b0, -b0);
                 uint64_t l_acc2 = pack_f32x2(0.0f, 0.0f);
-                auto pair = [&](int c, int i, float& p0, float& p1) {
-                    float e0, e1;
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), scale2, neg_base2), e0, e1);
-                    if (!MASKED && ((GMLP_GQA_POLY_MASK >> (i & 7)) & 1)) {
-                        ex2_poly_x2(e0, e1, p0, p1);
-                    } else {
-                        p0 = ex2_approx(e0);
-                        p1 = ex2_approx(e1);
-                    }
-                    l_acc2 = add_f32x2(l_acc2, pack_f32x2(p0, p1));
-                };
-                if constexpr (TWO) {
+                float e_top = -INFINITY;                                     // of those that take the cubic, which is none above 2^127
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t top[16], low[16];
+                for (int c = 0; c < 8; ++c) {                                // 16 keys
+                    float p[16];
+                    uint32_t top[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float p0, p1;
-                            pair(c, i, p0, p1);
-                            top[i] = pack_bf16x2(p0, p1);
-                            low[i] = pack_bf16x2(p0 - bf16_lo(top[i]), p1 - bf16_hi(top[i]));
+                    for (int i = 0; i < 8; ++i) {
+                        float e0, e1;
+                        const uint32_t* x = &v[c >> 1][16 * (c & 1) + 2 * i];
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), scale2, neg_base2), e0, e1);
+                        if ((GMLP_GQA_POLY_MASK >> i) & 1) {
+                            ex2_poly_x2(e0, e1, p[2 * i], p[2 * i + 1]);
+                            e_top = max3_f32(e_top, e0, e1);
+                        } else {
+                            p[2 * i] = ex2_approx(e0);
+                            p[2 * i + 1] = ex2_approx(e1);
                         }
-                        tmem_st_32x16(s_addr + 16 * c, top);
-                        tmem_st_32x16(s_addr + 64 + 16 * c, low);
+                        l_acc2 = add_f32x2(l_acc2, pack_f32x2(p[2 * i], p[2 * i + 1]));
+                        top[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
                     }
-                } else {
+                    tmem_st_32x8(s_addr + 8 * c, top);
+                    if (opaque(two)) {
 #pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        uint32_t packed[32];
-#pragma unroll
-                        for (int ci = 0; ci < 32; ++ci) {
-                            float p0, p1;
-                            pair(2 * hh + (ci >> 4), ci & 15, p0, p1);
-                            packed[ci] = pack_bf16x2(p0, p1);
-                        }
-                        tmem_st_32x32(s_addr + 32 * hh, packed);
+                        for (int i = 0; i < 8; ++i) top[i] = pack_bf16x2(p[2 * i] - bf16_lo(top[i]), p[2 * i + 1] - bf16_hi(top[i]));
+                        tmem_st_32x8(s_addr + 64 + 8 * c, top);
                     }
                 }
                 float l0, l1;
                 unpack_f32x2(l_acc2, l0, l1);
-                return l0 + l1;
-            };
-            // The base moves when a row's sum says that it is far too low, and from -infinity (no key so far, or only scores of
-            // -infinity): the first keys after that may score far below 0.  A row goes by its own sum alone, so that what its neighbours
-            // see (NaN, say) does not change its rounding.
-            float l_blk = 0.0f;
-            bool moved = first;
-            if (!first) {
-                l_blk = exp_pass();
-                moved = !(l_blk <= kGqaLazySum) || m_use == -INFINITY;
-            }
-            if (__any_sync(0xFFFFFFFFu, mine && moved)) {
-                float m_raw = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        m_raw = max3_f32(m_raw, __uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1]));
-                const float m_new = moved ? fmaxf(m_use, m_raw * a.scale_log2) : m_use;      // the scale is positive
-                if (!first && __any_sync(0xFFFFFFFFu, mine && m_new != m_use)) {
-                    // O of the steps so far is complete: this step's scores were issued after their matmuls
-                    const float alpha = m_new == m_use ? 1.0f : ex2_approx(m_use - m_new);
-                    l_run *= alpha;
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t o[32];
-                        ptx::tmem_ld_32x32(o_addr + 128u * (uint32_t)t + c, o);
-                        ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                        tmem_st_32x32(o_addr + 128u * (uint32_t)t + c, o);
-                    }
-                }
-                m_use = m_new;
-                l_blk = exp_pass();
+                l_blk = l0 + l1;
+                if (again) break;
+                moved = !(l_blk <= kGqaLazySum) || e_top > 126.0f || m_use == -INFINITY;
+                again = __any_sync(0xFFFFFFFFu, mine && moved);
+                if (!again) break;
             }
             l_run += l_blk;
             tmem_st_wait();
         };
 
+        // A few item: lane = key in a block's scores, channel in its output; the four warps agree on the base of the exponentials.
+        auto few_item = [&](const KvItem& it, const int32_t* table, bool bad, uint32_t ring, uint32_t ring_phase) -> bool {
+            const int blocks = it.blk1 - it.blk0, rows = it.npos * a.ratio;
+            // every row's part, row by row in registers, four rows at a time: those that the item does not have are not run
+            auto each_row = [&](auto part) {
+#pragma unroll
+                for (int g = 0; g < kKvFew; g += 4) {
+                    if (g < opaque(rows)) {
+#pragma unroll
+                        for (int n = g; n < g + 4; ++n) part(n);
+                    }
+                }
+            };
+            const int first = min(max(it.seen0, 0), it.keys);                // the first key that some row must not see
+            float m[kKvFew], l[kKvFew];
+            int seen[kKvFew];                                                // keys that row n sees
+            {
+                int pos = 0, next = a.ratio;
+#pragma unroll
+                for (int n = 0; n < kKvFew; ++n) {
+                    if (n == next) { ++pos; next += a.ratio; }
+                    m[n] = -INFINITY;
+                    l[n] = 0.0f;
+                    seen[n] = a.causal ? min(max(it.seen0 + pos, 0), it.keys) : it.keys;
+                }
+            }
+            const uint32_t q4 = (uint32_t)(warp & 3);
+            float* maxima = exchange + t * 128;                              // [16][4]
+            float* weights = maxima + 64;
+            auto agree = [&]() -> bool {                                     // what the four warps wrote before it they read after it
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(agree0 + 8 * t);
+                const bool ok = kv_wait(agree0 + 8 * t, agreed & 1u, abort_flag, 20);
+                agreed ^= 1u;
+                return ok;
+            };
+            const uint32_t p_at = q_smem + t * kKvRegion + P_AT + (uint32_t)(r >> 6) * P_HALF + (uint32_t)(r & 7) * 2u;
+            const uint32_t chunk = (uint32_t)(r & 63) >> 3;
+#pragma unroll 1
+            for (int j = 0; j < blocks; ++j) {
+                const uint32_t buf = (uint32_t)j & 1u;
+                const int key = (it.blk0 + j) * kKvBlock + r;
+                if (!kv_wait(s_full0 + 8 * (2 * t + buf), (s_phase >> buf) & 1u, abort_flag, 13)) return false;
+                s_phase ^= 1u << buf;
+                ptx::tc_fence_after_sync();
+                float x[kKvFew];
+                tmem_ld_32x16(s_addr + kKvFew * buf, x);
+                ptx::tmem_ld_wait();
+                ptx::tc_fence_before_sync();
+                if (opaque(bad) || (it.blk0 + j + 1) * kKvBlock > first) {
+                    const bool there = key < it.keys && (!bad || (uint32_t)table[key / a.page_size] < (uint32_t)a.n_pages);
+                    each_row([&](int n) {
+                        if (!there || key >= seen[n]) x[n] = -INFINITY;
+                    });
+                }
+                // the base of a row moves when a score passes it by 8 (a factor of 256), and from -infinity
+                const bool begins = opaque(j) == 0;
+                bool moves = begins;
+                if (!begins) {
+                    bool over = false;
+                    each_row([&](int n) {
+                        if (n < rows) over |= fmaf(x[n], a.scale_log2, m[n] == -INFINITY ? INFINITY : -m[n]) > 8.0f;
+                    });
+                    over = __any_sync(0xFFFFFFFFu, over);
+                    volatile uint32_t* v = votes + t * 8 + (agreed & 1u) * 4;
+                    if (lane == 0) v[q4] = over;
+                    if (!agree()) return false;
+                    moves = (v[0] | v[1] | v[2] | v[3]) != 0;
+                }
+                if (moves) {
+                    float mine = -INFINITY;
+                    each_row([&](int n) {
+                        const float top = redux_max_f32(x[n]);
+                        if (lane == n) mine = top;
+                    });
+                    if (lane < kKvFew) maxima[lane * 4 + q4] = mine;
+                    if (!agree()) return false;
+                    float f[kKvFew];
+                    bool any = false;
+                    each_row([&](int n) {
+                        const float4 w = *reinterpret_cast<const float4*>(maxima + 4 * n);
+                        const float top = fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)) * a.scale_log2;
+                        const bool moved = top > m[n] + 8.0f || m[n] == -INFINITY;
+                        f[n] = moved && top > m[n] ? ex2_approx(m[n] - top) : 1.0f;
+                        any |= f[n] != 1.0f && n < rows;
+                        if (moved) m[n] = fmaxf(m[n], top);
+                        l[n] *= f[n];
+                    });
+                    if (any && !begins) {                                      // the same for all four warps
+                        if (!kv_wait(o_full0 + 8 * (2 * t + (buf ^ 1u)), ((o_phase >> (buf ^ 1u)) & 1u) ^ 1u, abort_flag, 21)) return false;
+                        ptx::tc_fence_after_sync();
+                        float o[kKvFew];
+                        tmem_ld_32x16(o_addr + 128u * (uint32_t)t, o);
+                        ptx::tmem_ld_wait();
+                        uint32_t ow[kKvFew];
+                        each_row([&](int n) { ow[n] = __float_as_uint(o[n] * f[n]); });
+                        tmem_st_32x16(o_addr + 128u * (uint32_t)t, ow);
+                        tmem_st_wait();
+                        ptx::tc_fence_before_sync();
+                    }
+                }
+                // P of two steps ago has been read
+                if (j >= 2 && !kv_wait(o_full0 + 8 * (2 * t + buf), ((o_phase >> buf) & 1u) ^ 1u, abort_flag, 22)) return false;
+                o_phase ^= 1u << buf;                                        // parity of this buffer's next use
+                const uint32_t to = p_at + buf * P_BUF;
+                each_row([&](int n) {
+                    const float p = ex2_approx(fmaf(x[n], a.scale_log2, m[n] == -INFINITY ? 0.0f : -m[n]));
+                    l[n] += p;
+                    const bf16 top = __float2bfloat16_rn(p);
+                    const bf16 low = __float2bfloat16_rn(p - __bfloat162float(top));
+                    const uint32_t place = to + (uint32_t)n * 128u + ((chunk ^ (uint32_t)(n & 7)) << 4);
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(place), "h"(__bfloat16_as_ushort(top)) : "memory");
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(place + P_TERM), "h"(__bfloat16_as_ushort(low)) : "memory");
+                });
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * (2 * t + buf));
+            }
+            bool odd = false;
+            if (blocks > 0) {
+                // the rows' weights, summed over the warp's keys: at each exchange a lane keeps half of its rows, in the end row lane / 2
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) {
+                    const bool up = lane & (2 * w);
+#pragma unroll
+                    for (int n = 0; n < w; ++n) {
+                        const float keep = up ? l[n + w] : l[n], give = up ? l[n] : l[n + w];
+                        l[n] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, 2 * w);
+                    }
+                }
+                l[0] += __shfl_xor_sync(0xFFFFFFFFu, l[0], 1);
+                if ((lane & 1) == 0) weights[(lane >> 1) * 4 + q4] = l[0];
+                if (!agree()) return false;
+                const uint32_t buf = (uint32_t)(blocks - 1) & 1u;
+                if (!kv_wait(o_full0 + 8 * (2 * t + buf), ((o_phase >> buf) & 1u) ^ 1u, abort_flag, 14)) return false;
+                ptx::tc_fence_after_sync();
+                if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) return false;
+                odd = hidden[ring] != 0;
+            }
+            const bool whole = it.slot < 0;
+            const int64_t part = (int64_t)it.slot * a.slot_rows;
+            float* sums = reinterpret_cast<float*>(a.workspace + kv_ws_sums(gridDim.x, a.slot_rows)) + part * D + r;
+            bf16* out = a.O + ((int64_t)it.row0 * a.Hq + (int64_t)it.head * a.ratio) * D + r;
+            if (!whole && q4 == 0 && lane < kKvFew) {
+                float base_n = m[0];
+#pragma unroll
+                for (int n = 1; n < kKvFew; ++n)
+                    if (lane == n) base_n = m[n];
+                const float4 w = *reinterpret_cast<const float4*>(weights + 4 * lane);
+                if (lane < rows)
+                    (reinterpret_cast<float2*>(a.workspace + kv_ws_stats(gridDim.x)) + part)[lane] = make_float2(base_n, (w.x + w.y) + (w.z + w.w));
+            }
+            int pos = 0, head = 0;
+#pragma unroll 1
+            for (int n = 0; n < rows; ++n) {
+                float o = blocks > 0 ? tmem_ld_32x1(o_addr + 128u * (uint32_t)t + (uint32_t)n) : 0.0f;
+                const float4 w = *reinterpret_cast<const float4*>(weights + 4 * n);
+                const float sum = blocks > 0 ? (w.x + w.y) + (w.z + w.w) : 0.0f;             // 0: nothing was seen
+                ptx::tmem_ld_wait();
+                if (odd && r < D) {
+                    const int end = min(a.causal ? min(max(it.seen0 + pos, 0), it.keys) : it.keys, it.blk1 * kKvBlock);
+#pragma unroll 1
+                    for (int j = max(first, it.blk0 * kKvBlock); j < end; ++j) {
+                        const int page = table[j / a.page_size];
+                        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+                        const float v = __bfloat162float(a.v[(((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + r]);
+                        if (!(v - v == 0.0f)) o += v;
+                    }
+                }
+                if (r < D) {
+                    if (whole) *out = __float2bfloat16_rn(sum == 0.0f ? 0.0f : __fdividef(o, sum));
+                    else *sums = o;
+                }
+                out += D;
+                sums += D;
+                if (++head == a.ratio) {
+                    head = 0;
+                    ++pos;
+                    out += (int64_t)(a.Hq - a.ratio) * D;
+                }
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * ring);
+            return true;
+        };
+
         for (uint32_t i = 0;; ++i) {
             const uint32_t ring = i % kKvRing, ring_phase = (i / kKvRing) & 1u;
-            if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_full0 + 8 * ring, ring_phase, abort_flag, KERNEL_ID, 12, kKvItemWait))) break;
-            const KvItem it = items[ring];
+            if (!kv_wait(item_full0 + 8 * ring, ring_phase, abort_flag, 12)) break;
+            const KvItem& it = items[ring];                                  // stays until this warp lets it go
             if (it.last) break;
             const int blocks = it.blk1 - it.blk0;
-            const bool big = it.npos > a.tile_pos;
+            const bool big = it.mode == kKvBigItem;
+            const int32_t* table = a.table + (int64_t)it.b * a.width;
+            bool bad = false;                                                // pages that the cache does not have
+            if (it.mode == kKvFewItem && it.tile != t) {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * ring);
+                continue;
+            }
+            if (blocks > 0) {
+                if (!kv_wait(item_checked0 + 8 * ring, ring_phase, abort_flag, 19)) break;
+                bad = odd_pages[ring] != 0;
+            }
+            if (it.mode == kKvFewItem) {
+                if (!few_item(it, table, bad, ring, ring_phase)) break;
+                continue;
+            }
             const int pos = my_pos + (big ? t * a.tile_pos : 0);
             const bool mine = my_pos < a.tile_pos && pos < it.npos;          // this thread's row exists
             const bool active = __any_sync(0xFFFFFFFFu, mine);
             const int seen = mine ? min(max(a.causal ? it.seen0 + pos : it.keys, 0), it.keys) : 0;
             const int n_steps = big ? blocks : (blocks + 1 - t) / 2;         // of this tile
-            // pages that the cache does not have: looked for once, at the item's start
-            const int32_t* table = a.table + (int64_t)it.b * a.width;
-            bool bad = false;
-            if (active && blocks > 0) {
-                const int p1 = (min(it.keys, it.blk1 * kKvBlock) - 1) / a.page_size;
-                for (int p = it.blk0 * kKvBlock / a.page_size + lane; p <= p1; p += 32) bad |= (uint32_t)table[p] >= (uint32_t)a.n_pages;
-                bad = __any_sync(0xFFFFFFFFu, bad);
-            }
             m_use = -INFINITY;
             l_run = 0.0f;
+#pragma unroll 1
             for (int n = 0; n < n_steps; ++n) {
-                const int key0 = (it.blk0 + (big ? n : 2 * n + t)) * kKvBlock;
+                const int key0 = (it.blk0 + (opaque(big) ? n : 2 * n + t)) * kKvBlock;
                 // the scores are complete, and with them every matmul issued before them
-                if (!__all_sync(0xFFFFFFFFu, wait_bounded(s_full0 + 8 * t, s_phase, abort_flag, KERNEL_ID, 13))) { ok = false; break; }
+                if (!kv_wait(s_full0 + 16 * t, s_phase & 1u, abort_flag, 13)) { ok = false; break; }
                 s_phase ^= 1u;
                 ptx::tc_fence_after_sync();
-                if (active) {
+                if (opaque(active)) {
                     const int valid = max(0, min(kKvBlock, seen - key0));
                     uint32_t bits = 0xFFu;
-                    if (bad) {
+                    if (opaque(bad)) {
                         const int key = key0 + 16 * lane;
                         bool there = true;
                         if (lane < 8 && key < it.keys) there = (uint32_t)table[key / a.page_size] < (uint32_t)a.n_pages;
                         bits = __ballot_sync(0xFFFFFFFFu, there) & 0xFFu;
                     }
                     const bool masked = __any_sync(0xFFFFFFFFu, mine && valid < kKvBlock) || bits != 0xFFu;
-                    if (big) {
-                        if (masked) step_pass(std::true_type{}, std::false_type{}, n == 0, valid, bits, mine);
-                        else step_pass(std::false_type{}, std::false_type{}, n == 0, valid, bits, mine);
-                    } else {
-                        if (masked) step_pass(std::true_type{}, std::true_type{}, n == 0, valid, bits, mine);
-                        else step_pass(std::false_type{}, std::true_type{}, n == 0, valid, bits, mine);
-                    }
+                    step_pass(opaque(n) == 0, valid, bits, opaque(masked), opaque(!big), mine);
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * t);
+                if (lane == 0) ptx::mbar_arrive(p_full0 + 16 * t);
             }
             if (!ok) break;
             o_phase ^= (uint32_t)n_steps & 1u;                               // parity of the next use: one phase per step
             // a row whose scores were all -infinity (a NaN among them stays)
             if (m_use == -INFINITY && l_run < 1e-30f) l_run = 0.0f;
             if (n_steps > 0) {
-                if (!__all_sync(0xFFFFFFFFu, wait_bounded(o_full0 + 8 * t, o_phase ^ 1u, abort_flag, KERNEL_ID, 14))) { ok = false; break; }
+                if (!kv_wait(o_full0 + 16 * t, (o_phase & 1u) ^ 1u, abort_flag, 14)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
             }
             bool odd = false;                                                // numbers that are none, taken out of V
             if (blocks > 0) {
-                if (!__all_sync(0xFFFFFFFFu, wait_bounded(item_fixed0 + 8 * ring, ring_phase, abort_flag, KERNEL_ID, 15, kKvItemWait))) { ok = false; break; }
+                if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) { ok = false; break; }
                 odd = hidden[ring] != 0;
             }
 
@@ -742,9 +1112,9 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     ptx::tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(stats_full);
-                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(stats_done, joins & 1u, abort_flag, KERNEL_ID, 16))) { ok = false; break; }
+                    if (!kv_wait(stats_done, joins & 1u, abort_flag, 16)) { ok = false; break; }
                 } else {
-                    if (!__all_sync(0xFFFFFFFFu, wait_bounded(stats_full, joins & 1u, abort_flag, KERNEL_ID, 17))) { ok = false; break; }
+                    if (!kv_wait(stats_full, joins & 1u, abort_flag, 17)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
                     const float2 other = stats[r];
                     const float m_both = fmaxf(m_use, other.x), b0 = m_both == -INFINITY ? 0.0f : m_both;
@@ -764,47 +1134,44 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const float inv_l = 1.0f / l_run;
                 if (it.slot >= 0 && mine) reinterpret_cast<float2*>(a.workspace + kv_ws_stats(gridDim.x))[part] = make_float2(m_use, l_run);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
-                    if (n_steps > 0) {
-                        ptx::tmem_ld_32x32(o_addr + 128u * (uint32_t)t + c, o);
-                        ptx::tmem_ld_wait();
-                    }
-                    if (both) {
-                        uint32_t o1[32];
-                        ptx::tmem_ld_32x32(o_addr + 128u + c, o1);
+                for (int c = 0; c < D; c += 16) {
+                    float o[16];
+                    if (opaque(n_steps) > 0) tmem_ld_32x16(o_addr + 128u * (uint32_t)t + c, o);
+                    if (opaque(both)) {
+                        float o1[16];
+                        tmem_ld_32x16(o_addr + 128u + c, o1);
                         ptx::tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            o[k] = __float_as_uint(__uint_as_float(o[k]) * f_mine + __uint_as_float(o1[k]) * f_other);
+                        for (int k = 0; k < 16; ++k) o[k] = o[k] * f_mine + o1[k] * f_other;
+                    } else {
+                        ptx::tmem_ld_wait();
                     }
-                    if (odd) {
+                    if (opaque(odd)) {
 #pragma unroll 1
                         for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
                             const int page = table[j / a.page_size];
                             if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
                             const bf16* vr = a.v + (((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + c;
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) {
+                            for (int k = 0; k < 16; ++k) {
                                 const float x = __bfloat162float(vr[k]);
-                                if (!(x - x == 0.0f)) o[k] = __float_as_uint(__uint_as_float(o[k]) + x);
+                                if (!(x - x == 0.0f)) o[k] += x;
                             }
                         }
                     }
                     if (!mine) continue;
-                    if (it.slot < 0) {
+                    if (opaque(it.slot) < 0) {
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
+                        for (int w = 0; w < 2; ++w) {
                             uint32_t pk[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                pk[k] = zero ? 0u : pack_bf16x2(__uint_as_float(o[8 * w + 2 * k]) * inv_l, __uint_as_float(o[8 * w + 2 * k + 1]) * inv_l);
+                            for (int k = 0; k < 4; ++k) pk[k] = zero ? 0u : pack_bf16x2(o[8 * w + 2 * k] * inv_l, o[8 * w + 2 * k + 1] * inv_l);
                             *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
                         }
                     } else {
 #pragma unroll
-                        for (int w = 0; w < 8; ++w)
-                            *reinterpret_cast<uint4*>(sums + c + 4 * w) = make_uint4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
+                        for (int w = 0; w < 4; ++w)
+                            *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
                     }
                 }
             }
@@ -818,6 +1185,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
 
     if (*abort_flag) {
+        if (lane == 0) report_timeout(kKvKernelId, *abort_flag);
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
     ptx::tc_fence_before_sync();

@@ -188,14 +188,14 @@ bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, in
 }
 
 template <int D>
-int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, cudaStream_t st) {
+int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, cudaStream_t st) {
     if (!dev->kv_attr_set[D == 128]) {
         if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
         dev->kv_attr_set[D == 128] = true;
     }
     const int ctas = dev->sm_count;
-    int rc = launch_block(gmlp::kv_attention_kernel<D>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmK, tmV, k);
+    int rc = launch_block(gmlp::kv_attention_kernel<D>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
     rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)ctas, k.slot_rows > 64 ? 4 : 1), dim3(gmlp::kKvJoinThreads), 0, st, k, ctas);
@@ -250,16 +250,19 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     k.box = a->cache.page_size & -a->cache.page_size;
     if (k.box > gmlp::kKvBlock) k.box = gmlp::kKvBlock;
     const int q_pos = a->T < k.tile_pos ? (int)a->T : k.tile_pos, D = a->cache.head_dim;
+    k.few_pos = gmlp::kKvFew / ratio;                                        // 0: none
+    const int few_pos = k.few_pos == 0 ? q_pos : (a->T < k.few_pos ? (int)a->T : k.few_pos);
     k.q_bytes = ratio * q_pos * D * 2;
+    k.q_few_bytes = ratio * few_pos * D * 2;
     k.slot_rows = kv_slot_rows(a->T, ratio);
     k.min_stretch = 384;
     const uint64_t cache_rows = (uint64_t)a->cache.n_pages * (uint64_t)k.Hkv * (uint64_t)k.page_size;
-    CUtensorMap tmQ, tmK, tmV;
-    if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
+    CUtensorMap tmQ, tmQfew, tmK, tmV;
+    if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_kv_query(&tmQfew, a->Q, D, k.Hq, a->T, ratio, few_pos) || !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
         !encode_2d(&tmV, a->cache.v, (uint64_t)D, cache_rows, 64, (uint32_t)k.box))
         return GMLP_ERR_LAUNCH;
     prof_begin(st);
-    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmK, tmV, k, st) : launch_kv_attention<64>(dev, tmQ, tmK, tmV, k, st);
+    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmQfew, tmK, tmV, k, st) : launch_kv_attention<64>(dev, tmQ, tmQfew, tmK, tmV, k, st);
     if (rc != GMLP_OK) return rc;
     return finish_checked(dev, a->flags, st);
 }

@@ -54,8 +54,10 @@ struct KvAttnArgs {
 constexpr int kKvThreads = 384, kKvBlock = 128, kKvRing = 4;
 constexpr int kKvFew = 16;                       // rows of an item whose products are turned round
 constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
-constexpr int kKvItemCost = 128;                 // of an item's start and end, in keys
-constexpr int kKvRegsLight = 80, kKvRegsSoftmax = 208;
+// An item's start and end, in keys of its length on the axis (a prompt of 8192: 641 us with 64 for all, 560 with 256, 510 with 512 for big
+// ones; prompts with D = 64: 252, 223, 228).
+constexpr int kKvBigCost = 448, kKvSmallCost = 384, kKvFewCost = 256;
+constexpr int kKvRegsLight = 72, kKvRegsSoftmax = 216;
 constexpr int kKvKernelId = 30;
 constexpr uint32_t kKvWaitLimit = 8;                         // some 20 s: some waits last as long as an item
 __host__ __device__ constexpr int kv_slots(int D) { return D == 128 ? 5 : 10; }
@@ -72,7 +74,6 @@ __host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ct
 __host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) { return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255); }
 __host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) { return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4; }
 
-enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
 struct KvItem {
     int blk0, blk1;                  // blocks of keys; none: rows that see no key
     int b, head, row0;               // request, key/value head, row of Q of the first position
@@ -95,21 +96,25 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
     if (!fits) keys = 0;
     if (report && (!ok || !fits)) report_index(ok ? 6 : 7);
 }
-// Length on the axis of the first n of a request's tiles.
-__device__ __forceinline__ int64_t kv_cost(const KvAttnArgs& a, int rows, int keys, int n) {
-    const int s = 2 * a.tile_pos;
-    const int64_t start = (int64_t)n * kKvItemCost;
-    if (n == 0) return 0;
-    if (!a.causal) return start + (int64_t)n * keys;
-    const bool whole = (int64_t)n * s >= rows;                      // the last tile ends with the request
-    const int m = whole ? n - 1 : n, first = keys - rows;           // the others see first + (i + 1) s keys
-    const int none = first < 0 ? min(m, -first / s) : 0;
-    return start + (int64_t)(m - none) * first + (int64_t)s * ((int64_t)m * (m + 1) - (int64_t)none * (none + 1)) / 2 + (whole && n > 0 ? keys : 0);
-}
+enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
+__device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) { return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem); }
+__device__ __forceinline__ int kv_start(int mode) { return mode == kKvBigItem ? kKvBigCost : (mode == kKvSmallItem ? kKvSmallCost : kKvFewCost); }
 __device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int rows) { return (rows + 2 * a.tile_pos - 1) / (2 * a.tile_pos); }
+// Length on the axis of the first n of a request's tiles; all but the last are big.
+__device__ __forceinline__ int64_t kv_cost(const KvAttnArgs& a, int rows, int keys, int n) {
+    if (n == 0) return 0;
+    const int s = 2 * a.tile_pos;
+    const bool whole = (int64_t)n * s >= rows;                      // the last tile ends with the request
+    const int m = whole ? n - 1 : n;
+    int64_t cost = (int64_t)m * kKvBigCost + (whole ? kv_start(kv_mode(a, rows - m * s)) + keys : 0);
+    if (!a.causal) return cost + (int64_t)m * keys;
+    const int first = keys - rows;                                  // tile i of the others sees first + (i + 1) s keys
+    const int none = first < 0 ? min(m, -first / s) : 0;
+    return cost + (int64_t)(m - none) * first + (int64_t)s * ((int64_t)m * (m + 1) - (int64_t)none * (none + 1)) / 2;
+}
 // Blocks of an item of `keys` keys that lie before place x of it.
-__device__ __forceinline__ int kv_blocks_before(int64_t x, int keys) {
-    const int64_t n = x <= kKvItemCost ? 0 : (x - kKvItemCost + kKvBlock - 1) / kKvBlock;
+__device__ __forceinline__ int kv_blocks_before(int64_t x, int start, int keys) {
+    const int64_t n = x <= start ? 0 : (x - start + kKvBlock - 1) / kKvBlock;
     return (int)min(n, (int64_t)((keys + kKvBlock - 1) / kKvBlock));
 }
 
@@ -560,12 +565,14 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                             scores(t, q_lo + (uint32_t)t * (kKvRegion >> 4), t == 1);
                         }
                     }
+                    if (j + 2 == blocks) {                                   // Q has been used
+                        if (leader) {
+                            ptx::umma_commit(q_empty0);
+                            ptx::umma_commit(q_empty0 + 8);
+                        }
+                        __syncwarp();
+                    }
                 }
-                if (leader) {
-                    ptx::umma_commit(q_empty0);
-                    ptx::umma_commit(q_empty0 + 8);
-                }
-                __syncwarp();
             } else {
                 // block n to tile n & 1: S(0), S(1), P V(0), S(2), P V(1), ...
                 ok = wait_q(0);
@@ -579,10 +586,12 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (m < blocks) {
                         if (!wait_k(k_slot)) { ok = false; break; }
                         scores(t, q_lo, true);
+                        if (m == blocks - 1) {
+                            if (leader) ptx::umma_commit(q_empty0);
+                            __syncwarp();
+                        }
                     }
                 }
-                if (leader) ptx::umma_commit(q_empty0);
-                __syncwarp();
             }
             if (!ok) break;
             item_done(i);
@@ -616,20 +625,20 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 }
                 const int npos = min(2 * a.tile_pos, rows - pos0);
                 const int seen_last = a.causal ? max(keys - rows + pos0 + npos, 0) : keys;
-                const int64_t cost = (int64_t)seen_last + kKvItemCost;
+                const int mode = kv_mode(a, npos), start = kv_start(mode);
+                const int64_t cost = (int64_t)seen_last + start;
                 const int all = (seen_last + kKvBlock - 1) / kKvBlock;
                 const int64_t from = max(lo - x, (int64_t)0);
-                const int blk0 = kv_blocks_before(from, seen_last), blk1 = kv_blocks_before(min(hi - x, cost), seen_last);
+                const int blk0 = kv_blocks_before(from, start, seen_last), blk1 = kv_blocks_before(min(hi - x, cost), start, seen_last);
                 if (blk1 > blk0 || (all == 0 && from == 0)) {
                     const bool whole = blk0 == 0 && blk1 == all;
                     if (!whole && blk0 == 0) {                               // the first part of a cut item: whose are the others
-                        cut.parts = (int)((x + kKvItemCost + (int64_t)kKvBlock * (all - 1)) / stretch) - (int)blockIdx.x + 1;
+                        cut.parts = (int)((x + start + (int64_t)kKvBlock * (all - 1)) / stretch) - (int)blockIdx.x + 1;
                         cut.head = head;
                         cut.npos = npos;
                         cut.row0 = row0 + pos0;
                         cut.two_tiles = npos > a.tile_pos;
                     }
-                    const int mode = npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem);
                     const int tile_of = mode == kKvFewItem ? (int)(few_items & 1u) : 0;
                     const uint32_t p = i % kKvRing;
                     if (!kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 8)) { ok = false; break; }
@@ -755,15 +764,18 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem_base + 128u * (uint32_t)t + lane_addr;
         const uint32_t o_addr = tmem_base + 256u + lane_addr;                // tile A's; tile B's 128 columns on
-        const int my_pos = r / a.ratio, my_head = r - my_pos * a.ratio;
+        const int my_pos = r / a.ratio;
         uint32_t s_phase = 0, o_phase = 0, joins = 0, agreed = 0;           // bits: [buffer]
         float m_use = -INFINITY, l_run = 0.0f;                               // exponent base, row sum
         bool ok = true;
 
         // One step: as in gqa_attention.cuh.  `valid`: keys of the block that the row sees, `bits`: of the block's groups of 16 keys those whose
-        // page exists; `two`: probabilities in two bf16 terms.  (A masked score is -infinity and the cubic makes 2^-125 of it, not 0: next to nothing
-        // beside a key that counts, and a row that has none is told by its base.)
-        auto step_pass = [&](bool first, int valid, uint32_t bits, bool masked, bool two, bool mine) {
+        // page exists; TWO: probabilities in two bf16 terms (small items).
+        // (All exponentials take the special-function unit: with a quarter of them as a cubic, which pays in gqa_attention.cuh, a prompt of 8192
+        // without a mask took 924 us instead of 880: here the step's length counts, not the unit.)
+        auto step_pass = [&](auto two_tag, bool first, int valid, uint32_t bits, bool masked, bool mine) {
+            constexpr bool TWO = decltype(two_tag)::value;
+            constexpr int PART = TWO ? 8 : 32;                               // pairs stored at a time
             uint32_t v[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_addr + 32 * c, v[c]);
@@ -810,38 +822,34 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const float b0 = m_use == -INFINITY ? 0.0f : m_use;
                 const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_base2 = pack_f32x2(-b0, -b0);
                 uint64_t l_acc2 = pack_f32x2(0.0f, 0.0f);
-                float e_top = -INFINITY;                                     // of those that take the cubic, which is none above 2^127
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {                                // 16 keys
-                    float p[16];
-                    uint32_t top[8];
+                for (int c = 0; c < 64; c += PART) {                         // pairs of keys
+                    float p[2 * PART];
+                    uint32_t top[PART];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < PART; ++i) {
                         float e0, e1;
-                        const uint32_t* x = &v[c >> 1][16 * (c & 1) + 2 * i];
+                        const uint32_t* x = &v[(c + i) >> 4][2 * ((c + i) & 15)];
                         unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), scale2, neg_base2), e0, e1);
-                        if ((GMLP_GQA_POLY_MASK >> i) & 1) {
-                            ex2_poly_x2(e0, e1, p[2 * i], p[2 * i + 1]);
-                            e_top = max3_f32(e_top, e0, e1);
-                        } else {
-                            p[2 * i] = ex2_approx(e0);
-                            p[2 * i + 1] = ex2_approx(e1);
-                        }
+                        p[2 * i] = ex2_approx(e0);
+                        p[2 * i + 1] = ex2_approx(e1);
                         l_acc2 = add_f32x2(l_acc2, pack_f32x2(p[2 * i], p[2 * i + 1]));
                         top[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
                     }
-                    tmem_st_32x8(s_addr + 8 * c, top);
-                    if (opaque(two)) {
+                    if constexpr (TWO) {
+                        tmem_st_32x8(s_addr + c, top);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) top[i] = pack_bf16x2(p[2 * i] - bf16_lo(top[i]), p[2 * i + 1] - bf16_hi(top[i]));
-                        tmem_st_32x8(s_addr + 64 + 8 * c, top);
+                        for (int i = 0; i < PART; ++i) top[i] = pack_bf16x2(p[2 * i] - bf16_lo(top[i]), p[2 * i + 1] - bf16_hi(top[i]));
+                        tmem_st_32x8(s_addr + 64 + c, top);
+                    } else {
+                        tmem_st_32x32(s_addr + c, top);
                     }
                 }
                 float l0, l1;
                 unpack_f32x2(l_acc2, l0, l1);
                 l_blk = l0 + l1;
                 if (again) break;
-                moved = !(l_blk <= kGqaLazySum) || e_top > 126.0f || m_use == -INFINITY;
+                moved = !(l_blk <= kGqaLazySum) || m_use == -INFINITY;
                 again = __any_sync(0xFFFFFFFFu, mine && moved);
                 if (!again) break;
             }
@@ -850,7 +858,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         };
 
         // A few item: lane = key in a block's scores, channel in its output; the four warps agree on the base of the exponentials.
+        const int tile_no = t, row_no = r;
         auto few_item = [&](const KvItem& it, const int32_t* table, bool bad, uint32_t ring, uint32_t ring_phase) -> bool {
+            // (nothing that follows from these is worked out ahead and kept in registers through the other items' loops)
+            const int t = opaque(tile_no), r = opaque(row_no);
+            const uint32_t s_addr = tmem_base + 128u * (uint32_t)t + ((uint32_t)(r & ~31) << 16), o_addr = s_addr + 256u;
             const int blocks = it.blk1 - it.blk0, rows = it.npos * a.ratio;
             // every row's part, row by row in registers, four rows at a time: those that the item does not have are not run
             auto each_row = [&](auto part) {
@@ -875,7 +887,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     seen[n] = a.causal ? min(max(it.seen0 + pos, 0), it.keys) : it.keys;
                 }
             }
-            const uint32_t q4 = (uint32_t)(warp & 3);
+            const uint32_t q4 = (uint32_t)r >> 5;
             float* maxima = exchange + t * 128;                              // [16][4]
             float* weights = maxima + 64;
             auto agree = [&]() -> bool {                                     // what the four warps wrote before it they read after it
@@ -941,11 +953,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         if (!kv_wait(o_full0 + 8 * (2 * t + (buf ^ 1u)), ((o_phase >> (buf ^ 1u)) & 1u) ^ 1u, abort_flag, 21)) return false;
                         ptx::tc_fence_after_sync();
                         float o[kKvFew];
-                        tmem_ld_32x16(o_addr + 128u * (uint32_t)t, o);
+                        tmem_ld_32x16(o_addr, o);
                         ptx::tmem_ld_wait();
                         uint32_t ow[kKvFew];
                         each_row([&](int n) { ow[n] = __float_as_uint(o[n] * f[n]); });
-                        tmem_st_32x16(o_addr + 128u * (uint32_t)t, ow);
+                        tmem_st_32x16(o_addr, ow);
                         tmem_st_wait();
                         ptx::tc_fence_before_sync();
                     }
@@ -1004,7 +1016,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             int pos = 0, head = 0;
 #pragma unroll 1
             for (int n = 0; n < rows; ++n) {
-                float o = blocks > 0 ? tmem_ld_32x1(o_addr + 128u * (uint32_t)t + (uint32_t)n) : 0.0f;
+                float o = blocks > 0 ? tmem_ld_32x1(o_addr + (uint32_t)n) : 0.0f;
                 const float4 w = *reinterpret_cast<const float4*>(weights + 4 * n);
                 const float sum = blocks > 0 ? (w.x + w.y) + (w.z + w.w) : 0.0f;             // 0: nothing was seen
                 ptx::tmem_ld_wait();
@@ -1065,14 +1077,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int n_steps = big ? blocks : (blocks + 1 - t) / 2;         // of this tile
             m_use = -INFINITY;
             l_run = 0.0f;
+            // the steps of this tile's blocks, `stride` of them apart
+            auto steps = [&](auto two_tag, int key0, int stride) {
 #pragma unroll 1
-            for (int n = 0; n < n_steps; ++n) {
-                const int key0 = (it.blk0 + (opaque(big) ? n : 2 * n + t)) * kKvBlock;
-                // the scores are complete, and with them every matmul issued before them
-                if (!kv_wait(s_full0 + 16 * t, s_phase & 1u, abort_flag, 13)) { ok = false; break; }
-                s_phase ^= 1u;
-                ptx::tc_fence_after_sync();
-                if (opaque(active)) {
+                for (int n = 0; n < n_steps; ++n, key0 += stride) {
                     const int valid = max(0, min(kKvBlock, seen - key0));
                     uint32_t bits = 0xFFu;
                     if (opaque(bad)) {
@@ -1082,16 +1090,20 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         bits = __ballot_sync(0xFFFFFFFFu, there) & 0xFFu;
                     }
                     const bool masked = __any_sync(0xFFFFFFFFu, mine && valid < kKvBlock) || bits != 0xFFu;
-                    step_pass(opaque(n) == 0, valid, bits, opaque(masked), opaque(!big), mine);
+                    // the scores are complete, and with them every matmul issued before them
+                    if (!kv_wait(s_full0 + 16 * t, s_phase & 1u, abort_flag, 13)) return false;
+                    s_phase ^= 1u;
+                    ptx::tc_fence_after_sync();
+                    if (opaque(active)) step_pass(two_tag, opaque(n) == 0, valid, bits, opaque(masked), mine);
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(p_full0 + 16 * t);
                 }
-                ptx::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(p_full0 + 16 * t);
-            }
+                return true;
+            };
+            ok = big ? steps(std::false_type{}, it.blk0 * kKvBlock, kKvBlock) : steps(std::true_type{}, (it.blk0 + t) * kKvBlock, 2 * kKvBlock);
             if (!ok) break;
             o_phase ^= (uint32_t)n_steps & 1u;                               // parity of the next use: one phase per step
-            // a row whose scores were all -infinity (a NaN among them stays)
-            if (m_use == -INFINITY && l_run < 1e-30f) l_run = 0.0f;
             if (n_steps > 0) {
                 if (!kv_wait(o_full0 + 16 * t, (o_phase & 1u) ^ 1u, abort_flag, 14)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
@@ -1126,6 +1138,9 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 ++joins;
             }
             if (active && (big || t == 0)) {
+                const int t = opaque(tile_no), r = opaque(row_no);           // (as in few_item)
+                const int my_head = r % a.ratio;
+                const uint32_t o_addr = tmem_base + 256u + ((uint32_t)(r & ~31) << 16);
                 const int row_in_slot = (big ? 128 * t : 0) + r;
                 const int64_t part = (int64_t)it.slot * a.slot_rows + row_in_slot;
                 float* sums = reinterpret_cast<float*>(a.workspace + kv_ws_sums(gridDim.x, a.slot_rows)) + part * D;
@@ -1196,36 +1211,120 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
 }
 
-// The parts of cut items, added in order: CTA (c, y) takes a share of the rows of the item that was cut at the end of CTA c's stretch;
-// a warp takes a row at a time.
-constexpr int kKvJoinThreads = 256;
+// The parts of cut items, added in order.  The rows of all of them lie end to end.  Many rows (of some two parts each: a prompt's items): eight
+// lanes or a warp take a row.  Few (a long conversation: as many parts as SMs, of a handful of rows): a CTA does, its warps take every eighth
+// part each.
+constexpr int kKvJoinThreads = 256, kKvMostCtas = 512;
 template <int D>
 __global__ void __launch_bounds__(kKvJoinThreads)
 kv_join_kernel(const KvAttnArgs a, int ctas)
 {
-    constexpr int C = D / 32;
+    constexpr int WARPS = kKvJoinThreads / 32;
+    __shared__ int s_end[kKvMostCtas];                               // rows of the cut items up to and with the one cut at the end of a CTA's stretch
+    __shared__ int s_warp[WARPS];
+    __shared__ float s_sum[WARPS][D], s_l[WARPS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    const int lane = threadIdx.x & 31, warps = kKvJoinThreads / 32;
-    const KvCut cut = reinterpret_cast<const KvCut*>(a.workspace)[blockIdx.x];
-    if (cut.parts < 2) return;
+    const KvCut* cuts = reinterpret_cast<const KvCut*>(a.workspace);
+    int total = 0;
+    for (int c0 = 0; c0 < ctas; c0 += kKvJoinThreads) {
+        const int c = c0 + tid;
+        int upto = c < ctas && cuts[c].parts >= 2 ? cuts[c].npos * a.ratio : 0;
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, upto, w);
+            if (lane >= w) upto += v;
+        }
+        if (lane == 31) s_warp[warp] = upto;
+        __syncthreads();
+        int all = total;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            if (w == warp) upto += all;
+            all += s_warp[w];
+        }
+        if (c < ctas) s_end[c] = upto;
+        total = all;
+        __syncthreads();
+    }
     const float2* stats = reinterpret_cast<const float2*>(a.workspace + kv_ws_stats(ctas));
     const float* sums = reinterpret_cast<const float*>(a.workspace + kv_ws_sums(ctas, a.slot_rows));
-    for (int i = blockIdx.y * warps + (threadIdx.x >> 5); i < cut.npos * a.ratio; i += gridDim.y * warps) {
-        const int pos = i / a.ratio, head = i - pos * a.ratio;
+    // row i of all: where its parts lie and where it goes
+    int parts, first, in_slot;                                       // parts, slot of the first of two or more, row in each slot
+    bf16* out;
+    auto find = [&](int i) {
+        int lo = 0, hi = ctas - 1;                                   // the first CTA with i < s_end
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (i < s_end[mid]) hi = mid;
+            else lo = mid + 1;
+        }
+        const KvCut cut = cuts[lo];
+        const int in = i - (s_end[lo] - cut.npos * a.ratio);
+        const int pos = in / a.ratio, head = in - pos * a.ratio;
         const int t = cut.two_tiles && pos >= a.tile_pos ? 1 : 0;
-        const int row = 128 * t + (pos - t * a.tile_pos) * a.ratio + head;
-        auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + p)) * a.slot_rows + row; };
+        in_slot = 128 * t + (pos - t * a.tile_pos) * a.ratio + head;
+        parts = cut.parts;
+        first = lo;
+        out = a.O + ((int64_t)(cut.row0 + pos) * a.Hq + (int64_t)cut.head * a.ratio + head) * D;
+    };
+    auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * first + 1 : 2 * (first + p)) * a.slot_rows + in_slot; };
+    // LANES to a row, four channels at a time (two where a warp has no more to give): lane, lane + LANES, ...
+    auto by_lanes = [&](auto lanes_tag) {
+        constexpr int LANES = decltype(lanes_tag)::value, ROWS = 32 / LANES, V = D / LANES >= 4 ? 4 : 2, N = D / LANES / V;
+        const int sub = lane % LANES;
+        for (int i = (blockIdx.x * WARPS + warp) * ROWS + lane / LANES; i < total; i += gridDim.x * WARPS * ROWS) {
+            find(i);
+            float top = -INFINITY;
+#pragma unroll 4
+            for (int p = 0; p < parts; ++p) top = fmaxf(top, stats[part(p)].x);
+            const float b0 = top == -INFINITY ? 0.0f : top;
+            float o[N][V] = {}, l = 0.0f;
+#pragma unroll 4
+            for (int p = 0; p < parts; ++p) {
+                const float2 s = stats[part(p)];
+                const float* x = sums + part(p) * D + sub * V;
+                float v[N][V];
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    if constexpr (V == 4) *reinterpret_cast<float4*>(v[c]) = *reinterpret_cast<const float4*>(x + c * LANES * V);
+                    else *reinterpret_cast<float2*>(v[c]) = *reinterpret_cast<const float2*>(x + c * LANES * V);
+                }
+                const float f = ex2_approx(s.x - b0);
+                l += s.y * f;
+#pragma unroll
+                for (int c = 0; c < N; ++c)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) o[c][k] += v[c][k] * f;
+            }
+            const float inv = 1.0f / l;
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                uint32_t pk[V / 2];
+#pragma unroll
+                for (int k = 0; k < V / 2; ++k) pk[k] = l == 0.0f ? 0u : pack_bf16x2(o[c][2 * k] * inv, o[c][2 * k + 1] * inv);
+                uint32_t* to = reinterpret_cast<uint32_t*>(out + (sub + c * LANES) * V);
+                if constexpr (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(pk[0], pk[1]);
+                else *to = pk[0];
+            }
+        }
+    };
+    // measured, whole calls: 37 thousand rows of some two parts (a chunk of 2048) 267 us with a warp to a row, 258 with eight lanes; 3900 rows
+    // of nine parts 154 with a warp, 162 with eight lanes, 156 with a CTA; 256 rows of 148 parts 498 with a warp, 154 with a CTA
+    if (total > (int)gridDim.x * WARPS) return by_lanes(std::integral_constant<int, 8>{});
+    if (total > (int)gridDim.x) return by_lanes(std::integral_constant<int, 32>{});
+    constexpr int C = D / 32;
+    for (int i = blockIdx.x; i < total; i += gridDim.x) {
+        find(i);
         float top = -INFINITY;
-        for (int p = lane; p < cut.parts; p += 32) top = fmaxf(top, stats[part(p)].x);
+        for (int p = lane; p < parts; p += 32) top = fmaxf(top, stats[part(p)].x);
 #pragma unroll
         for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
         const float b0 = top == -INFINITY ? 0.0f : top;
-        float o[C], l = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = 0.0f;
+        float o[C] = {}, l = 0.0f;
 #pragma unroll 4
-        for (int p = 0; p < cut.parts; ++p) {
+        for (int p = warp; p < parts; p += WARPS) {
             const float2 s = stats[part(p)];
             const float f = ex2_approx(s.x - b0);
             l += s.y * f;
@@ -1236,13 +1335,20 @@ kv_join_kernel(const KvAttnArgs a, int ctas)
 #pragma unroll
             for (int c = 0; c < C; ++c) o[c] += v[c] * f;
         }
-        const float inv = 1.0f / l;
-        uint32_t pk[C / 2];
 #pragma unroll
-        for (int c = 0; c < C / 2; ++c) pk[c] = l == 0.0f ? 0u : pack_bf16x2(o[2 * c] * inv, o[2 * c + 1] * inv);
-        bf16* out = a.O + ((int64_t)(cut.row0 + pos) * a.Hq + (int64_t)cut.head * a.ratio + head) * D + lane * C;
-        if constexpr (C == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pk[0], pk[1]);
-        else *reinterpret_cast<uint32_t*>(out) = pk[0];
+        for (int c = 0; c < C; ++c) s_sum[warp][lane * C + c] = o[c];
+        if (lane == 0) s_l[warp] = l;
+        __syncthreads();
+        if (tid < D) {
+            float sum = 0.0f, weight = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                sum += s_sum[w][tid];
+                weight += s_l[w];
+            }
+            out[tid] = __float2bfloat16_rn(weight == 0.0f ? 0.0f : sum / weight);
+        }
+        __syncthreads();
     }
 }
 

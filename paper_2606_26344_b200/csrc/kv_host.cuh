@@ -62,17 +62,26 @@ int launch_block(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t smem, cud
 }
 
 int launch_rotate(DeviceState* dev, gmlp::RotateArgs& k, bool interleaved, cudaStream_t st) {
-    const int half = k.rot / 2;
-    const bool inter = interleaved || k.rot == 0;
+    const int half = k.rot / 2, rest = k.D - k.rot;
+    const bool inter = interleaved;
     const int vec = (inter ? k.rot : half) % 8 == 0 ? 8 : 2;
-    const int units = inter ? k.D / vec : half / vec + (k.D - k.rot) / vec;
-    const int y = units >= gmlp::kRotateThreads ? 1 : gmlp::kRotateThreads / units;
-    // whole tokens per CTA, more of them once there are enough CTAs; the heads of few tokens go to several CTAs
+    k.apart = rest % (2 * vec) == 0 ? rest / 2 : 0;
+    k.turned_apart = !inter || k.rot % (2 * vec) == 0 ? half : 0;
+    const int units = (k.turned_apart > 0 ? half : k.rot) / vec + rest / vec / (k.apart > 0 ? 2 : 1);
+    // Threads: `lanes` to a unit of a token's heads, each with as many heads as the next, and as many tokens side by side as fit.  Whole tokens
+    // per CTA, two or four rounds of them while there are enough CTAs (four per SM); the heads of few tokens go to several CTAs.
     const int heads = k.Hq + 2 * k.Hkv, sms = dev->sm_count;
-    k.tokens = k.T >= 64 * sms ? 4 : (k.T >= 16 * sms ? 2 : 1);
+    const int most = units >= gmlp::kRotateThreads ? 1 : gmlp::kRotateThreads / units, rounds = (heads + most - 1) / most;
+    k.lanes = (heads + rounds - 1) / rounds;
+    int side = most / k.lanes;
+    if (side > gmlp::kRotateMaxTokens / 2) side = gmlp::kRotateMaxTokens / 2;
+    if (side > k.T / sms) side = k.T / sms;
+    if (side < 1) side = 1;
+    k.tokens = k.T >= 16 * side * sms ? 4 * side : (k.T >= 8 * side * sms ? 2 * side : side);
+    if (k.tokens > gmlp::kRotateMaxTokens) k.tokens = gmlp::kRotateMaxTokens;
     int split = k.T >= sms ? 1 : sms / k.T;
-    if (split > (heads + y - 1) / y) split = (heads + y - 1) / y;
-    const dim3 grid((unsigned)((k.T + k.tokens - 1) / k.tokens), (unsigned)split), block((unsigned)units, (unsigned)y);
+    if (split > rounds) split = rounds;
+    const dim3 grid((unsigned)((k.T + k.tokens - 1) / k.tokens), (unsigned)split), block((unsigned)units, (unsigned)(side * k.lanes));
     const uint32_t smem = (uint32_t)(k.tokens * half * sizeof(float2));
     if (vec == 8) return inter ? launch_block(gmlp::rotate_kernel<8, true>, grid, block, smem, st, k)
                                : launch_block(gmlp::rotate_kernel<8, false>, grid, block, smem, st, k);

@@ -47,16 +47,18 @@ struct KvAttnArgs {
     int few_pos;                     // positions per 16 rows (0: more than 16 heads share a key/value head)
     int q_bytes, q_few_bytes;        // of one tile's Q boxes
     int slot_rows;                   // rows of a partial result
-    int min_stretch;                 // of a CTA, in keys
+    int min_stretch;                 // of a CTA, on the axis; more than a block of a big item
     float scale_log2;
 };
 
 constexpr int kKvThreads = 384, kKvBlock = 128, kKvRing = 4;
 constexpr int kKvFew = 16;                       // rows of an item whose products are turned round
 constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
-// An item's start and end, in keys of its length on the axis (a prompt of 8192: 641 us with 64 for all, 560 with 256, 510 with 512 for big
-// ones; prompts with D = 64: 252, 223, 228).
-constexpr int kKvBigCost = 448, kKvSmallCost = 384, kKvFewCost = 256;
+// The axis: what a key of an item takes, and an item's start and end.  In a batch of both, big items are bound by the tensor pipe and the
+// softmax and the others by the copies, which run the faster the fewer SMs make them (40 single tokens and three chunks: 301 us with the
+// same for all, 265 with 3 : 2 : 2, 244 with 4 : 3 : 2, 267 with 5 : 3 : 2).  Starts: a prompt of 8192 641 us with 64 keys, 560 with 256, 515 now.
+constexpr int kKvBigKey = 4, kKvSmallKey = 3, kKvFewKey = 2;
+constexpr int kKvBigStart = 448 * kKvBigKey, kKvSmallStart = 384 * kKvSmallKey, kKvFewStart = 256 * kKvFewKey;
 constexpr int kKvRegsLight = 72, kKvRegsSoftmax = 216;
 constexpr int kKvKernelId = 30;
 constexpr uint32_t kKvWaitLimit = 8;                         // some 20 s: some waits last as long as an item
@@ -96,9 +98,13 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
     if (!fits) keys = 0;
     if (report && (!ok || !fits)) report_index(ok ? 6 : 7);
 }
+// Up to this length an item is never cut: a part costs as much as the keys that it saves.  (Where a CTA's stretch is short, items that are
+// longer than it by this much stay whole too.  8 requests of 300 keys: 18.2 us cut, 14.0 whole.)
+constexpr int kKvSnap = 1024;
 enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
 __device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) { return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem); }
-__device__ __forceinline__ int kv_start(int mode) { return mode == kKvBigItem ? kKvBigCost : (mode == kKvSmallItem ? kKvSmallCost : kKvFewCost); }
+__host__ __device__ constexpr int kv_start(int mode) { return mode == kKvBigItem ? kKvBigStart : (mode == kKvSmallItem ? kKvSmallStart : kKvFewStart); }
+__host__ __device__ constexpr int kv_key(int mode) { return mode == kKvBigItem ? kKvBigKey : (mode == kKvSmallItem ? kKvSmallKey : kKvFewKey); }
 __device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int rows) { return (rows + 2 * a.tile_pos - 1) / (2 * a.tile_pos); }
 // Length on the axis of the first n of a request's tiles; all but the last are big.
 __device__ __forceinline__ int64_t kv_cost(const KvAttnArgs& a, int rows, int keys, int n) {
@@ -106,16 +112,21 @@ __device__ __forceinline__ int64_t kv_cost(const KvAttnArgs& a, int rows, int ke
     const int s = 2 * a.tile_pos;
     const bool whole = (int64_t)n * s >= rows;                      // the last tile ends with the request
     const int m = whole ? n - 1 : n;
-    int64_t cost = (int64_t)m * kKvBigCost + (whole ? kv_start(kv_mode(a, rows - m * s)) + keys : 0);
-    if (!a.causal) return cost + (int64_t)m * keys;
+    int64_t cost = (int64_t)m * kKvBigStart;
+    if (whole) {
+        const int mode = kv_mode(a, rows - m * s);
+        cost += kv_start(mode) + (int64_t)kv_key(mode) * keys;
+    }
+    if (!a.causal) return cost + (int64_t)kKvBigKey * m * keys;
     const int first = keys - rows;                                  // tile i of the others sees first + (i + 1) s keys
     const int none = first < 0 ? min(m, -first / s) : 0;
-    return cost + (int64_t)(m - none) * first + (int64_t)s * ((int64_t)m * (m + 1) - (int64_t)none * (none + 1)) / 2;
+    return cost + kKvBigKey * ((int64_t)(m - none) * first + (int64_t)s * ((int64_t)m * (m + 1) - (int64_t)none * (none + 1)) / 2);
 }
-// Blocks of an item of `keys` keys that lie before place x of it.
-__device__ __forceinline__ int kv_blocks_before(int64_t x, int start, int keys) {
-    const int64_t n = x <= start ? 0 : (x - start + kKvBlock - 1) / kKvBlock;
-    return (int)min(n, (int64_t)((keys + kKvBlock - 1) / kKvBlock));
+// Blocks of an item that lie before place x of it.
+__device__ __forceinline__ int kv_blocks_before(int64_t x, int mode, int blocks) {
+    const int each = kKvBlock * kv_key(mode);
+    const int64_t n = x <= kv_start(mode) ? 0 : (x - kv_start(mode) + each - 1) / each;
+    return (int)min(n, (int64_t)blocks);
 }
 
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -302,6 +313,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
     const int64_t total = per_head * a.Hkv;
     const int64_t stretch = max((total + gridDim.x - 1) / gridDim.x, (int64_t)a.min_stretch);
+    const int64_t snap = kKvSnap + (stretch < 2048 ? stretch : 0);           // longest item that is not cut
     const int64_t lo = stretch * blockIdx.x, hi = min(total, lo + stretch);
     const int head_lo = lo < hi ? (int)(lo / per_head) : 0;
     if (lo < hi) {
@@ -625,15 +637,18 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 }
                 const int npos = min(2 * a.tile_pos, rows - pos0);
                 const int seen_last = a.causal ? max(keys - rows + pos0 + npos, 0) : keys;
-                const int mode = kv_mode(a, npos), start = kv_start(mode);
-                const int64_t cost = (int64_t)seen_last + start;
+                const int mode = kv_mode(a, npos);
+                const int64_t cost = kv_start(mode) + (int64_t)kv_key(mode) * seen_last;
                 const int all = (seen_last + kKvBlock - 1) / kKvBlock;
                 const int64_t from = max(lo - x, (int64_t)0);
-                const int blk0 = kv_blocks_before(from, start, seen_last), blk1 = kv_blocks_before(min(hi - x, cost), start, seen_last);
+                // a short item goes whole to the CTA in whose stretch it starts
+                const bool short_item = cost <= snap;
+                const int blk0 = short_item ? (from > 0 ? all : 0) : kv_blocks_before(from, mode, all);
+                const int blk1 = short_item ? all : kv_blocks_before(min(hi - x, cost), mode, all);
                 if (blk1 > blk0 || (all == 0 && from == 0)) {
                     const bool whole = blk0 == 0 && blk1 == all;
                     if (!whole && blk0 == 0) {                               // the first part of a cut item: whose are the others
-                        cut.parts = (int)((x + start + (int64_t)kKvBlock * (all - 1)) / stretch) - (int)blockIdx.x + 1;
+                        cut.parts = (int)((x + kv_start(mode) + (int64_t)kKvBlock * kv_key(mode) * (all - 1)) / stretch) - (int)blockIdx.x + 1;
                         cut.head = head;
                         cut.npos = npos;
                         cut.row0 = row0 + pos0;

@@ -197,7 +197,7 @@ bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, in
 }
 
 template <int D>
-int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, cudaStream_t st) {
+int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, bool join, cudaStream_t st) {
     if (!dev->kv_attr_set[D == 128]) {
         if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
@@ -208,6 +208,7 @@ int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensor
     int rc = launch_block(gmlp::kv_attention_kernel<D>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
+    if (!join) return GMLP_OK;
     rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)(ctas * (k.slot_rows > 64 ? 8 : 4))), dim3(gmlp::kKvJoinThreads), 0, st, k, ctas);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_join", st);
@@ -265,14 +266,17 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     k.q_bytes = ratio * q_pos * D * 2;
     k.q_few_bytes = ratio * few_pos * D * 2;
     k.slot_rows = kv_slot_rows(a->T, ratio);
-    k.min_stretch = 384;
+    k.min_stretch = 768;
     const uint64_t cache_rows = (uint64_t)a->cache.n_pages * (uint64_t)k.Hkv * (uint64_t)k.page_size;
     CUtensorMap tmQ, tmQfew, tmK, tmV;
     if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_kv_query(&tmQfew, a->Q, D, k.Hq, a->T, ratio, few_pos) || !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
         !encode_2d(&tmV, a->cache.v, (uint64_t)D, cache_rows, 64, (uint32_t)k.box))
         return GMLP_ERR_LAUNCH;
     prof_begin(st);
-    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmQfew, tmK, tmV, k, st) : launch_kv_attention<64>(dev, tmQ, tmQfew, tmK, tmV, k, st);
+    // no item is long enough to be cut where the table has few pages
+    const int mode = a->T <= k.few_pos ? gmlp::kKvFewItem : (a->T <= k.tile_pos ? gmlp::kKvSmallItem : gmlp::kKvBigItem);
+    const bool join = gmlp::kv_start(mode) + a->table_width * k.page_size * gmlp::kv_key(mode) > gmlp::kKvSnap;
+    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmQfew, tmK, tmV, k, join, st) : launch_kv_attention<64>(dev, tmQ, tmQfew, tmK, tmV, k, join, st);
     if (rc != GMLP_OK) return rc;
     return finish_checked(dev, a->flags, st);
 }

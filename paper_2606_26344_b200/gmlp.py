@@ -1178,7 +1178,7 @@ def kv_attention(Q, cache: KvCache, block_table, lengths, n_q_heads: int, q_star
         o = O.data_ptr()
     else:
         o = _pointer(O, "O", torch.bfloat16, shape, device)
-    need = 0 if workspace is not None else lib().gmlp_kv_workspace_bytes(T, n_q_heads, cache.n_kv_heads, D, _sm_count(device))
+    need = 0 if workspace is not None else lib().gmlp_kv_workspace_bytes(T, n_q_heads, cache.n_kv_heads, D, _sm_count(device)) or 1
     keep, ws, ws_bytes = _workspace(workspace, need, device, stream)
     _run(lib().gmlp_kv_attention,
          GmlpKvAttentionArgs(_SIZE_KV_ATTENTION, (KV_CAUSAL if causal else 0) | (FLAG_CHECKED if checked else 0), q, o, cache.struct, table, n,

@@ -204,7 +204,8 @@ template <int SLOTS> struct KvCursor {
     }
 };
 
-template <int D>
+// FEW: with the code of few items; without it they are small ones.
+template <int D, bool FEW>
 __global__ void __launch_bounds__(kKvThreads, 1)
 kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQfew, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const KvAttnArgs a)
@@ -470,7 +471,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int open = first_hidden(it) / kKvBlock - it.blk0;          // blocks of the item before this one need no mending
             uint32_t k_slot = 0, v_slot = 0;
             bool ok;
-            if (it.mode == kKvFewItem) {
+            if constexpr (FEW) if (it.mode == kKvFewItem) {
                 const int t = it.tile;
                 const uint32_t q0 = q_lo + (uint32_t)t * (kKvRegion >> 4), p0 = p_lo + (uint32_t)t * (kKvRegion >> 4);
                 auto scores = [&](int n) -> bool {
@@ -1072,7 +1073,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const bool big = it.mode == kKvBigItem;
             const int32_t* table = a.table + (int64_t)it.b * a.width;
             bool bad = false;                                                // pages that the cache does not have
-            if (it.mode == kKvFewItem && it.tile != t) {
+            if (FEW && it.mode == kKvFewItem && it.tile != t) {
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * ring);
                 continue;
@@ -1081,9 +1082,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!kv_wait(item_checked0 + 8 * ring, ring_phase, abort_flag, 19)) break;
                 bad = odd_pages[ring] != 0;
             }
-            if (it.mode == kKvFewItem) {
-                if (!few_item(it, table, bad, ring, ring_phase)) break;
-                continue;
+            if constexpr (FEW) {
+                if (it.mode == kKvFewItem) {
+                    if (!few_item(it, table, bad, ring, ring_phase)) break;
+                    continue;
+                }
             }
             const int pos = my_pos + (big ? t * a.tile_pos : 0);
             const bool mine = my_pos < a.tile_pos && pos < it.npos;          // this thread's row exists
@@ -1176,19 +1179,6 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     } else {
                         ptx::tmem_ld_wait();
                     }
-                    if (opaque(odd)) {
-#pragma unroll 1
-                        for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
-                            const int page = table[j / a.page_size];
-                            if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-                            const bf16* vr = a.v + (((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + c;
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                const float x = __bfloat162float(vr[k]);
-                                if (!(x - x == 0.0f)) o[k] += x;
-                            }
-                        }
-                    }
                     if (!mine) continue;
                     if (opaque(it.slot) < 0) {
 #pragma unroll
@@ -1202,6 +1192,21 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
                             *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
+                    }
+                }
+                if (odd && mine) {                                           // the row that was just written gets what V held in place of numbers
+#pragma unroll 1
+                    for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
+                        const int page = table[j / a.page_size];
+                        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+                        const bf16* vr = a.v + (((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D;
+#pragma unroll 1
+                        for (int k = 0; k < D; ++k) {
+                            const float x = __bfloat162float(vr[k]);
+                            if (x - x == 0.0f) continue;
+                            if (it.slot < 0) out[k] = __float2bfloat16_rn(__bfloat162float(out[k]) + x);
+                            else sums[k] += x;
+                        }
                     }
                 }
             }

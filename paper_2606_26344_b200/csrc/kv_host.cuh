@@ -196,16 +196,17 @@ bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, in
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool FEW>
 int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, bool join, cudaStream_t st) {
-    if (!dev->kv_attr_set[D == 128]) {
-        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
+    bool& set = dev->kv_attr_set[2 * (D == 128) + FEW];
+    if (!set) {
+        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
-        dev->kv_attr_set[D == 128] = true;
+        set = true;
     }
     const int ctas = dev->sm_count;
     if (ctas > gmlp::kKvMostCtas) return GMLP_ERR_UNSUPPORTED;
-    int rc = launch_block(gmlp::kv_attention_kernel<D>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
+    int rc = launch_block(gmlp::kv_attention_kernel<D, FEW>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
     if (!join) return GMLP_OK;
@@ -261,7 +262,10 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     k.box = a->cache.page_size & -a->cache.page_size;
     if (k.box > gmlp::kKvBlock) k.box = gmlp::kKvBlock;
     const int q_pos = a->T < k.tile_pos ? (int)a->T : k.tile_pos, D = a->cache.head_dim;
-    k.few_pos = gmlp::kKvFew / ratio;                                        // 0: none
+    // Where a request has more than 256 rows (a big item's) on average, most belong to big items, and these run better in the kernel that has no
+    // code for few ones (a chunk of 2048 237 us with, 226 without; 40 single tokens and three chunks of 500, 143 rows on average, 234 and 246).
+    const bool few = a->T * ratio <= 256 * a->B;
+    k.few_pos = few ? gmlp::kKvFew / ratio : 0;                              // 0: none
     const int few_pos = k.few_pos == 0 ? q_pos : (a->T < k.few_pos ? (int)a->T : k.few_pos);
     k.q_bytes = ratio * q_pos * D * 2;
     k.q_few_bytes = ratio * few_pos * D * 2;
@@ -276,7 +280,9 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     // no item is long enough to be cut where the table has few pages
     const int mode = a->T <= k.few_pos ? gmlp::kKvFewItem : (a->T <= k.tile_pos ? gmlp::kKvSmallItem : gmlp::kKvBigItem);
     const bool join = gmlp::kv_start(mode) + a->table_width * k.page_size * gmlp::kv_key(mode) > gmlp::kKvSnap;
-    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmQfew, tmK, tmV, k, join, st) : launch_kv_attention<64>(dev, tmQ, tmQfew, tmK, tmV, k, join, st);
+#define GMLP_KV_ATTENTION(D) \
+    (few ? launch_kv_attention<D, true>(dev, tmQ, tmQfew, tmK, tmV, k, join, st) : launch_kv_attention<D, false>(dev, tmQ, tmQfew, tmK, tmV, k, join, st))
+    rc = D == 128 ? GMLP_KV_ATTENTION(128) : GMLP_KV_ATTENTION(64);
     if (rc != GMLP_OK) return rc;
     return finish_checked(dev, a->flags, st);
 }

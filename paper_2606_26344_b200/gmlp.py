@@ -1027,9 +1027,8 @@ def kv4_attention(Q, cache: Kv4Cache, block_table, lengths, n_q_heads: int, q_le
 
 # --------------------------------------------------------------------------- rotary positions, bf16 cache and its attention
 
-def rope_steps(rotary_dim: int, base: float = 10000.0, scaling=None):
-    """gmlp_rope_steps: (turns per position of each pair in units of 2^-64, as a list of ints; amplitude).  ``scaling``: None,
-    ("linear", factor), ("bands", factor, low, high, original) or ("ramp", factor, high, low, original)."""
+def _rope_table(rotary_dim: int, base: float, scaling):
+    """(a C array of the steps, amplitude)"""
     if scaling is None:
         s = None
     else:
@@ -1045,7 +1044,14 @@ def rope_steps(rotary_dim: int, base: float = 10000.0, scaling=None):
     rc = lib().gmlp_rope_steps(rotary_dim, base, s, steps, ctypes.byref(amplitude))
     if rc != OK:
         raise GmlpError(rc)
-    return list(steps), amplitude.value
+    return steps, amplitude.value
+
+
+def rope_steps(rotary_dim: int, base: float = 10000.0, scaling=None):
+    """gmlp_rope_steps: (turns per position of each pair in units of 2^-64, as a list of ints; amplitude).  ``scaling``: None,
+    ("linear", factor), ("bands", factor, low, high, original) or ("ramp", factor, high, low, original)."""
+    steps, amplitude = _rope_table(rotary_dim, base, scaling)
+    return list(steps), amplitude
 
 
 class Rope:
@@ -1055,9 +1061,8 @@ class Rope:
 
     def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None,
                  amplitude: Optional[float] = None, device="cuda"):
-        steps, own = rope_steps(rotary_dim, base, scaling)
-        signed = [v - (1 << 64) if v >> 63 else v for v in steps]
-        self.steps = torch.tensor(signed, dtype=torch.int64).to(device)
+        steps, own = _rope_table(rotary_dim, base, scaling)
+        self.steps = torch.frombuffer(steps, dtype=torch.int64).to(device)
         if self.steps.device.type != "cuda":
             raise TypeError("device: expected a CUDA device")
         self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, bool(interleaved), own if amplitude is None else float(amplitude)

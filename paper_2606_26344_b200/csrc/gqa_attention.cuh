@@ -111,9 +111,10 @@ __device__ __forceinline__ float max3_f32(float a, float b, float c) {
 }
 // 2^x on the FMA pipe for part of the exponentials: x is split into the nearest integer n (taken from the mantissa
 // of x + 1.5 * 2^23) and f in [-1/2, 1/2]; 2^f is a cubic fitted for minimum relative error (7.5e-5, a twenty-fifth
-// of the bf16 rounding that P gets next); n is added to the exponent field.  Both values of a pair at once.
+// of the bf16 rounding that P gets next); n is added to the exponent field.  Both values of a pair at once.  (From 2^128 on the exponent
+// field would wrap round to some other number, and the sum that tells when the base has to move would not tell: x stays at 127.)
 __device__ __forceinline__ void ex2_poly_x2(float x0, float x1, float& p0, float& p1) {
-    const uint64_t x = pack_f32x2(fmaxf(x0, -125.0f), fmaxf(x1, -125.0f));
+    const uint64_t x = pack_f32x2(fminf(fmaxf(x0, -125.0f), 127.0f), fminf(fmaxf(x1, -125.0f), 127.0f));
     const uint64_t t = add_f32x2(x, pack_f32x2(12582912.0f, 12582912.0f));
     const uint64_t n = add_f32x2(t, pack_f32x2(-12582912.0f, -12582912.0f));
     const uint64_t f = fma_f32x2(n, pack_f32x2(-1.0f, -1.0f), x);

@@ -134,6 +134,20 @@ def test_long(reqs, Hq, Hkv, D, page):
     Batch(reqs, Hq, Hkv, D, page).check()
 
 
+@pytest.mark.parametrize("reqs,Hq,Hkv,D,page", [([(1, 300), (2000, 2100), (1, 5000), (3, 40)], 8, 2, 128, 64),       # single tokens beside a long chunk
+                                                ([(1500, 3000)], 32, 8, 128, 64), ([(1200, 1200), (1300, 4000)], 12, 4, 64, 48),
+                                                ([(33, 6000)] * 12, 8, 2, 128, 32), ([(20, 3000)] * 9, 16, 4, 64, 16),  # every cut item has one tile
+                                                ([(1, 700)] * 300, 8, 2, 128, 64), ([(4, 1100)] * 90, 8, 2, 64, 16)])
+def test_items_of_each_kind_cut_between_ctas(reqs, Hq, Hkv, D, page):
+    Batch(reqs, Hq, Hkv, D, page).check(only=range(0, len(reqs), max(1, len(reqs) // 12)))
+
+
+@pytest.mark.parametrize("n", [300, 1400, 1401, 1535, 1536, 1537, 1700])
+@pytest.mark.parametrize("r", [1, 20, 40])
+def test_around_the_length_that_is_cut(n, r):
+    Batch([(r, n)] * 40, 8, 2, 128, 64).check(only=range(0, 40, 7))
+
+
 def test_wide_tables_and_uniform_rows():
     batch = Batch([(4, 100), (4, 3), (4, 1500)], 8, 2, 128, 64, extra_width=5000, behind=0)
     O = batch.check()

@@ -68,9 +68,11 @@ constexpr uint32_t kKvRegion = 32768;            // of a tile: Q, and in few ite
 // the tiles' regions, FIFO; base and weight of rows; what the warps of few items exchange; items and barriers
 constexpr uint32_t kv_attn_smem(int D) { return 2 * kKvRegion + kv_slots(D) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
 
-// Workspace: one descriptor per CTA, then base and weight of the rows of each of its two partial results, then their sums.
+// Workspace: one descriptor per CTA - the cut item that its stretch ends in - then base and weight of the rows of each of its two partial
+// results, then their sums.
 struct KvCut {
-    int parts, head, row0, npos, two_tiles, pad[3];
+    int parts, first;                // parts (less than two: none), the CTA that has the first of them
+    int head, row0, npos, two_tiles, pad[2];
 };
 __host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ctas * sizeof(KvCut) + 255) & ~(uint64_t)255; }
 __host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) { return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255); }
@@ -648,8 +650,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const int blk1 = short_item ? all : kv_blocks_before(min(hi - x, cost), mode, all);
                 if (blk1 > blk0 || (all == 0 && from == 0)) {
                     const bool whole = blk0 == 0 && blk1 == all;
-                    if (!whole && blk0 == 0) {                               // the first part of a cut item: whose are the others
-                        cut.parts = (int)((x + kv_start(mode) + (int64_t)kKvBlock * kv_key(mode) * (all - 1)) / stretch) - (int)blockIdx.x + 1;
+                    if (blk1 < all) {                                        // cut at the end of the stretch: whose are the parts
+                        const int64_t block0 = x + kv_start(mode);
+                        cut.first = (int)(block0 / stretch);
+                        cut.parts = (int)((block0 + (int64_t)kKvBlock * kv_key(mode) * (all - 1)) / stretch) - cut.first + 1;
                         cut.head = head;
                         cut.npos = npos;
                         cut.row0 = row0 + pos0;
@@ -1231,70 +1235,39 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
 }
 
-// The parts of cut items, added in order.  The rows of all of them lie end to end.  Many rows (of some two parts each: a prompt's items): eight
-// lanes or a warp take a row.  Few (a long conversation: as many parts as SMs, of a handful of rows): a CTA does, its warps take every eighth
-// part each.
-constexpr int kKvJoinThreads = 256, kKvMostCtas = 512;
+// The parts of cut items, added in order.  An item's rows are shared out to the CTAs (c, y) of all c whose stretch ends in it: one c for a
+// prompt's item of two parts, nearly all where one long conversation is cut into as many parts as SMs.  A CTA takes a row at a time (its warps
+// every eighth part each), or eight (a warp each), or 32 (eight lanes each), by how many it has.
+constexpr int kKvJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kKvJoinThreads)
-kv_join_kernel(const KvAttnArgs a, int ctas)
+kv_join_kernel(const KvAttnArgs a)
 {
     constexpr int WARPS = kKvJoinThreads / 32;
-    __shared__ int s_end[kKvMostCtas];                               // rows of the cut items up to and with the one cut at the end of a CTA's stretch
-    __shared__ int s_warp[WARPS];
     __shared__ float s_sum[WARPS][D], s_l[WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    const KvCut* cuts = reinterpret_cast<const KvCut*>(a.workspace);
-    int total = 0;
-    for (int c0 = 0; c0 < ctas; c0 += kKvJoinThreads) {
-        const int c = c0 + tid;
-        int upto = c < ctas && cuts[c].parts >= 2 ? cuts[c].npos * a.ratio : 0;
-#pragma unroll
-        for (int w = 1; w < 32; w <<= 1) {
-            const int v = __shfl_up_sync(0xFFFFFFFFu, upto, w);
-            if (lane >= w) upto += v;
-        }
-        if (lane == 31) s_warp[warp] = upto;
-        __syncthreads();
-        int all = total;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w == warp) upto += all;
-            all += s_warp[w];
-        }
-        if (c < ctas) s_end[c] = upto;
-        total = all;
-        __syncthreads();
-    }
-    const float2* stats = reinterpret_cast<const float2*>(a.workspace + kv_ws_stats(ctas));
-    const float* sums = reinterpret_cast<const float*>(a.workspace + kv_ws_sums(ctas, a.slot_rows));
-    // row i of all: where its parts lie and where it goes
-    int parts, first, in_slot;                                       // parts, slot of the first of two or more, row in each slot
+    const KvCut cut = reinterpret_cast<const KvCut*>(a.workspace)[blockIdx.x];
+    if (cut.parts < 2) return;
+    const float2* stats = reinterpret_cast<const float2*>(a.workspace + kv_ws_stats(gridDim.x));
+    const float* sums = reinterpret_cast<const float*>(a.workspace + kv_ws_sums(gridDim.x, a.slot_rows));
+    const int rows = cut.npos * a.ratio, shares = (cut.parts - 1) * gridDim.y, share = (blockIdx.x - cut.first) * gridDim.y + blockIdx.y;
+    const int parts = cut.parts, mine = (rows - share + shares - 1) / shares;        // rows share, share + shares, ...
+    int in_slot;                                                     // a row's place in each part, and where it goes
     bf16* out;
     auto find = [&](int i) {
-        int lo = 0, hi = ctas - 1;                                   // the first CTA with i < s_end
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (i < s_end[mid]) hi = mid;
-            else lo = mid + 1;
-        }
-        const KvCut cut = cuts[lo];
-        const int in = i - (s_end[lo] - cut.npos * a.ratio);
-        const int pos = in / a.ratio, head = in - pos * a.ratio;
+        const int row = share + i * shares, pos = row / a.ratio, head = row - pos * a.ratio;
         const int t = cut.two_tiles && pos >= a.tile_pos ? 1 : 0;
         in_slot = 128 * t + (pos - t * a.tile_pos) * a.ratio + head;
-        parts = cut.parts;
-        first = lo;
         out = a.O + ((int64_t)(cut.row0 + pos) * a.Hq + (int64_t)cut.head * a.ratio + head) * D;
     };
-    auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * first + 1 : 2 * (first + p)) * a.slot_rows + in_slot; };
+    auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * cut.first + 1 : 2 * (cut.first + p)) * a.slot_rows + in_slot; };
     // LANES to a row, four channels at a time (two where a warp has no more to give): lane, lane + LANES, ...
     auto by_lanes = [&](auto lanes_tag) {
         constexpr int LANES = decltype(lanes_tag)::value, ROWS = 32 / LANES, V = D / LANES >= 4 ? 4 : 2, N = D / LANES / V;
         const int sub = lane % LANES;
-        for (int i = (blockIdx.x * WARPS + warp) * ROWS + lane / LANES; i < total; i += gridDim.x * WARPS * ROWS) {
+        for (int i = warp * ROWS + lane / LANES; i < mine; i += WARPS * ROWS) {
             find(i);
             float top = -INFINITY;
 #pragma unroll 4
@@ -1330,45 +1303,41 @@ kv_join_kernel(const KvAttnArgs a, int ctas)
             }
         }
     };
-    // measured, whole calls: 37 thousand rows of some two parts (a chunk of 2048) 267 us with a warp to a row, 258 with eight lanes; 3900 rows
-    // of nine parts 154 with a warp, 162 with eight lanes, 156 with a CTA; 256 rows of 148 parts 498 with a warp, 154 with a CTA
-    if (total > (int)gridDim.x * WARPS) return by_lanes(std::integral_constant<int, 8>{});
-    if (total > (int)gridDim.x) return by_lanes(std::integral_constant<int, 32>{});
+    if (mine > WARPS) return by_lanes(std::integral_constant<int, 8>{});
+    if (mine > 1) return by_lanes(std::integral_constant<int, 32>{});
+    if (mine < 1) return;
     constexpr int C = D / 32;
-    for (int i = blockIdx.x; i < total; i += gridDim.x) {
-        find(i);
-        float top = -INFINITY;
-        for (int p = lane; p < parts; p += 32) top = fmaxf(top, stats[part(p)].x);
+    find(0);
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 32) top = fmaxf(top, stats[part(p)].x);
 #pragma unroll
-        for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
-        const float b0 = top == -INFINITY ? 0.0f : top;
-        float o[C] = {}, l = 0.0f;
+    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
+    const float b0 = top == -INFINITY ? 0.0f : top;
+    float o[C] = {}, l = 0.0f;
 #pragma unroll 4
-        for (int p = warp; p < parts; p += WARPS) {
-            const float2 s = stats[part(p)];
-            const float f = ex2_approx(s.x - b0);
-            l += s.y * f;
-            const float* x = sums + part(p) * D + lane * C;
-            float v[C];
-            if constexpr (C == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
-            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
+    for (int p = warp; p < parts; p += WARPS) {
+        const float2 s = stats[part(p)];
+        const float f = ex2_approx(s.x - b0);
+        l += s.y * f;
+        const float* x = sums + part(p) * D + lane * C;
+        float v[C];
+        if constexpr (C == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] += v[c] * f;
+        for (int c = 0; c < C; ++c) o[c] += v[c] * f;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) s_sum[warp][lane * C + c] = o[c];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    if (tid < D) {
+        float sum = 0.0f, weight = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            sum += s_sum[w][tid];
+            weight += s_l[w];
         }
-#pragma unroll
-        for (int c = 0; c < C; ++c) s_sum[warp][lane * C + c] = o[c];
-        if (lane == 0) s_l[warp] = l;
-        __syncthreads();
-        if (tid < D) {
-            float sum = 0.0f, weight = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                sum += s_sum[w][tid];
-                weight += s_l[w];
-            }
-            out[tid] = __float2bfloat16_rn(weight == 0.0f ? 0.0f : sum / weight);
-        }
-        __syncthreads();
+        out[tid] = __float2bfloat16_rn(weight == 0.0f ? 0.0f : sum / weight);
     }
 }
 

@@ -205,12 +205,11 @@ int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensor
         set = true;
     }
     const int ctas = dev->sm_count;
-    if (ctas > gmlp::kKvMostCtas) return GMLP_ERR_UNSUPPORTED;
     int rc = launch_block(gmlp::kv_attention_kernel<D, FEW>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
     if (!join) return GMLP_OK;
-    rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)(ctas * (k.slot_rows > 64 ? 8 : 4))), dim3(gmlp::kKvJoinThreads), 0, st, k, ctas);
+    rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)ctas, k.slot_rows > 64 ? 8 : 4), dim3(gmlp::kKvJoinThreads), 0, st, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_join", st);
     return GMLP_OK;

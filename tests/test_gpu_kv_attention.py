@@ -355,6 +355,53 @@ def test_accuracy_by_the_error_s_norm(reqs, most):
     assert (err / own) ** 0.5 <= most, (err / own) ** 0.5
 
 
+def test_the_most_requests_and_rows():
+    """65535 requests (places of a padded batch among them) that share their pages, and 2^24 rows of one request."""
+    g, D = gen(1), 64
+    k, v = (torch.randn(5, 1, 16, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    cache, B = gmlp.KvCache(k, v), 65535
+    lengths = torch.randint(0, 40, (B,), generator=g, device=DEV).to(torch.int32)
+    table = torch.randint(0, 5, (B, 3), generator=g, device=DEV).to(torch.int32)
+    Q = torch.randn(B, D, generator=g, device=DEV).to(torch.bfloat16)
+    O = gmlp.kv_attention(Q, cache, table, lengths, 1, checked=True)
+    j = torch.arange(48, device=DEV)
+    for lo in range(0, B, 8192):
+        rows = slice(lo, min(B, lo + 8192))
+        kk, vv = (c[table[rows].long(), 0].flatten(1, 2).double() for c in (k, v))
+        s = torch.einsum("bd,bnd->bn", Q[rows].double(), kk) / 8
+        p = torch.where(j < lengths[rows, None], s, -math.inf).softmax(-1).nan_to_num(0.0)
+        want, A = torch.einsum("bn,bnd->bd", p, vv), torch.einsum("bn,bnd->bd", p, vv.abs())
+        E = (torch.einsum("bd,bnd->bn", Q[rows].double().abs(), kk.abs()) / 8).amax(-1, keepdim=True).expand_as(want)
+        assert bool(((O[rows].double() - want).abs() <= P.attention_bound(want, A, E, D, 48)).all())
+    T = 1 << 24
+    Q = torch.randn(T, D, generator=g, device=DEV, dtype=torch.bfloat16)
+    n = torch.tensor([70], dtype=torch.int32, device=DEV)
+    table = torch.arange(5, dtype=torch.int32, device=DEV)[None]
+    O = gmlp.kv_attention(Q, cache, table, n, 1, q_len=T, checked=True)
+    assert int(torch.count_nonzero(O[:T - 70])) == 0
+    kk, vv = (P.rows_of(c, table[0], 70) for c in (k, v))
+    want, A, E = P.attention(Q[T - 200:], kk, vv, 1, 0.125)
+    assert bool(((O[T - 200:].double() - want).abs() <= P.attention_bound(want, A, E, D, 70)).all())
+    O = gmlp.kv_attention(Q, cache, table, n, 1, q_len=T, causal=False, checked=True)
+    for at in (0, 255, 256, T // 2, T - 200):
+        want, A, E = P.attention(Q[at:at + 200], kk, vv, 1, 0.125, causal=False)
+        assert bool(((O[at:at + 200].double() - want).abs() <= P.attention_bound(want, A, E, D, 70)).all())
+
+
+def test_workspaces_of_the_caller():
+    batch = Batch([(3, 2000), (200, 300)], 8, 2, 64, 16, behind=0)
+    want, need = batch.run().clone(), gmlp.kv_workspace_bytes(batch.Q.shape[0], 8, 2, 64)
+    ws = torch.full((need + 512,), 255, dtype=torch.uint8, device=DEV)
+    assert torch.equal(batch.run(workspace=ws[:need]), want)
+    assert bool((ws[need:] == 255).all())                                # nothing behind it is touched
+    for bad, status in ((ws[:need - 1], gmlp.ERR_WORKSPACE), (ws[16:], gmlp.ERR_ALIGN)):
+        with pytest.raises(gmlp.GmlpError) as e:
+            batch.run(workspace=bad)
+        assert e.value.status == status
+    with pytest.raises(ValueError):
+        batch.run(workspace=torch.empty(need, dtype=torch.uint8))
+
+
 def test_refusals_of_the_binding():
     batch = Batch([(2, 40), (3, 20)], 8, 2, 64, 16, behind=0)
     ok = dict(Q=batch.Q, cache=batch.cache, block_table=batch.table, lengths=batch.lengths, n_q_heads=8, q_start=batch.start)

@@ -100,9 +100,11 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
     if (!fits) keys = 0;
     if (report && (!ok || !fits)) report_index(ok ? 6 : 7);
 }
-// Up to this length an item is never cut: a part costs as much as the keys that it saves.  (Where a CTA's stretch is short, items that are
-// longer than it by this much stay whole too.  8 requests of 300 keys: 18.2 us cut, 14.0 whole.)
-constexpr int kKvSnap = 1024;
+// Up to this length an item is never cut: a part costs as much as the keys that it saves.  Items of nearly the same length stay whole too
+// where no CTA then has more than this on top of an equal share.  One token over this many keys, 32 query and 8 key/value heads of 128, cut
+// and whole: 100 requests of 400 keys 65 and 58 us; 16 of 1500 30.4 and 26.7; 16 of 4000 57.8 and 53.7.  52 of 837 to 1402 with two heads
+// and a quarter more per CTA than that were slower whole, 32 against 24.
+constexpr int kKvSnap = 1536;
 enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
 __device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) { return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem); }
 __host__ __device__ constexpr int kv_start(int mode) { return mode == kKvBigItem ? kKvBigStart : (mode == kKvSmallItem ? kKvSmallStart : kKvFewStart); }
@@ -261,6 +263,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     int64_t* s_scan = reinterpret_cast<int64_t*>(stats);
     int64_t* s_rest = s_scan + kKvThreads / 32;
     int* s_start = reinterpret_cast<int*>(s_rest + 1);
+    int2* s_range = reinterpret_cast<int2*>(s_start + 2);                    // shortest and longest item
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -295,18 +298,29 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     // ---------------- this CTA's stretch of the axis ----------------
     const int per = (a.B + kKvThreads - 1) / kKvThreads, b_lo = min(a.B, tid * per), b_hi = min(a.B, b_lo + per);
     int64_t mine = 0;
+    int least = 0x7FFFFFFF, most = 0;                                        // shortest and longest item
     for (int b = b_lo; b < b_hi; ++b) {
         int row0, rows, keys;
         kv_request(a, b, row0, rows, keys, blockIdx.x == 0);
         mine += kv_cost(a, rows, keys, kv_tiles(a, rows));
+        if (rows > 0) {
+            const int mode = kv_mode(a, rows), c = kv_start(mode) + kv_key(mode) * min(keys, 1 << 28);
+            least = min(least, rows > 2 * a.tile_pos ? 1 : c);               // several tiles: of unlike lengths
+            most = max(most, c);
+        }
     }
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
     int64_t upto = mine;
 #pragma unroll
     for (int w = 1; w < 32; w <<= 1) {
         const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, w);
         if (lane >= w) upto += v;
     }
-    if (lane == 31) s_scan[warp] = upto;
+    if (lane == 31) {
+        s_scan[warp] = upto;
+        s_range[warp] = make_int2(least, most);
+    }
     __syncthreads();
     int64_t per_head = 0;
 #pragma unroll
@@ -316,7 +330,6 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
     const int64_t total = per_head * a.Hkv;
     const int64_t stretch = max((total + gridDim.x - 1) / gridDim.x, (int64_t)a.min_stretch);
-    const int64_t snap = kKvSnap + (stretch < 2048 ? stretch : 0);           // longest item that is not cut
     const int64_t lo = stretch * blockIdx.x, hi = min(total, lo + stretch);
     const int head_lo = lo < hi ? (int)(lo / per_head) : 0;
     if (lo < hi) {
@@ -620,6 +633,12 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         bool ok = true;
         if (lo < hi) {
             int head = head_lo, b = s_start[0], tile = s_start[1], window = -1;
+            // No more than stretch / least items, rounded up, start in one stretch: if they take little longer than it, none is cut.
+            // (Worked out here: in every thread it cost the steady loops of long prompts 1 to 2 per cent.)
+            least = __reduce_min_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].x);
+            most = __reduce_max_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].y);
+            const bool even = stretch < 0x40000000 && (int64_t)(((uint32_t)stretch + least - 1) / (uint32_t)least) * most <= stretch + kKvSnap;
+            const int snap = even && most > kKvSnap ? most : kKvSnap;        // longest item that is not cut
             int w_row0 = 0, w_rows = 0, w_keys = 0;                          // this lane's request of the window
             int64_t x = lo - *s_rest;                                        // where the item starts
             while (ok && x < hi) {

@@ -148,6 +148,13 @@ def test_around_the_length_that_is_cut(n, r):
     Batch([(r, n)] * 40, 8, 2, 128, 64).check(only=range(0, 40, 7))
 
 
+@pytest.mark.parametrize("B,n,r", [(18, 1000, 1), (16, 1500, 1), (16, 4000, 1), (17, 4000, 1), (40, 700, 1), (16, 2000, 20), (9, 900, 60)])
+@pytest.mark.parametrize("spread", [0, 1, 100, 400])
+def test_batches_of_nearly_the_same_length(B, n, r, spread):
+    """Whether such items are cut depends on their number and on the shortest and the longest of them."""
+    Batch([(r, n - spread * (b % 3) // 2) for b in range(B)] + [(0, 50)], 32, 8, 128, 64).check()
+
+
 def test_wide_tables_and_uniform_rows():
     batch = Batch([(4, 100), (4, 3), (4, 1500)], 8, 2, 128, 64, extra_width=5000, behind=0)
     O = batch.check()

@@ -8,8 +8,8 @@
 //                                  end.  Bytes bound these, so the probabilities get a second bf16 term (16 bits) for the tensor pipe's spare time;
 //   few   (up to 16 rows, e.g. single tokens): the products are turned round, S^T = K Q^T and O^T += V^T P^T, so that the 128 keys
 //                                  of a block, not 16 rows of 128, are the threads' lanes: a block's softmax takes some 16 exponentials a thread
-//                                  instead of 128 (0.4 us instead of 1.9, two terms as well), which leaves the copies as the bound.  The items of a CTA
-//                                  go to the two tiles in turn, so that one's end and the next one's start overlap.
+//                                  instead of 128 (0.4 us instead of 1.9, two terms as well), which leaves the copies as the bound.  The
+//                                  items of a CTA go to the two tiles in turn, so that one's end and the next one's start overlap.
 // Order and split.  All items lie end to end on one axis, heads outermost, an item as long as the keys that its last position sees plus
 // a constant; every CTA (one per SM) takes an equal stretch of the axis, computed by itself from the lengths on the device (the host knows
 // none of them).  So a decode batch of ragged lengths, one long conversation and a prompt's chunk all load the GPU evenly, without a plan
@@ -20,8 +20,8 @@
 //               are zeros in V, which a probability of 0 would not hide if they were NaN
 //   warp 1      MMA issuer:   S_t = Q_t K^T (TMEM columns 128 t), O_t += P_t V (columns 256 + 128 t)
 //   warp 2      walks the axis, hands items to the others through a ring, loads Q
-//   warp 3      looks for pages outside of the cache, and mends V blocks that hold keys which some row must not see: rows past the request's end become zeros, numbers that are none
-//               become 0 and are added by the epilogue for the rows that see them
+//   warp 3      looks for pages outside of the cache, and mends V blocks that hold keys which some row must not see: rows past the
+//               request's end become zeros, numbers that are none become 0 and are added by the epilogue for the rows that see them
 //   warps 4..7  softmax and epilogue of tile A, warps 8..11 of tile B: thread = row.  As in gqa_attention.cuh: scores are read once, the base
 //               of the exponentials moves only when a row's sum of a block passes 2^10, P goes back to TMEM over the scores.
 // Every wait is bounded.
@@ -75,8 +75,12 @@ struct KvCut {
     int head, row0, npos, two_tiles, pad[2];
 };
 __host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ctas * sizeof(KvCut) + 255) & ~(uint64_t)255; }
-__host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) { return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255); }
-__host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) { return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4; }
+__host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) {
+    return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255);
+}
+__host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) {
+    return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4;
+}
 
 struct KvItem {
     int blk0, blk1;                  // blocks of keys; none: rows that see no key
@@ -106,7 +110,9 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
 // and a quarter more per CTA than that were slower whole, 32 against 24.
 constexpr int kKvSnap = 1536;
 enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
-__device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) { return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem); }
+__device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) {
+    return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem);
+}
 __host__ __device__ constexpr int kv_start(int mode) { return mode == kKvBigItem ? kKvBigStart : (mode == kKvSmallItem ? kKvSmallStart : kKvFewStart); }
 __host__ __device__ constexpr int kv_key(int mode) { return mode == kKvBigItem ? kKvBigKey : (mode == kKvSmallItem ? kKvSmallKey : kKvFewKey); }
 __device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int rows) { return (rows + 2 * a.tile_pos - 1) / (2 * a.tile_pos); }
@@ -501,7 +507,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (leader) {
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)
-                            ptx::umma_bf16_halves(tmem_base + 128u * (uint32_t)t + (uint32_t)(kKvFew * (n & 1)), ad[k], bd[k], desc_hi, kIdescFewQK, k != 0 ? 1u : 0u);
+                            ptx::umma_bf16_halves(tmem_base + 128u * (uint32_t)t + (uint32_t)(kKvFew * (n & 1)), ad[k], bd[k], desc_hi,
+                                                  kIdescFewQK, k != 0 ? 1u : 0u);
                         ptx::umma_commit(s_full0 + 8 * (2 * t + (n & 1)));
                         ptx::umma_commit(kv_empty0 + 8 * k_slot);
                     }
@@ -767,7 +774,9 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         uint4 v = make_uint4(0, 0, 0, 0);
                         if (c < end * 8) {
                             v = rows[h * 1024 + c];
-                            if (!(bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) || bf16_pair_not_finite(v.w))) continue;
+                            if (!(bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) ||
+                                  bf16_pair_not_finite(v.w)))
+                                continue;
                             none = true;
                             uint32_t* w = &v.x;
 #pragma unroll

@@ -177,14 +177,17 @@ int kv_append_impl(const gmlp_kv_append_args* a) {
 constexpr int64_t kKvMostKeys = (int64_t)1 << 30;        // of one request: positions stay well inside 31 bits
 constexpr int kKvMaxRatio = 128;                         // query heads to a key/value head: a tile's rows
 int check_kv_attention(int64_t B, int64_t T, int Hq, int Hkv, int64_t width, int page_size) {
-    if (B < 0 || B > 65535 || T < 0 || T > kRopeMaxRows || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq > 65535 || width < 1 || width > kKvMostKeys / page_size)
+    if (B < 0 || B > 65535 || T < 0 || T > kRopeMaxRows || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq > 65535 || width < 1 ||
+        width > kKvMostKeys / page_size)
         return GMLP_ERR_SHAPE;
     return Hq / Hkv > kKvMaxRatio ? GMLP_ERR_UNSUPPORTED : GMLP_OK;
 }
 
 // Rows of a partial result: a big item's two tiles of 128, or what all rows of the call make.
 int kv_slot_rows(int64_t T, int ratio) { return T * ratio <= 128 ? (int)(T * ratio) : 256; }
-uint64_t kv_attention_workspace(int64_t T, int Hq, int Hkv, int head_dim, int sms) { return gmlp::kv_ws_bytes(sms, kv_slot_rows(T, Hq / Hkv), head_dim); }
+uint64_t kv_attention_workspace(int64_t T, int Hq, int Hkv, int head_dim, int sms) {
+    return gmlp::kv_ws_bytes(sms, kv_slot_rows(T, Hq / Hkv), head_dim);
+}
 
 bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, int64_t T, int box_heads, int box_rows) {
     const cuuint64_t gdim[3] = {(cuuint64_t)head_dim, (cuuint64_t)Hq, (cuuint64_t)T};
@@ -197,15 +200,18 @@ bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, in
 }
 
 template <int D, bool FEW>
-int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV, const gmlp::KvAttnArgs& k, bool join, cudaStream_t st) {
+int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                        const gmlp::KvAttnArgs& k, bool join, cudaStream_t st) {
     bool& set = dev->kv_attr_set[2 * (D == 128) + FEW];
     if (!set) {
-        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
+        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
         set = true;
     }
     const int ctas = dev->sm_count;
-    int rc = launch_block(gmlp::kv_attention_kernel<D, FEW>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
+    int rc = launch_block(gmlp::kv_attention_kernel<D, FEW>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ,
+                          tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
     if (!join) return GMLP_OK;
@@ -272,7 +278,8 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     k.min_stretch = 768;
     const uint64_t cache_rows = (uint64_t)a->cache.n_pages * (uint64_t)k.Hkv * (uint64_t)k.page_size;
     CUtensorMap tmQ, tmQfew, tmK, tmV;
-    if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_kv_query(&tmQfew, a->Q, D, k.Hq, a->T, ratio, few_pos) || !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
+    if (!encode_kv_query(&tmQ, a->Q, D, k.Hq, a->T, ratio, q_pos) || !encode_kv_query(&tmQfew, a->Q, D, k.Hq, a->T, ratio, few_pos) ||
+        !encode_2d(&tmK, a->cache.k, (uint64_t)D, cache_rows, 64, (uint32_t)k.box) ||
         !encode_2d(&tmV, a->cache.v, (uint64_t)D, cache_rows, 64, (uint32_t)k.box))
         return GMLP_ERR_LAUNCH;
     prof_begin(st);
@@ -280,7 +287,8 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     const int mode = a->T <= k.few_pos ? gmlp::kKvFewItem : (a->T <= k.tile_pos ? gmlp::kKvSmallItem : gmlp::kKvBigItem);
     const bool join = gmlp::kv_start(mode) + a->table_width * k.page_size * gmlp::kv_key(mode) > gmlp::kKvSnap;
 #define GMLP_KV_ATTENTION(D) \
-    (few ? launch_kv_attention<D, true>(dev, tmQ, tmQfew, tmK, tmV, k, join, st) : launch_kv_attention<D, false>(dev, tmQ, tmQfew, tmK, tmV, k, join, st))
+    (few ? launch_kv_attention<D, true>(dev, tmQ, tmQfew, tmK, tmV, k, join, st)                                                            \
+         : launch_kv_attention<D, false>(dev, tmQ, tmQfew, tmK, tmV, k, join, st))
     rc = D == 128 ? GMLP_KV_ATTENTION(128) : GMLP_KV_ATTENTION(64);
     if (rc != GMLP_OK) return rc;
     return finish_checked(dev, a->flags, st);

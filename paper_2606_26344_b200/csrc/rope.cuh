@@ -7,8 +7,8 @@
 // 131072 would be off by 2^-8 radians: half a unit in the last place of its 17 bits before the point.)
 //
 // What bounds it: bytes, one read and one write of each row.  A pair's cosine and sine (some 40 instructions) serve all heads of a
-// token, so a CTA takes whole tokens and computes them once, into shared memory; a thread then keeps those of its channels and goes over the heads, 16
-// bytes or twice 16 at a time, 64 bytes of loads in flight each, four CTAs per SM.
+// token, so a CTA takes whole tokens and computes them once, into shared memory; a thread then keeps those of its channels and goes
+// over the heads, 16 bytes or twice 16 at a time, 64 bytes of loads in flight each, four CTAs per SM.
 // 8191 tokens of 64 heads of 128 (268 MB both ways, floor 41.6 us): 69 us with 128 bytes in flight (two CTAs per SM), 51 with one token per
 // CTA, 45 now; interleaved in units of one access 54.
 #pragma once

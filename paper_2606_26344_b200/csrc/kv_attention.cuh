@@ -1077,6 +1077,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         const float v = __bfloat162float(a.v[(((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + r]);
                         if (!(v - v == 0.0f)) o += v;
                     }
+                    __syncwarp();
                 }
                 if (r < D) {
                     if (whole) *out = __float2bfloat16_rn(sum == 0.0f ? 0.0f : __fdividef(o, sum));
@@ -1211,20 +1212,22 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     } else {
                         ptx::tmem_ld_wait();
                     }
-                    if (!mine) continue;
-                    if (opaque(it.slot) < 0) {
+                    if (mine) {
+                        if (opaque(it.slot) < 0) {
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            uint32_t pk[4];
+                            for (int w = 0; w < 2; ++w) {
+                                uint32_t pk[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) pk[k] = zero ? 0u : pack_bf16x2(o[8 * w + 2 * k] * inv_l, o[8 * w + 2 * k + 1] * inv_l);
-                            *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                                for (int k = 0; k < 4; ++k) pk[k] = zero ? 0u : pack_bf16x2(o[8 * w + 2 * k] * inv_l, o[8 * w + 2 * k + 1] * inv_l);
+                                *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < 4; ++w)
+                                *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
                         }
-                    } else {
-#pragma unroll
-                        for (int w = 0; w < 4; ++w)
-                            *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
                     }
+                    __syncwarp();                                            // the next loads from TMEM are the whole warp's
                 }
                 if (odd && mine) {                                           // the row that was just written gets what V held in place of numbers
 #pragma unroll 1

@@ -1229,7 +1229,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     __syncwarp();                                            // the next loads from TMEM are the whole warp's
                 }
-                if (odd && mine) {                                           // the row that was just written gets what V held in place of numbers
+                // the row that was just written gets what V held in place of numbers (not a row of zeros: the join tells for a cut item's)
+                if (odd && mine && !(zero && it.slot < 0)) {
 #pragma unroll 1
                     for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
                         const int page = table[j / a.page_size];

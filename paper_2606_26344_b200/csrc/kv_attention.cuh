@@ -25,6 +25,14 @@
 //   warps 4..7  softmax and epilogue of tile A, warps 8..11 of tile B: thread = row.  As in gqa_attention.cuh: scores are read once, the base
 //               of the exponentials moves only when a row's sum of a block passes 2^10, P goes back to TMEM over the scores.
 // Every wait is bounded.
+//
+// Values of any size.  O is a sum of p V before it is divided by the sum of p, and p may pass 1 (the base moves late), so large values pass the
+// largest float although the result does not; an infinity that a row sees in a block that is not mended may become NaN, since the second
+// term of its probability may be negative or 0.  An epilogue that finds such a sum asks for a second pass over its CTA's stretch (`careful`):
+// the same items one at a time, with every block of V mended and multiplied by 2^-48 (the sums of p stay below 2^40), and what is not finite
+// from the first pass is written anew; the rest stays.  Parts of cut items are divided by their own sum of p, so that the join weighs means.
+// Calls without a second pass pay for the test, the join's weights and the longer code: 256 requests of 200 keys 90 us, 87 before; one token over
+// 2^20 keys 102 and 99; 64 of 4096 keys 179 and 178; a prompt of 8192 the same.  A second pass takes three to five times as long as a first.
 #pragma once
 #include <type_traits>
 #include <cuda.h>
@@ -61,6 +69,7 @@ constexpr int kKvBigKey = 4, kKvSmallKey = 3, kKvFewKey = 2;
 constexpr int kKvBigStart = 448 * kKvBigKey, kKvSmallStart = 384 * kKvSmallKey, kKvFewStart = 256 * kKvFewKey;
 constexpr int kKvRegsLight = 72, kKvRegsSoftmax = 216;
 constexpr int kKvKernelId = 30;
+constexpr float kKvCareful = 0x1p-48f;                       // what the second pass multiplies V by
 constexpr uint32_t kKvWaitLimit = 8;                         // some 20 s: some waits last as long as an item
 __host__ __device__ constexpr int kv_slots(int D) { return D == 128 ? 5 : 10; }
 __host__ __device__ constexpr uint32_t kv_tile_bytes(int D) { return 128u * D * 2; }
@@ -69,7 +78,7 @@ constexpr uint32_t kKvRegion = 32768;            // of a tile: Q, and in few ite
 constexpr uint32_t kv_attn_smem(int D) { return 2 * kKvRegion + kv_slots(D) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
 
 // Workspace: one descriptor per CTA - the cut item that its stretch ends in - then base and weight of the rows of each of its two partial
-// results, then their sums.
+// results, then their rows, divided by the weight.
 struct KvCut {
     int parts, first;                // parts (less than two: none), the CTA that has the first of them
     int head, row0, npos, two_tiles, pad[2];
@@ -90,7 +99,8 @@ struct KvItem {
     int slot;                        // of the partial result, or -1: the rows' final values
     int last;                        // no more items (this one is none)
     int mode, tile;                  // kKvBigItem ..; the tile of a few item
-    int pad[4];
+    int careful;                     // the second pass
+    int pad[3];
 };
 
 // Request b: its first row, rows and keys; what the arrays hold outside of their ranges is left out (and reported by one CTA).
@@ -110,6 +120,7 @@ __device__ __forceinline__ void kv_request(const KvAttnArgs& a, int b, int& row0
 // and a quarter more per CTA than that were slower whole, 32 against 24.
 constexpr int kKvSnap = 1536;
 enum { kKvBigItem = 0, kKvSmallItem = 1, kKvFewItem = 2 };
+constexpr uint32_t kKvHidden = 1, kKvSeen = 2;               // of keys that some row must not see; in the second pass, of the others
 __device__ __forceinline__ int kv_mode(const KvAttnArgs& a, int npos) {
     return npos <= a.few_pos ? kKvFewItem : (npos <= a.tile_pos ? kKvSmallItem : kKvBigItem);
 }
@@ -173,6 +184,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap,
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool is_finite(float x) { return x - x == 0.0f; }
+__device__ __forceinline__ uint32_t bf16_pair_times(uint32_t w, float f) {
+    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), __float2bfloat162_rn(f));
+    return *reinterpret_cast<const uint32_t*>(&p);
 }
 __device__ __forceinline__ bool bf16_pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
@@ -259,12 +275,16 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const uint32_t stats_full = item_checked0 + 8 * kKvRing, stats_done = stats_full + 8;
     const uint32_t agree0 = stats_done + 8;                                  // [tile] the warps of a few item's tile
     constexpr int BARS = 2 * SLOTS + 20 + 2 * kKvMends + 4 * kKvRing;
-    volatile uint32_t* hidden = reinterpret_cast<volatile uint32_t*>(bars + BARS);   // [ring] V held numbers that are none
+    volatile uint32_t* hidden = reinterpret_cast<volatile uint32_t*>(bars + BARS);   // [ring] V held numbers that are none (kKvHidden, kKvSeen)
     volatile uint32_t* odd_pages = hidden + kKvRing;                         // [ring] the table has pages outside of the cache
     volatile uint32_t* votes = odd_pages + kKvRing;                          // [tile][parity][4 warps]
     uint32_t* tmem_slot = const_cast<uint32_t*>(votes) + 16;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert(sizeof(KvItem) * kKvRing + 8 * BARS + 4 * (2 * kKvRing + 18) <= 1024, "items and barriers");
+    volatile int* redo = abort_flag + 1;                                     // some O was not finite
+    static_assert(sizeof(KvItem) * kKvRing + 8 * BARS + 4 * (2 * kKvRing + 19) <= 1024, "items and barriers");
+    // (second pass) [channel]: the sum of the numbers that are none in V of keys that all rows of the item see.  One item at a time, so that
+    // what the other kinds of items exchange is free.
+    auto seen_by_all = [&](int mode) { return mode == kKvFewItem ? reinterpret_cast<float*>(stats) : exchange; };
     // for the start only, in the same place as `stats`: sums of costs, the place within the first item, its request and tile
     int64_t* s_scan = reinterpret_cast<int64_t*>(stats);
     int64_t* s_rest = s_scan + kKvThreads / 32;
@@ -288,6 +308,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         init(item_checked0, kKvRing, 1);
         init(stats_full, 4, 4);
         *abort_flag = 0;
+        *redo = 0;
         ptx::fence_mbar_init();
         ptx::fence_proxy_async_smem();
         ptx::prefetch_tensormap(&tmQ);
@@ -368,17 +389,34 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;                                   // S_t at + 128 t, O_t at + 256 + 128 t
 
+    // All warps meet here at the end of a pass, at item i, which is the last, or after a wait that ran out.  True: there is a second pass, from the
+    // next item on.
+    auto next_pass = [&](uint32_t& i) -> bool {
+        ptx::tc_fence_before_sync();
+        asm volatile("bar.sync 0;" ::: "memory");
+        ptx::tc_fence_after_sync();
+        if (__builtin_expect(*redo == 0 || *abort_flag != 0, 1) || items[i % kKvRing].careful) return false;
+        __syncwarp();
+        if (lane == 0 && warp == 3) {                                        // (one phase of each of the place's barriers per use)
+            ptx::mbar_arrive(item_checked0 + 8 * (i % kKvRing));
+            ptx::mbar_arrive(item_fixed0 + 8 * (i % kKvRing));
+        }
+        if (lane == 0 && warp != 2) ptx::mbar_arrive(item_empty0 + 8 * (i % kKvRing));
+        ++i;
+        return true;
+    };
+
     if (warp < 4) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kKvRegsLight));
-      // the item in ring place i; false when there is no more
+      auto item_done = [&](uint32_t i) {
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * (i % kKvRing));
+      };
+      // the item in ring place i; false when there is no more in this pass
       auto next_item = [&](uint32_t i, KvItem& it) -> bool {
           if (!kv_wait(item_full0 + 8 * (i % kKvRing), (i / kKvRing) & 1u, abort_flag, 1)) return false;
           it = items[i % kKvRing];
           return it.last == 0;
-      };
-      auto item_done = [&](uint32_t i) {
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * (i % kKvRing));
       };
       // the first key of the item that some row of it must not see
       auto first_hidden = [&](const KvItem& it) { return min(max(it.seen0, 0), it.keys); };
@@ -392,7 +430,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const uint32_t box_bytes = (uint32_t)a.box * 128u;
         const int my = lane % boxes, half = lane / boxes;                    // this lane's box of a block and half of the channels
         const bool copies = lane < boxes * HALVES;
-        for (uint32_t i = 0; next_item(i, it); ++i) {
+        uint32_t i = 0;
+        do for (; next_item(i, it); ++i) {
             const int32_t* table = a.table + (int64_t)it.b * a.width;
             // the page of this lane's box in block j: -1 past the request's end, -2 outside of the cache
             auto page_of = [&](int j, int& place) -> int {
@@ -403,7 +442,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const int page = table[index];
                 return page >= 0 && page < a.n_pages ? page : -2;
             };
-            const int open = first_hidden(it) / kKvBlock;                    // blocks before this one need no mending
+            const int open = it.careful ? 0 : first_hidden(it) / kKvBlock;   // blocks before this one need no mending
             int place_next = 0, page_next = page_of(it.blk0, place_next);
             bool ok = true;
 #pragma unroll 1
@@ -438,7 +477,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             if (!ok) break;
             item_done(i);
-        }
+        } while (next_pass(i));
         __syncwarp();
       } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
@@ -485,11 +524,12 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             p_phase ^= 1u << at;
             return ok;
         };
-        for (uint32_t i = 0; next_item(i, it); ++i) {
+        uint32_t i = 0;
+        do for (; next_item(i, it); ++i) {
             const int blocks = it.blk1 - it.blk0;
             if (blocks == 0) { item_done(i); continue; }
             const bool big = it.mode == kKvBigItem;
-            const int open = first_hidden(it) / kKvBlock - it.blk0;          // blocks of the item before this one need no mending
+            const int open = it.careful ? 0 : first_hidden(it) / kKvBlock - it.blk0;     // blocks of the item before this one need no mending
             uint32_t k_slot = 0, v_slot = 0;
             bool ok;
             if constexpr (FEW) if (it.mode == kKvFewItem) {
@@ -630,24 +670,27 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             if (!ok) break;
             item_done(i);
-        }
+        } while (next_pass(i));
         __syncwarp();
       } else if (warp == 2) {
         // ---------------- items and Q ----------------
         KvCut* cuts = reinterpret_cast<KvCut*>(a.workspace);
         KvCut cut = {};
         uint32_t i = 0, loads = 0, few_items = 0;                            // loads: bits, parity of [tile]'s
-        bool ok = true;
-        if (lo < hi) {
-            int head = head_lo, b = s_start[0], tile = s_start[1], window = -1;
+        bool ok = true, careful = false;
+        const int b_first = s_start[0], tile_first = s_start[1];
+        const int64_t x_first = lo - *s_rest;                                // where the first item starts
+        least = __reduce_min_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].x);
+        most = __reduce_max_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].y);
+        do {
+          if (lo < hi) {
+            int head = head_lo, b = b_first, tile = tile_first, window = -1;
             // No more than stretch / least items, rounded up, start in one stretch: if they take little longer than it, none is cut.
             // (Worked out here: in every thread it cost the steady loops of long prompts 1 to 2 per cent.)
-            least = __reduce_min_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].x);
-            most = __reduce_max_sync(0xFFFFFFFFu, s_range[lane % (kKvThreads / 32)].y);
             const bool even = stretch < 0x40000000 && (int64_t)(((uint32_t)stretch + least - 1) / (uint32_t)least) * most <= stretch + kKvSnap;
             const int snap = even && most > kKvSnap ? most : kKvSnap;        // longest item that is not cut
             int w_row0 = 0, w_rows = 0, w_keys = 0;                          // this lane's request of the window
-            int64_t x = lo - *s_rest;                                        // where the item starts
+            int64_t x = x_first;
             while (ok && x < hi) {
                 if (b >= a.B) { b = 0; ++head; tile = 0; continue; }
                 if (window != b / 32) {
@@ -687,7 +730,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     const int tile_of = mode == kKvFewItem ? (int)(few_items & 1u) : 0;
                     const uint32_t p = i % kKvRing;
-                    if (!kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 8)) { ok = false; break; }
+                    // a free place; in the second pass all of them
+                    for (uint32_t n = i; ok && n < i + (careful ? kKvRing : 1); ++n)
+                        ok = kv_wait(item_empty0 + 8 * (n % kKvRing), ((n / kKvRing) & 1u) ^ 1u, abort_flag, 8);
+                    if (!ok) break;
                     if (lane == 0) {
                         KvItem it;
                         it.blk0 = blk0;
@@ -702,6 +748,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         it.last = 0;
                         it.mode = mode;
                         it.tile = tile_of;
+                        it.careful = careful;
                         items[p] = it;
                         hidden[p] = 0;
                         ptx::mbar_arrive(item_full0 + 8 * p);
@@ -728,22 +775,26 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 x += cost;
                 ++tile;
             }
-        }
-        if (lane == 0) cuts[blockIdx.x] = cut;
-        const uint32_t p = i % kKvRing;
-        if (ok && kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 10)) {
-            if (lane == 0) {
-                items[p].last = 1;
-                ptx::mbar_arrive(item_full0 + 8 * p);
-            }
-        }
+          }
+          const uint32_t p = i % kKvRing;
+          if (lane == 0) cuts[blockIdx.x] = cut;
+          if (ok && kv_wait(item_empty0 + 8 * p, ((i / kKvRing) & 1u) ^ 1u, abort_flag, 10)) {
+              if (lane == 0) {
+                  items[p].last = 1;
+                  items[p].careful = careful;
+                  ptx::mbar_arrive(item_full0 + 8 * p);
+              }
+          }
+          __syncwarp();
+          careful = true;
+        } while (next_pass(i));
         __syncwarp();
       } else {
         // ---------------- V mender ----------------
         KvCursor<SLOTS> at = {1, 0};
-        uint32_t n_fixed = 0;
+        uint32_t n_fixed = 0, i = 0;
         KvItem it;
-        for (uint32_t i = 0; next_item(i, it); ++i) {
+        do for (; next_item(i, it); ++i) {
             bool pages = false;                                              // some outside of the cache
             if (it.blk1 > it.blk0) {
                 const int32_t* table = a.table + (int64_t)it.b * a.width;
@@ -757,9 +808,15 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 ptx::mbar_arrive(item_checked0 + 8 * (i % kKvRing));
             }
             const int first = first_hidden(it);
-            const int from = max(it.blk0, first / kKvBlock);
+            const int from = it.careful ? it.blk0 : max(it.blk0, first / kKvBlock);
+            float* of_all = seen_by_all(it.mode);
+            if (__builtin_expect(it.careful, 0)) {
+#pragma unroll 1
+                for (int c = lane; c < D; c += 32) of_all[c] = 0.0f;
+                __syncwarp();
+            }
             at.skip(2u * (uint32_t)max(0, min(from, it.blk1) - it.blk0));
-            bool ok = true, none = false;
+            bool ok = true, none = false, none_seen = false;
 #pragma unroll 1
             for (int j = from; j < it.blk1; ++j) {
                 // (the producer has filled the slot anew: before that, its barrier's parity could be that of an older use)
@@ -767,6 +824,37 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     !kv_wait(kv_full0 + 8 * at.slot, at.phase, abort_flag, 11)) { ok = false; break; }
                 const int r0 = max(0, first - j * kKvBlock), end = it.keys - j * kKvBlock;       // rows from r0 on; from `end` on none
                 uint4* rows = reinterpret_cast<uint4*>(fifo_ptr + at.slot * TILE);               // [half][key][16 B]
+                if (__builtin_expect(it.careful, 0)) {
+#pragma unroll 1
+                    for (int c = lane; c < HALVES * kKvBlock * 8; c += 32) {
+                        const int key = (c >> 3) & (kKvBlock - 1);
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (key < end) {
+                            v = rows[c];
+                            if (bf16_pair_not_finite(v.x) || bf16_pair_not_finite(v.y) || bf16_pair_not_finite(v.z) || bf16_pair_not_finite(v.w)) {
+                                volatile uint16_t* row = reinterpret_cast<volatile uint16_t*>(rows + c);
+                                float* sum = of_all + (c >> 10) * 64 + ((c ^ key) & 7) * 8;      // (16 bytes of a row change places by its number)
+#pragma unroll 1
+                                for (int k = 0; k < 8; ++k) {
+                                    const float x = __uint_as_float((uint32_t)row[k] << 16);
+                                    if (is_finite(x)) continue;
+                                    if (key < r0) {
+                                        atomicAdd(sum + k, x);
+                                        none_seen = true;
+                                    } else {
+                                        none = true;
+                                    }
+                                    row[k] = 0;
+                                }
+                                asm volatile("" ::: "memory");
+                                v = rows[c];
+                            }
+                            v = make_uint4(bf16_pair_times(v.x, kKvCareful), bf16_pair_times(v.y, kKvCareful), bf16_pair_times(v.z, kKvCareful),
+                                           bf16_pair_times(v.w, kKvCareful));
+                        }
+                        rows[c] = v;
+                    }
+                } else
 #pragma unroll 1
                 for (int c = r0 * 8 + lane; c < kKvBlock * 8; c += 32) {
 #pragma unroll
@@ -796,12 +884,13 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             if (!ok) break;
             none = __any_sync(0xFFFFFFFFu, none);
+            none_seen = __any_sync(0xFFFFFFFFu, none_seen);
             if (lane == 0) {
-                if (none) hidden[i % kKvRing] = 1;
+                if (none || none_seen) hidden[i % kKvRing] = (none ? kKvHidden : 0u) | (none_seen ? kKvSeen : 0u);
                 ptx::mbar_arrive(item_fixed0 + 8 * (i % kKvRing));
             }
             item_done(i);
-        }
+        } while (next_pass(i));
         __syncwarp();
       }
     } else {
@@ -1027,7 +1116,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * (2 * t + buf));
             }
-            bool odd = false;
+            uint32_t odd = 0;
             if (blocks > 0) {
                 // the rows' weights, summed over the warp's keys: at each exchange a lane keeps half of its rows, in the end row lane / 2
 #pragma unroll
@@ -1046,7 +1135,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!kv_wait(o_full0 + 8 * (2 * t + buf), ((o_phase >> buf) & 1u) ^ 1u, abort_flag, 14)) return false;
                 ptx::tc_fence_after_sync();
                 if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) return false;
-                odd = hidden[ring] != 0;
+                odd = hidden[ring];
             }
             const bool whole = it.slot < 0;
             const int64_t part = (int64_t)it.slot * a.slot_rows;
@@ -1061,27 +1150,37 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (lane < rows)
                     (reinterpret_cast<float2*>(a.workspace + kv_ws_stats(gridDim.x)) + part)[lane] = make_float2(base_n, (w.x + w.y) + (w.z + w.w));
             }
+            const bool careful = it.careful != 0;
+            const float of_all = odd & kKvSeen ? seen_by_all(kKvFewItem)[r] : 0.0f;
+            bool not_finite = false;
             int pos = 0, head = 0;
 #pragma unroll 1
             for (int n = 0; n < rows; ++n) {
-                float o = blocks > 0 ? tmem_ld_32x1(o_addr + (uint32_t)n) : 0.0f;
+                const float o = blocks > 0 ? tmem_ld_32x1(o_addr + (uint32_t)n) : 0.0f;
                 const float4 w = *reinterpret_cast<const float4*>(weights + 4 * n);
                 const float sum = blocks > 0 ? (w.x + w.y) + (w.z + w.w) : 0.0f;             // 0: nothing was seen
                 ptx::tmem_ld_wait();
-                if (odd && r < D) {
+                not_finite |= !is_finite(o) && is_finite(sum) && sum != 0.0f;
+                float value = sum == 0.0f ? 0.0f : __fdividef(o, sum);
+                if (__builtin_expect(careful, 0)) value = value * (1.0f / kKvCareful) + of_all;
+                if ((odd & kKvHidden) && r < D) {
                     const int end = min(a.causal ? min(max(it.seen0 + pos, 0), it.keys) : it.keys, it.blk1 * kKvBlock);
 #pragma unroll 1
                     for (int j = max(first, it.blk0 * kKvBlock); j < end; ++j) {
                         const int page = table[j / a.page_size];
                         if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
                         const float v = __bfloat162float(a.v[(((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D + r]);
-                        if (!(v - v == 0.0f)) o += v;
+                        if (!is_finite(v)) value += v;
                     }
                     __syncwarp();
                 }
                 if (r < D) {
-                    if (whole) *out = __float2bfloat16_rn(sum == 0.0f ? 0.0f : __fdividef(o, sum));
-                    else *sums = o;
+                    // (in the second pass only what was not finite)
+                    if (whole) {
+                        if (!careful || !is_finite(__bfloat162float(*out))) *out = __float2bfloat16_rn(sum == 0.0f ? 0.0f : value);
+                    } else {
+                        if (!careful || !is_finite(*sums)) *sums = value;
+                    }
                 }
                 out += D;
                 sums += D;
@@ -1091,13 +1190,15 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     out += (int64_t)(a.Hq - a.ratio) * D;
                 }
             }
+            if (not_finite && r < D && !careful) *redo = 1;
             ptx::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * ring);
             return true;
         };
 
-        for (uint32_t i = 0;; ++i) {
+        uint32_t i = 0;
+        do for (;; ++i) {
             const uint32_t ring = i % kKvRing, ring_phase = (i / kKvRing) & 1u;
             if (!kv_wait(item_full0 + 8 * ring, ring_phase, abort_flag, 12)) break;
             const KvItem& it = items[ring];                                  // stays until this warp lets it go
@@ -1159,10 +1260,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!kv_wait(o_full0 + 16 * t, (o_phase & 1u) ^ 1u, abort_flag, 14)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
             }
-            bool odd = false;                                                // numbers that are none, taken out of V
+            uint32_t odd = 0;                                                // numbers that are none, taken out of V
             if (blocks > 0) {
                 if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) { ok = false; break; }
-                odd = hidden[ring] != 0;
+                odd = hidden[ring];
             }
 
             // Small items of several blocks: both tiles hold sums of the same rows.  Tile B's warps hand base and weight over, tile A's (which may
@@ -1199,38 +1300,69 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const bool zero = l_run == 0.0f;                             // nothing was seen
                 const float inv_l = 1.0f / l_run;
                 if (it.slot >= 0 && mine) reinterpret_cast<float2*>(a.workspace + kv_ws_stats(gridDim.x))[part] = make_float2(m_use, l_run);
+                if (__builtin_expect(opaque(it.careful), 0)) {
+                    // what was not finite in the first pass; few calls come here: short code, a channel at a time
+                    const float* of_all = seen_by_all(kKvBigItem);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    float o[16];
-                    if (opaque(n_steps) > 0) tmem_ld_32x16(o_addr + 128u * (uint32_t)t + c, o);
-                    if (opaque(both)) {
-                        float o1[16];
-                        tmem_ld_32x16(o_addr + 128u + c, o1);
+                    for (int c = 0; c < D; ++c) {
+                        float o = 0.0f, o1 = 0.0f;
+                        if (opaque(n_steps) > 0) o = tmem_ld_32x1(o_addr + 128u * (uint32_t)t + c);
+                        if (opaque(both)) o1 = tmem_ld_32x1(o_addr + 128u + c);
                         ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = o[k] * f_mine + o1[k] * f_other;
-                    } else {
-                        ptx::tmem_ld_wait();
-                    }
-                    if (mine) {
-                        if (opaque(it.slot) < 0) {
-#pragma unroll
-                            for (int w = 0; w < 2; ++w) {
-                                uint32_t pk[4];
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) pk[k] = zero ? 0u : pack_bf16x2(o[8 * w + 2 * k] * inv_l, o[8 * w + 2 * k + 1] * inv_l);
-                                *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                        if (both) o = o * f_mine + o1 * f_other;
+                        float value = zero ? 0.0f : o * inv_l * (1.0f / kKvCareful);
+                        if ((odd & kKvSeen) && !(zero && it.slot < 0)) value += of_all[c];
+                        if (mine) {
+                            if (it.slot < 0) {
+                                if (!is_finite(__bfloat162float(out[c]))) out[c] = __float2bfloat16_rn(value);
+                            } else if (!is_finite(sums[c])) {
+                                sums[c] = value;
                             }
-                        } else {
-#pragma unroll
-                            for (int w = 0; w < 4; ++w)
-                                *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
                         }
+                        __syncwarp();
                     }
-                    __syncwarp();                                            // the next loads from TMEM are the whole warp's
+                } else {
+                    uint64_t test = pack_f32x2(0.0f, 0.0f);                  // NaN once some O is not finite
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        float o[16];
+                        if (opaque(n_steps) > 0) tmem_ld_32x16(o_addr + 128u * (uint32_t)t + c, o);
+                        if (opaque(both)) {
+                            float o1[16];
+                            tmem_ld_32x16(o_addr + 128u + c, o1);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = o[k] * f_mine + o1[k] * f_other;
+                        } else {
+                            ptx::tmem_ld_wait();
+                        }
+                        if (mine) {
+#pragma unroll
+                            for (int k = 0; k < 16; k += 2) test = fma_f32x2(pack_f32x2(o[k], o[k + 1]), pack_f32x2(0.0f, 0.0f), test);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = zero ? 0.0f : o[k] * inv_l;
+                            if (opaque(it.slot) < 0) {
+#pragma unroll
+                                for (int w = 0; w < 2; ++w) {
+                                    uint32_t pk[4];
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) pk[k] = pack_bf16x2(o[8 * w + 2 * k], o[8 * w + 2 * k + 1]);
+                                    *reinterpret_cast<uint4*>(out + c + 8 * w) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int w = 0; w < 4; ++w)
+                                    *reinterpret_cast<float4*>(sums + c + 4 * w) = make_float4(o[4 * w], o[4 * w + 1], o[4 * w + 2], o[4 * w + 3]);
+                            }
+                        }
+                        __syncwarp();                                        // the next loads from TMEM are the whole warp's
+                    }
+                    float t0, t1;
+                    unpack_f32x2(test, t0, t1);
+                    if (mine && !is_finite(t0 + t1) && is_finite(l_run) && !zero) *redo = 1;
                 }
                 // the row that was just written gets what V held in place of numbers (not a row of zeros: the join tells for a cut item's)
-                if (odd && mine && !(zero && it.slot < 0)) {
+                if ((odd & kKvHidden) && mine && !(zero && it.slot < 0)) {
 #pragma unroll 1
                     for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
                         const int page = table[j / a.page_size];
@@ -1252,19 +1384,14 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (both && t == 0) ptx::mbar_arrive(stats_done);
                 ptx::mbar_arrive(item_empty0 + 8 * ring);
             }
-        }
+        } while (next_pass(i));
     }
 
     if (*abort_flag) {
         if (lane == 0) report_timeout(kKvKernelId, *abort_flag);
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
-    ptx::tc_fence_before_sync();
-    __syncthreads();
-    if (warp == 1) {
-        ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc(tmem_base, 512);
-    }
+    if (warp == 1) ptx::tmem_dealloc(tmem_base, 512);
 }
 
 // The parts of cut items, added in order.  An item's rows are shared out to the CTAs (c, y) of all c whose stretch ends in it: one c for a
@@ -1272,11 +1399,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 // every eighth part each), or eight (a warp each), or 32 (eight lanes each), by how many it has.
 constexpr int kKvJoinThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kKvJoinThreads)
+__global__ void __launch_bounds__(kKvJoinThreads, 4)                       // (four per SM: all start at once)
 kv_join_kernel(const KvAttnArgs a)
 {
     constexpr int WARPS = kKvJoinThreads / 32;
-    __shared__ float s_sum[WARPS][D], s_l[WARPS];
+    __shared__ float s_sum[WARPS][D];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
@@ -1295,81 +1422,124 @@ kv_join_kernel(const KvAttnArgs a)
         out = a.O + ((int64_t)(cut.row0 + pos) * a.Hq + (int64_t)cut.head * a.ratio + head) * D;
     };
     auto part = [&](int p) { return (int64_t)(p == 0 ? 2 * cut.first + 1 : 2 * (cut.first + p)) * a.slot_rows + in_slot; };
-    // LANES to a row, four channels at a time (two where a warp has no more to give): lane, lane + LANES, ...
-    auto by_lanes = [&](auto lanes_tag) {
-        constexpr int LANES = decltype(lanes_tag)::value, ROWS = 32 / LANES, V = D / LANES >= 4 ? 4 : 2, N = D / LANES / V;
-        const int sub = lane % LANES;
-        for (int i = warp * ROWS + lane / LANES; i < mine; i += WARPS * ROWS) {
-            find(i);
-            float top = -INFINITY;
-#pragma unroll 4
-            for (int p = 0; p < parts; ++p) top = fmaxf(top, stats[part(p)].x);
+    // Part p's share of the row's weight, given the row's base and the inverse of its weight.
+    auto share_of = [&](int p, float base, float inv) {
+        const float2 s = stats[part(p)];
+        return s.y * ex2_approx(s.x - base) * inv;
+    };
+    // LANES lanes work out a row's base and weight together
+    auto base_of = [&](auto lanes_tag, int sub, float& base, float& weight) {
+        constexpr int LANES = decltype(lanes_tag)::value;
+        constexpr int AT_ONCE = 6;                                   // loads in flight: one round for a part per SM and 32 lanes
+        float top = -INFINITY;                                       // of this lane's parts
+        weight = 0.0f;
+#pragma unroll 1
+        for (int p0 = sub; p0 < parts; p0 += AT_ONCE * LANES) {
+            float2 s[AT_ONCE];
+            const float before = top;
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) s[k] = p0 + k * LANES < parts ? stats[part(p0 + k * LANES)] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) top = fmaxf(top, s[k].x);
             const float b0 = top == -INFINITY ? 0.0f : top;
-            float o[N][V] = {}, l = 0.0f;
+            weight *= ex2_approx(before - b0);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) weight += s[k].y * ex2_approx(s[k].x - b0);
+        }
+        const float own = top;
+#pragma unroll
+        for (int w = LANES / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
+        base = top == -INFINITY ? 0.0f : top;
+        weight *= ex2_approx(own - base);
+#pragma unroll
+        for (int w = LANES / 2; w > 0; w >>= 1) weight += __shfl_xor_sync(0xFFFFFFFFu, weight, w);
+    };
+    // Channel `at` of the row where the sum of its parts is no number: one that is none counts however small its part's share, and a weight
+    // that is no number is the answer.
+    auto with_care = [&](int at, float base, float weight) {
+        float o = weight - weight;
+#pragma unroll 1
+        for (int p = 0; p < parts; ++p) {
+            const float v = sums[part(p) * D + at], x = v * share_of(p, base, 1.0f / weight);
+            o += x == x ? x : v;
+        }
+        return o;
+    };
+    if (mine > 1) {
+        // eight lanes to a row, four channels at a time: sub, sub + 8, ...
+        constexpr int LANES = 8, ROWS = 32 / LANES, N = D / LANES / 4;
+        const int sub = lane % LANES;
+#pragma unroll 1
+        for (int i0 = warp * ROWS; i0 < mine; i0 += WARPS * ROWS) {
+            const int i = i0 + lane / LANES;
+            find(min(i, mine - 1));
+            float base, weight;
+            base_of(std::integral_constant<int, LANES>{}, sub, base, weight);
+            const float inv = 1.0f / weight;
+            float o[N][4] = {};
 #pragma unroll 4
             for (int p = 0; p < parts; ++p) {
-                const float2 s = stats[part(p)];
-                const float* x = sums + part(p) * D + sub * V;
-                float v[N][V];
+                const float4* x = reinterpret_cast<const float4*>(sums + part(p) * D) + sub;
+                float4 v[N];
+#pragma unroll
+                for (int c = 0; c < N; ++c) v[c] = x[c * LANES];
+                const float w = share_of(p, base, inv);
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
-                    if constexpr (V == 4) *reinterpret_cast<float4*>(v[c]) = *reinterpret_cast<const float4*>(x + c * LANES * V);
-                    else *reinterpret_cast<float2*>(v[c]) = *reinterpret_cast<const float2*>(x + c * LANES * V);
+                    o[c][0] += v[c].x * w;
+                    o[c][1] += v[c].y * w;
+                    o[c][2] += v[c].z * w;
+                    o[c][3] += v[c].w * w;
                 }
-                const float f = ex2_approx(s.x - b0);
-                l += s.y * f;
-#pragma unroll
-                for (int c = 0; c < N; ++c)
-#pragma unroll
-                    for (int k = 0; k < V; ++k) o[c][k] += v[c][k] * f;
             }
-            const float inv = 1.0f / l;
+            if (i < mine) {
 #pragma unroll
-            for (int c = 0; c < N; ++c) {
-                uint32_t pk[V / 2];
+                for (int c = 0; c < N; ++c) {
+                    uint2* to = reinterpret_cast<uint2*>(out) + sub + c * LANES;
+                    if (weight == 0.0f) *to = make_uint2(0, 0);
+                    else *to = make_uint2(pack_bf16x2(o[c][0], o[c][1]), pack_bf16x2(o[c][2], o[c][3]));
+                }
+                float test = 0.0f;
 #pragma unroll
-                for (int k = 0; k < V / 2; ++k) pk[k] = l == 0.0f ? 0u : pack_bf16x2(o[c][2 * k] * inv, o[c][2 * k + 1] * inv);
-                uint32_t* to = reinterpret_cast<uint32_t*>(out + (sub + c * LANES) * V);
-                if constexpr (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(pk[0], pk[1]);
-                else *to = pk[0];
+                for (int c = 0; c < N; ++c) test += (o[c][0] + o[c][1]) * 0.0f + (o[c][2] + o[c][3]) * 0.0f;
+                if (__builtin_expect(!(test == 0.0f) && weight != 0.0f, 0)) {
+#pragma unroll 1
+                    for (int k = 0; k < 4 * N; ++k) {                // of this lane's channels those that are not finite; the others stay
+                        const int c = (k / 4 * LANES + sub) * 4 + k % 4;
+                        if (!is_finite(__bfloat162float(out[c]))) out[c] = __float2bfloat16_rn(with_care(c, base, weight));
+                    }
+                }
             }
+            __syncwarp();
         }
-    };
-    if (mine > WARPS) return by_lanes(std::integral_constant<int, 8>{});
-    if (mine > 1) return by_lanes(std::integral_constant<int, 32>{});
+        return;
+    }
     if (mine < 1) return;
     constexpr int C = D / 32;
     find(0);
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 32) top = fmaxf(top, stats[part(p)].x);
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
-    const float b0 = top == -INFINITY ? 0.0f : top;
-    float o[C] = {}, l = 0.0f;
-#pragma unroll 4
+    float base, weight;
+    base_of(std::integral_constant<int, 32>{}, lane, base, weight);
+    const float inv = 1.0f / weight;
+    float o[C] = {};
+#pragma unroll 8
     for (int p = warp; p < parts; p += WARPS) {
-        const float2 s = stats[part(p)];
-        const float f = ex2_approx(s.x - b0);
-        l += s.y * f;
+        const float w = share_of(p, base, inv);
         const float* x = sums + part(p) * D + lane * C;
         float v[C];
         if constexpr (C == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
         else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] += v[c] * f;
+        for (int c = 0; c < C; ++c) o[c] += v[c] * w;
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) s_sum[warp][lane * C + c] = o[c];
-    if (lane == 0) s_l[warp] = l;
     __syncthreads();
     if (tid < D) {
-        float sum = 0.0f, weight = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            sum += s_sum[w][tid];
-            weight += s_l[w];
-        }
-        out[tid] = __float2bfloat16_rn(weight == 0.0f ? 0.0f : sum / weight);
+        for (int w = 0; w < WARPS; ++w) sum += s_sum[w][tid];
+        if (__builtin_expect(!(sum == sum) && weight != 0.0f, 0)) sum = with_care(tid, base, weight);
+        out[tid] = __float2bfloat16_rn(weight == 0.0f ? 0.0f : sum);
     }
 }
 

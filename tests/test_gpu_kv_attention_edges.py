@@ -1,10 +1,12 @@
-"""gmlp_kv_attention at edges of its rows, values and lengths: rows that end inside a warp, rows without weight."""
+"""gmlp_kv_attention at edges of its rows, values and lengths: rows that end inside a warp, rows without weight, values
+near the largest bf16 and values that are no numbers."""
 import math
 
 import pytest
 import torch
 
-from test_gpu_kv_attention import Batch
+from paper_2606_26344_b200 import gmlp
+from test_gpu_kv_attention import Batch, gen
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda")
@@ -32,3 +34,111 @@ def test_rows_whose_scores_are_all_minus_infinity_are_zeros_whatever_their_value
     O = batch.run()
     assert bool((O[:B * r] == 0).all())
     batch.check_rows(O, only=(B,))
+
+
+# Items of each kind over keys that are one item or several parts: (requests, Hq, Hkv, D, page)
+KINDS = [([(1, 400)], 8, 2, 128, 64), ([(1, 9000), (3, 70)], 8, 2, 128, 16), ([(2, 5000)] * 3, 4, 1, 64, 48), ([(10, 100)], 8, 2, 128, 64),
+         ([(10, 9000)], 8, 2, 128, 64), ([(20, 4000)] * 3, 6, 2, 64, 16), ([(300, 3000), (1, 700)], 8, 2, 128, 64),
+         ([(150, 150), (90, 2000), (1, 3000)] * 9, 12, 4, 64, 48), ([(500, 2500)], 16, 2, 64, 128),
+         ([(1, 200), (1, 150), (2, 20)] * 90, 32, 8, 128, 64), ([(10, 100), (1, 70), (12, 300)] * 90, 32, 8, 64, 16),     # many items to a CTA
+         ([(70, 100), (40, 400), (1, 90), (0, 10), (3, 0)] * 40, 32, 8, 128, 32)]
+
+
+@pytest.mark.parametrize("reqs,Hq,Hkv,D,page", KINDS)
+@pytest.mark.parametrize("size", [1e34, 1e36, 3.38e38])
+@pytest.mark.parametrize("equal", [False, True])
+def test_large_values(reqs, Hq, Hkv, D, page, size, equal):
+    """Sums of p V pass the largest float where their mean does not: keys of about the same score (or the very same, values of one sign), every
+    value near `size`, up to the largest bf16."""
+    batch = Batch(reqs, Hq, Hkv, D, page)
+    v = batch.cache.v
+    if equal:
+        batch.Q.zero_()
+        v.copy_(torch.where(torch.isnan(v), v, size * (0.5 + 0.5 * torch.rand(v.shape, generator=gen(2), device=DEV)).to(torch.bfloat16)))
+    else:
+        v.copy_(torch.where(torch.isnan(v), v, size * (2 * torch.rand(v.shape, generator=gen(2), device=DEV) - 1).to(torch.bfloat16)))
+    O = batch.check(only=range(0, len(reqs), max(1, len(reqs) // 20)))
+    assert bool(torch.isfinite(O).all())
+
+
+@pytest.mark.parametrize("reqs,Hq,Hkv,D,page", KINDS)
+def test_large_values_leave_the_other_channels_and_requests_as_they_are(reqs, Hq, Hkv, D, page):
+    """One channel of one head of the first request is near the largest bf16, the others are ordinary or tiny: those keep their bits."""
+    batch = Batch(reqs, Hq, Hkv, D, page)
+    batch.cache.v[..., 1::2] *= 2.0 ** -100
+    some = range(0, len(reqs), max(1, len(reqs) // 20))
+    clean = batch.check(only=some).view(-1, Hq, D)
+    r, n = reqs[0]
+    j = torch.arange(n, device=DEV)
+    batch.cache.v[batch.table[0, j // page].long(), 0, j % page, 6] = 3e38
+    O = batch.check(only=some).view(-1, Hq, D)
+    other = torch.ones_like(O, dtype=torch.bool)
+    other[:r, :Hq // Hkv, 6] = False
+    assert torch.equal(O[other], clean[other])
+    assert bool(((O[~other].double() - 3e38).abs() <= 2.0 ** -7 * 3e38).all())       # a constant: half a step of V, one of P and one of O
+
+
+@pytest.mark.parametrize("reqs,Hq,Hkv,D,page", KINDS)
+@pytest.mark.parametrize("values", [(math.inf,), (-math.inf,), (math.nan,), (math.inf, -math.inf), (math.inf, math.inf)])
+def test_values_that_are_no_numbers_reach_the_rows_that_see_them(reqs, Hq, Hkv, D, page, values):
+    """Wherever their keys sit, and beside nothing else: V of some keys of the first request's first head holds `values` in two channels."""
+    batch = Batch(reqs, Hq, Hkv, D, page)
+    clean = batch.run().view(-1, Hq, D).clone()
+    r, n = reqs[0]
+    want = sum(values)
+    hidden = -(-(n - r) // 3)                                            # two keys that all rows see, one that some do not, one that only the last does
+    for at in ((0, n // 2), (n // 3, 0), (hidden, n - 1), (n - 1 - r // 2, 5)):
+        for j, value in zip(at, values):
+            batch.cache.v[batch.table[0, j // page].long(), 0, j % page, [2, D - 3]] = value
+        O = batch.run().view(-1, Hq, D)
+        hit = torch.zeros_like(O, dtype=torch.bool)
+        expect = torch.zeros(O.shape[0], device=DEV)
+        for i in range(r):
+            seen = [v for j, v in zip(at, values) if j <= n - r + i]
+            if seen:
+                hit[i, :Hq // Hkv, 2] = True
+                hit[i, :Hq // Hkv, D - 3] = True
+                expect[i] = sum(seen)
+        assert torch.equal(O[~hit], clean[~hit])
+        got = O[hit].float()
+        assert torch.equal(got.nan_to_num(nan=7.0, posinf=1.0, neginf=-1.0),
+                           expect[:, None, None].expand(-1, Hq, D)[hit].nan_to_num(nan=7.0, posinf=1.0, neginf=-1.0)), (at, want)
+        for j in at[:len(values)]:
+            batch.cache.v[batch.table[0, j // page].long(), 0, j % page, [2, D - 3]] = 0.5
+        clean = batch.run().view(-1, Hq, D).clone()
+
+
+@pytest.mark.parametrize("r,n", [(1, 300), (10, 300), (300, 700), (1, 9000), (10, 9000), (300, 9000)])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_values_that_are_no_numbers_count_however_small_their_weight(r, n, value):
+    """Scores rise by thousands of binary orders along the keys, so that the weight of key 3 is no fp32 number but 0."""
+    batch = Batch([(r, n)], 8, 2, 128, 64)
+    j = torch.arange(n, device=DEV)
+    batch.Q[:, ::128], batch.cache.k[..., 0] = 64.0, 0.0
+    batch.cache.k[batch.table[0, j // 64].long(), :, j % 64, 0] = (8.0 * j / n * 64)[:, None].to(torch.bfloat16)
+    batch.cache.v[batch.table[0, 0].long(), :, 3, 7] = value
+    o = batch.run()[:r].view(r, 8, 128)
+    assert bool(torch.isnan(o[..., 7]).all()) if math.isnan(value) else bool((o[..., 7] == value).all())
+    o[..., 7] = 0
+    assert bool(torch.isfinite(o).all())
+
+
+def test_a_second_pass_keeps_nothing():
+    """Calls that need it and calls that do not, in one graph and one workspace, by turns."""
+    batch = Batch([(1, 3000), (200, 900), (9, 400)], 8, 2, 128, 64, behind=0)
+    v = batch.cache.v.clone()
+    v[torch.isnan(v)] = 0.0
+    want = []
+    for x in (v, v * 1e37):
+        batch.cache.v.copy_(x)
+        want.append(batch.check().clone())
+    ws = torch.empty(gmlp.kv_workspace_bytes(batch.Q.shape[0], 8, 2, 128), dtype=torch.uint8, device=DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = [gmlp.kv_attention(batch.Q, batch.cache, batch.table, batch.lengths, 8, q_start=batch.start, workspace=ws) for _ in range(3)]
+    for i in range(4):
+        batch.cache.v.copy_((v, v * 1e37)[i % 2])
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[i % 2]) for o in outs)
+    del g

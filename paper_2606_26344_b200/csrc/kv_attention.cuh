@@ -252,7 +252,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     extern __shared__ __align__(1024) uint8_t base_ptr[];
     const uint32_t base = ptx::smem_addr(base_ptr);
     if (base & 1023u) {                                                      // the swizzled tiles count on it
-        if (threadIdx.x == 0) report_timeout(kKvKernelId, 0);
+        ptx::grid_dependency_wait();
+        if (threadIdx.x == 0) {
+            report_timeout(kKvKernelId, 0);
+            reinterpret_cast<KvCut*>(a.workspace)[blockIdx.x] = KvCut{};         // nothing to join
+        }
         return;
     }
     const uint32_t q_smem = base, fifo = base + 2 * kKvRegion;

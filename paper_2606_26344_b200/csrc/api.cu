@@ -140,7 +140,7 @@ struct DeviceState {
     bool addss_attr_set = false;
     bool multi_attr_set = false;
     bool gqa_attr_set = false;
-    bool kv_attr_set[4] = {};                    // head dimension 64, 128, each without and with few items
+    bool kv_attr_set[8] = {};                    // head dimension 64, 128, each without and with few items, each without and with long ones
     bool umma_attr_set = false;
     bool pair_attr_set = false;
     bool rowscale_attr_set = false;

@@ -61,6 +61,10 @@ struct KvAttnArgs {
 
 constexpr int kKvThreads = 384, kKvBlock = 128, kKvRing = 4;
 constexpr int kKvFew = 16;                       // rows of an item whose products are turned round
+// Blocks that a few item's O is summed over before it is added to a second sum, 16 columns on.  The tensor pipe cuts where it adds, always
+// towards 0, 16 times a block: over 8192 blocks in one sum (2^20 keys) the error's norm was 1.8 times that of the last rounding, 3.8 with values
+// of one sign.
+constexpr int kKvFewSum = 256;
 constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
 // The axis: what a key of an item takes, and an item's start and end.  In a batch of both, big items are bound by the tensor pipe and the
 // softmax and the others by the copies, which run the faster the fewer SMs make them (40 single tokens and three chunks: 301 us with the
@@ -173,6 +177,9 @@ __device__ __forceinline__ float tmem_ld_32x1(uint32_t taddr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=f"(r) : "r"(taddr) : "memory");
     return r;
 }
+__device__ __forceinline__ void tmem_st_32x1(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
+}
 // the largest of a warp's values, NaN left out
 __device__ __forceinline__ float redux_max_f32(float v) {
     float r;
@@ -230,8 +237,9 @@ template <int SLOTS> struct KvCursor {
     }
 };
 
-// FEW: with the code of few items; without it they are small ones.
-template <int D, bool FEW>
+// FEW: with the code of few items; without it they are small ones.  LONG: an item may have more than kKvFewSum blocks; the others need no code for
+// that (256 requests of 200 keys 91 us without it, 95 with it; 64 of 4096 keys 178 and 179).
+template <int D, bool FEW, bool LONG>
 __global__ void __launch_bounds__(kKvThreads, 1)
 kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQfew, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const KvAttnArgs a)
@@ -577,7 +585,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
                         for (int k = 0; k < 16; ++k)                         // both terms
                             ptx::umma_bf16_halves(tmem_base + 256u + 128u * (uint32_t)t, ad[k & 7], bd[k & 7] + (k >= 8 ? P_TERM >> 4 : 0u), desc_hi,
-                                                  kIdescFewPV, n != 0 || k != 0 ? 1u : 0u);
+                                                  kIdescFewPV, (LONG ? n % kKvFewSum != 0 : n != 0) || k != 0 ? 1u : 0u);
                         ptx::umma_commit(o_full0 + 8 * (2 * t + (n & 1)));
                         ptx::umma_commit(kv_empty0 + 8 * v_slot);
                         if (n == blocks - 1) ptx::umma_commit(q_empty0 + 8 * t);         // P lies in the region too
@@ -1038,6 +1046,20 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 agreed ^= 1u;
                 return ok;
             };
+            // O's two sums added, into the columns from `to` on (once in many blocks: short code)
+            auto add_sums = [&](bool both, uint32_t to) {
+                ptx::tc_fence_after_sync();
+#pragma unroll 1
+                for (uint32_t n = 0; n < kKvFew; ++n) {
+                    const float o = tmem_ld_32x1(o_addr + n);
+                    float other = 0.0f;
+                    if (both) other = tmem_ld_32x1(o_addr + kKvFew + n);
+                    ptx::tmem_ld_wait();
+                    tmem_st_32x1(o_addr + to + n, o + other);
+                    tmem_st_wait();
+                }
+                ptx::tc_fence_before_sync();
+            };
             const uint32_t p_at = q_smem + t * kKvRegion + P_AT + (uint32_t)(r >> 6) * P_HALF + (uint32_t)(r & 7) * 2u;
             const uint32_t chunk = (uint32_t)(r & 63) >> 3;
 #pragma unroll 1
@@ -1056,6 +1078,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     each_row([&](int n) {
                         if (!there || key >= seen[n]) x[n] = -INFINITY;
                     });
+                }
+                if (LONG && opaque(j) % kKvFewSum == 0 && j > 0) {           // PV of this block begins a new sum
+                    if (!kv_wait(o_full0 + 8 * (2 * t + (buf ^ 1u)), ((o_phase >> (buf ^ 1u)) & 1u) ^ 1u, abort_flag, 23)) return false;
+                    add_sums(j > kKvFewSum, kKvFew);
                 }
                 // the base of a row moves when a score passes it by 8 (a factor of 256), and from -infinity
                 const bool begins = opaque(j) == 0;
@@ -1093,13 +1119,18 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (any && !begins) {                                      // the same for all four warps
                         if (!kv_wait(o_full0 + 8 * (2 * t + (buf ^ 1u)), ((o_phase >> (buf ^ 1u)) & 1u) ^ 1u, abort_flag, 21)) return false;
                         ptx::tc_fence_after_sync();
-                        float o[kKvFew];
-                        tmem_ld_32x16(o_addr, o);
-                        ptx::tmem_ld_wait();
-                        uint32_t ow[kKvFew];
-                        each_row([&](int n) { ow[n] = __float_as_uint(o[n] * f[n]); });
-                        tmem_st_32x16(o_addr, ow);
-                        tmem_st_wait();
+                        uint32_t c = 0;
+                        for (;;) {                                           // the sum that PV adds to, and the other one if there is one
+                            float o[kKvFew];
+                            tmem_ld_32x16(o_addr + c, o);
+                            ptx::tmem_ld_wait();
+                            uint32_t ow[kKvFew];
+                            each_row([&](int n) { ow[n] = __float_as_uint(o[n] * f[n]); });
+                            tmem_st_32x16(o_addr + c, ow);
+                            tmem_st_wait();
+                            if (!LONG || opaque(j) < kKvFewSum || c != 0) break;
+                            c = kKvFew;
+                        }
                         ptx::tc_fence_before_sync();
                     }
                 }
@@ -1138,6 +1169,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const uint32_t buf = (uint32_t)(blocks - 1) & 1u;
                 if (!kv_wait(o_full0 + 8 * (2 * t + buf), ((o_phase >> buf) & 1u) ^ 1u, abort_flag, 14)) return false;
                 ptx::tc_fence_after_sync();
+                if (LONG && opaque(blocks) > kKvFewSum) add_sums(true, 0);
                 if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) return false;
                 odd = hidden[ring];
             }

@@ -199,19 +199,19 @@ bool encode_kv_query(CUtensorMap* map, const void* ptr, int head_dim, int Hq, in
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool FEW>
+template <int D>
 int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensorMap& tmQfew, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                        const gmlp::KvAttnArgs& k, bool join, cudaStream_t st) {
-    bool& set = dev->kv_attr_set[2 * (D == 128) + FEW];
+                        const gmlp::KvAttnArgs& k, bool few, bool long_items, bool join, cudaStream_t st) {
+    const auto kernel = few ? (long_items ? gmlp::kv_attention_kernel<D, true, true> : gmlp::kv_attention_kernel<D, true, false>)
+                            : (long_items ? gmlp::kv_attention_kernel<D, false, true> : gmlp::kv_attention_kernel<D, false, false>);
+    bool& set = dev->kv_attr_set[4 * (D == 128) + 2 * few + long_items];
     if (!set) {
-        if (cudaFuncSetAttribute(gmlp::kv_attention_kernel<D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gmlp::kv_attn_smem(D)) != cudaSuccess)
             return GMLP_ERR_LAUNCH;
         set = true;
     }
     const int ctas = dev->sm_count;
-    int rc = launch_block(gmlp::kv_attention_kernel<D, FEW>, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ,
-                          tmQfew, tmK, tmV, k);
+    int rc = launch_block(kernel, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
     prof_mark("kv_attention", st);
     if (!join) return GMLP_OK;
@@ -286,10 +286,9 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     // no item is long enough to be cut where the table has few pages
     const int mode = a->T <= k.few_pos ? gmlp::kKvFewItem : (a->T <= k.tile_pos ? gmlp::kKvSmallItem : gmlp::kKvBigItem);
     const bool join = gmlp::kv_start(mode) + a->table_width * k.page_size * gmlp::kv_key(mode) > gmlp::kKvSnap;
-#define GMLP_KV_ATTENTION(D) \
-    (few ? launch_kv_attention<D, true>(dev, tmQ, tmQfew, tmK, tmV, k, join, st)                                                            \
-         : launch_kv_attention<D, false>(dev, tmQ, tmQfew, tmK, tmV, k, join, st))
-    rc = D == 128 ? GMLP_KV_ATTENTION(128) : GMLP_KV_ATTENTION(64);
+    const bool long_items = a->table_width * k.page_size > gmlp::kKvFewSum * gmlp::kKvBlock;
+    rc = D == 128 ? launch_kv_attention<128>(dev, tmQ, tmQfew, tmK, tmV, k, few, long_items, join, st)
+                  : launch_kv_attention<64>(dev, tmQ, tmQfew, tmK, tmV, k, few, long_items, join, st);
     if (rc != GMLP_OK) return rc;
     return finish_checked(dev, a->flags, st);
 }

@@ -142,3 +142,51 @@ def test_a_second_pass_keeps_nothing():
         torch.cuda.synchronize()
         assert all(torch.equal(o, want[i % 2]) for o in outs)
     del g
+
+
+def long_sums(r, n, mean, rise=0.0, seed=1):
+    """37 requests of r positions over the same n keys, 4 key heads: 148 items of one length, which stay whole, one on each SM.  Values of mean
+    `mean`, scores that rise by `rise` along the keys.  Returns the error's norm over that of the last rounding alone, of two requests and heads."""
+    Hkv, ratio, D, page, B, g = 4, 4, 128, 64, 37, gen(seed)
+    k, v = (torch.empty(-(-n // page), Hkv, page, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for c, at in ((k, 0.0), (v, mean)):
+        for p in range(0, k.shape[0], 2048):
+            c[p:p + 2048] = torch.randn(c[p:p + 2048].shape, generator=g, device=DEV) + at
+    table = torch.arange(k.shape[0], dtype=torch.int32, device=DEV).expand(B, -1).contiguous()
+    Q = torch.randn(B * r, Hkv * ratio * D, generator=g, device=DEV).to(torch.bfloat16)
+    if rise:
+        Q[:, ::D] = 8.0
+        k[..., 0] = (rise * D ** 0.5 / 8 / n * torch.arange(k.shape[0] * page, device=DEV).view(-1, 1, page)).to(torch.bfloat16)
+    lengths = torch.full((B,), n, dtype=torch.int32, device=DEV)
+    O = gmlp.kv_attention(Q, gmlp.KvCache(k, v), table, lengths, Hkv * ratio, q_len=r, checked=True)
+    err = own = 0.0
+    for b, h in ((0, 0), (36, 3)):
+        q = Q[b * r:(b + 1) * r].double().view(r, Hkv, ratio * D)[:, h].reshape(-1, D)
+        seen = (n - r + 1 + torch.arange(r, device=DEV)).repeat_interleave(ratio)[:, None]
+        top, total, acc = torch.full((len(q), 1), -1e300, dtype=torch.float64, device=DEV), 0.0, 0.0
+        for lo in range(0, n, 1 << 16):
+            kk, vv = (c[:, h].reshape(-1, D)[lo:min(n, lo + (1 << 16))].double() for c in (k, v))
+            s = (q @ kk.T / D ** 0.5).masked_fill(lo + torch.arange(len(kk), device=DEV) >= seen, -math.inf)
+            now = torch.maximum(top, s.amax(1, keepdim=True))
+            p, f, top = torch.exp(s - now), torch.exp(top - now), now
+            total, acc = total * f + p.sum(1, keepdim=True), acc * f + p @ vv
+        want = acc / total
+        got = O[b * r:(b + 1) * r].double().view(r, Hkv, ratio * D)[:, h].reshape(-1, D)
+        err += float((got - want).square().sum())
+        own += float((want.to(torch.bfloat16).double() - want).square().sum())
+    return (err / own) ** 0.5
+
+
+@pytest.mark.parametrize("n", [32768, 32769, 65535, 131071, 1 << 20])
+@pytest.mark.parametrize("mean", [0.0, 1.0])
+def test_long_sums_of_single_tokens(n, mean):
+    """A CTA goes over all keys of an item.  Adding towards 0 costs at most 2^-23 of the sum so far each time, 16 times a block of 128 keys, 2^-24
+    on average: 256 blocks 2^-13 of the sum at the end (half of that, as the sum grows along the keys), a sixteenth of the rounding to bf16
+    (2^-9 / sqrt(3) = 2^-9.8) by norm or less: sqrt(1 + 2^-6.4) = 1.006, and the second terms of the probabilities, 2^-17: 1.02 in all."""
+    assert long_sums(1, n, mean) <= 1.02
+
+
+@pytest.mark.parametrize("rise", [8.0, 20.0])
+def test_long_sums_whose_base_moves(rise):
+    """The base of the exponentials moves in sums that have been set aside before."""
+    assert long_sums(1, 131071, 1.0, rise) <= 1.02

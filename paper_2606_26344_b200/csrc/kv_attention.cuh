@@ -65,6 +65,10 @@ constexpr int kKvFew = 16;                       // rows of an item whose produc
 // towards 0, 16 times a block: over 8192 blocks in one sum (2^20 keys) the error's norm was 1.8 times that of the last rounding, 3.8 with values
 // of one sign.
 constexpr int kKvFewSum = 256;
+// Big and small items have no tensor memory for a second sum.  They are handed out in pieces of this many blocks; between two of them their rows'
+// sums wait in the workspace (one such item over 2^20 keys: 3.6 times the last rounding's error without pieces with values of one sign).
+constexpr int kKvPiece = 512;
+enum { kKvGoesOn = 1, kKvMore = 2 };             // a piece: earlier ones went before it, others come after it
 constexpr int kKvMends = 8;                       // more than the FIFO holds blocks of V
 // The axis: what a key of an item takes, and an item's start and end.  In a batch of both, big items are bound by the tensor pipe and the
 // softmax and the others by the copies, which run the faster the fewer SMs make them (40 single tokens and three chunks: 301 us with the
@@ -82,7 +86,7 @@ constexpr uint32_t kKvRegion = 32768;            // of a tile: Q, and in few ite
 constexpr uint32_t kv_attn_smem(int D) { return 2 * kKvRegion + kv_slots(D) * kv_tile_bytes(D) + 1024 + 1024 + 1024; }
 
 // Workspace: one descriptor per CTA - the cut item that its stretch ends in - then base and weight of the rows of each of its two partial
-// results, then their rows, divided by the weight.
+// results, then their rows, divided by the weight, then the sums of each tile's rows between two pieces of an item.
 struct KvCut {
     int parts, first;                // parts (less than two: none), the CTA that has the first of them
     int head, row0, npos, two_tiles, pad[2];
@@ -91,8 +95,12 @@ __host__ __device__ inline uint64_t kv_ws_stats(int ctas) { return ((uint64_t)ct
 __host__ __device__ inline uint64_t kv_ws_sums(int ctas, int slot_rows) {
     return kv_ws_stats(ctas) + (((uint64_t)ctas * 2 * slot_rows * 8 + 255) & ~(uint64_t)255);
 }
-__host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) {
+__host__ __device__ inline uint64_t kv_ws_pieces(int ctas, int slot_rows, int D) {
     return kv_ws_sums(ctas, slot_rows) + (uint64_t)ctas * 2 * slot_rows * D * 4;
+}
+__host__ __device__ inline int kv_tile_rows(int slot_rows) { return slot_rows < 128 ? slot_rows : 128; }
+__host__ __device__ inline uint64_t kv_ws_bytes(int ctas, int slot_rows, int D) {
+    return kv_ws_pieces(ctas, slot_rows, D) + (uint64_t)ctas * 2 * kv_tile_rows(slot_rows) * D * 4;
 }
 
 struct KvItem {
@@ -104,7 +112,8 @@ struct KvItem {
     int last;                        // no more items (this one is none)
     int mode, tile;                  // kKvBigItem ..; the tile of a few item
     int careful;                     // the second pass
-    int pad[3];
+    int piece, part0;                // kKvGoesOn, kKvMore; the first block of the item's part in this CTA
+    int pad;
 };
 
 // Request b: its first row, rows and keys; what the arrays hold outside of their ranges is left out (and reported by one CTA).
@@ -638,7 +647,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             };
             if (big) {
                 // both tiles over each block: S_A(0), S_B(0), then P_A V(j), S_A(j + 1), P_B V(j), S_B(j + 1)
-                ok = wait_q(0) && wait_q(1);
+                ok = (LONG && (it.piece & kKvGoesOn)) || (wait_q(0) && wait_q(1));
 #pragma unroll 1
                 for (int j = -1; j < blocks && ok; ++j) {
 #pragma unroll
@@ -652,7 +661,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                             scores(t, q_lo + (uint32_t)t * (kKvRegion >> 4), t == 1);
                         }
                     }
-                    if (j + 2 == blocks) {                                   // Q has been used
+                    if (j + 2 == blocks && !(LONG && (it.piece & kKvMore))) {        // Q has been used
                         if (leader) {
                             ptx::umma_commit(q_empty0);
                             ptx::umma_commit(q_empty0 + 8);
@@ -662,7 +671,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 }
             } else {
                 // block n to tile n & 1: S(0), S(1), P V(0), S(2), P V(1), ...
-                ok = wait_q(0);
+                ok = (LONG && (it.piece & kKvGoesOn)) || wait_q(0);
 #pragma unroll 1
                 for (int m = 0; m < blocks + 2 && ok; ++m) {
                     const int t = m & 1;
@@ -673,7 +682,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (m < blocks) {
                         if (!wait_k(k_slot)) { ok = false; break; }
                         scores(t, q_lo, true);
-                        if (m == blocks - 1) {
+                        if (m == blocks - 1 && !(LONG && (it.piece & kKvMore))) {
                             if (leader) ptx::umma_commit(q_empty0);
                             __syncwarp();
                         }
@@ -741,6 +750,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         cut.two_tiles = npos > a.tile_pos;
                     }
                     const int tile_of = mode == kKvFewItem ? (int)(few_items & 1u) : 0;
+                  for (int from_blk = blk0;;) {
+                    const int to_blk = LONG && mode != kKvFewItem ? min(blk1, from_blk + kKvPiece) : blk1;
                     const uint32_t p = i % kKvRing;
                     // a free place; in the second pass all of them
                     for (uint32_t n = i; ok && n < i + (careful ? kKvRing : 1); ++n)
@@ -748,8 +759,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (!ok) break;
                     if (lane == 0) {
                         KvItem it;
-                        it.blk0 = blk0;
-                        it.blk1 = blk1;
+                        it.blk0 = from_blk;
+                        it.blk1 = to_blk;
                         it.b = b;
                         it.head = head;
                         it.row0 = row0 + pos0;
@@ -761,6 +772,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         it.mode = mode;
                         it.tile = tile_of;
                         it.careful = careful;
+                        it.piece = (from_blk > blk0 ? kKvGoesOn : 0) | (to_blk < blk1 ? kKvMore : 0);
+                        it.part0 = blk0;
                         items[p] = it;
                         hidden[p] = 0;
                         ptx::mbar_arrive(item_full0 + 8 * p);
@@ -768,7 +781,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     __syncwarp();
                     ++i;
                     if (mode == kKvFewItem) ++few_items;
-                    for (int t = tile_of; ok && blk1 > blk0 && t < (mode == kKvBigItem ? 2 : tile_of + 1); ++t) {
+                    for (int t = tile_of; ok && blk1 > blk0 && from_blk == blk0 && t < (mode == kKvBigItem ? 2 : tile_of + 1); ++t) {
                         if (!kv_wait(q_empty0 + 8 * t, ((loads >> t) & 1u) ^ 1u, abort_flag, 9)) { ok = false; break; }
                         loads ^= 1u << t;
                         if (lane == 0) {
@@ -782,7 +795,10 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         }
                         __syncwarp();
                     }
-                    if (!ok) break;
+                    if (!ok || to_blk == blk1) break;
+                    from_blk = to_blk;
+                  }
+                  if (!ok) break;
                 }
                 x += cost;
                 ++tile;
@@ -822,7 +838,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int first = first_hidden(it);
             const int from = it.careful ? it.blk0 : max(it.blk0, first / kKvBlock);
             float* of_all = seen_by_all(it.mode);
-            if (__builtin_expect(it.careful, 0)) {
+            if (__builtin_expect(it.careful && !(it.piece & kKvGoesOn), 0)) {
 #pragma unroll 1
                 for (int c = lane; c < D; c += 32) of_all[c] = 0.0f;
                 __syncwarp();
@@ -916,6 +932,8 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const int my_pos = r / a.ratio;
         uint32_t s_phase = 0, o_phase = 0, joins = 0, agreed = 0;           // bits: [buffer]
         float m_use = -INFINITY, l_run = 0.0f;                               // exponent base, row sum
+        float m_piece = 0.0f;                                                // the base of what waits in the workspace
+        uint32_t odd = 0;                                                    // numbers that are none, taken out of V
         bool ok = true;
 
         // One step: as in gqa_attention.cuh.  `valid`: keys of the block that the row sees, `bits`: of the block's groups of 16 keys those whose
@@ -1263,8 +1281,13 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const bool active = __any_sync(0xFFFFFFFFu, mine);
             const int seen = mine ? min(max(a.causal ? it.seen0 + pos : it.keys, 0), it.keys) : 0;
             const int n_steps = big ? blocks : (blocks + 1 - t) / 2;         // of this tile
-            m_use = -INFINITY;
-            l_run = 0.0f;
+            const int piece = LONG ? it.piece : 0;
+            if (!(piece & kKvGoesOn)) {
+                m_use = -INFINITY;
+                l_run = 0.0f;
+                odd = 0;
+            }
+            const int n_first = piece & kKvGoesOn ? -1 : 0;                  // the step that sets the base: not in a later piece
             // the steps of this tile's blocks, `stride` of them apart
             auto steps = [&](auto two_tag, int key0, int stride) {
 #pragma unroll 1
@@ -1282,7 +1305,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (!kv_wait(s_full0 + 16 * t, s_phase & 1u, abort_flag, 13)) return false;
                     s_phase ^= 1u;
                     ptx::tc_fence_after_sync();
-                    if (opaque(active)) step_pass(two_tag, opaque(n) == 0, valid, bits, opaque(masked), mine);
+                    if (opaque(active)) step_pass(two_tag, opaque(n) == n_first, valid, bits, opaque(masked), mine);
                     ptx::tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(p_full0 + 16 * t);
@@ -1296,15 +1319,55 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!kv_wait(o_full0 + 16 * t, (o_phase & 1u) ^ 1u, abort_flag, 14)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
             }
-            uint32_t odd = 0;                                                // numbers that are none, taken out of V
             if (blocks > 0) {
                 if (!kv_wait(item_fixed0 + 8 * ring, ring_phase, abort_flag, 15)) { ok = false; break; }
-                odd = hidden[ring];
+                odd |= hidden[ring];
+            }
+            if (LONG && opaque(piece) != 0) {
+                // the sum so far: into the workspace, from the last piece into tensor memory, where the rest expects it
+                const int t = opaque(tile_no), r = opaque(row_no);
+                const uint32_t o_addr = tmem_base + 256u + 128u * (uint32_t)t + ((uint32_t)(r & ~31) << 16);
+                float* waits = reinterpret_cast<float*>(a.workspace + kv_ws_pieces(gridDim.x, a.slot_rows, D)) +
+                               ((int64_t)(2 * (int)blockIdx.x + t) * kv_tile_rows(a.slot_rows) + r) * D;
+                const float f = ex2_approx(m_piece - (m_use == -INFINITY ? 0.0f : m_use));
+                if (active) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 4) {
+                        float o[4];
+                        float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[k] = opaque(n_steps) > 0 ? tmem_ld_32x1(o_addr + (uint32_t)(c + k)) : 0.0f;
+                        if (mine && (piece & kKvGoesOn)) w = *reinterpret_cast<const float4*>(waits + c);
+                        ptx::tmem_ld_wait();
+                        if (piece & kKvGoesOn) {
+                            o[0] += w.x * f;
+                            o[1] += w.y * f;
+                            o[2] += w.z * f;
+                            o[3] += w.w * f;
+                        }
+                        __syncwarp();
+                        if (piece & kKvMore) {
+                            if (mine) *reinterpret_cast<float4*>(waits + c) = make_float4(o[0], o[1], o[2], o[3]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) tmem_st_32x1(o_addr + (uint32_t)(c + k), o[k]);
+                            tmem_st_wait();
+                        }
+                        __syncwarp();
+                    }
+                }
+                m_piece = m_use;
+                if (piece & kKvMore) {
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(item_empty0 + 8 * ring);
+                    continue;
+                }
             }
 
             // Small items of several blocks: both tiles hold sums of the same rows.  Tile B's warps hand base and weight over, tile A's (which may
             // read the same lanes of tile B's columns) do the rest.
-            const bool both = !big && blocks > 1;
+            const bool both = !big && (blocks > 1 || (piece & kKvGoesOn));
             float f_mine = 1.0f, f_other = 0.0f;
             if (both) {
                 if (t == 1) {
@@ -1400,7 +1463,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 // the row that was just written gets what V held in place of numbers (not a row of zeros: the join tells for a cut item's)
                 if ((odd & kKvHidden) && mine && !(zero && it.slot < 0)) {
 #pragma unroll 1
-                    for (int j = max(min(max(it.seen0, 0), it.keys), it.blk0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
+                    for (int j = max(min(max(it.seen0, 0), it.keys), it.part0 * kKvBlock); j < min(seen, it.blk1 * kKvBlock); ++j) {
                         const int page = table[j / a.page_size];
                         if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
                         const bf16* vr = a.v + (((int64_t)page * a.Hkv + it.head) * a.page_size + j % a.page_size) * D;

@@ -187,6 +187,43 @@ def test_long_sums_of_single_tokens(n, mean):
 
 
 @pytest.mark.parametrize("rise", [8.0, 20.0])
-def test_long_sums_whose_base_moves(rise):
+@pytest.mark.parametrize("r,most", [(1, 1.02), (10, 1.02), (64, 1.05 * 2 ** 0.5)])
+def test_long_sums_whose_base_moves(rise, r, most):
     """The base of the exponentials moves in sums that have been set aside before."""
-    assert long_sums(1, 131071, 1.0, rise) <= 1.02
+    assert long_sums(r, 131071, 1.0, rise) <= most
+
+
+@pytest.mark.parametrize("n", [65536, 65537, 65664, 131072, 131073, 1 << 20])
+@pytest.mark.parametrize("r,mean,most", [(10, 0.0, 1.02), (10, 1.0, 1.02), (64, 0.0, 1.02 * 2 ** 0.5), (64, 1.0, 1.02)])
+def test_long_sums_of_chunks(r, mean, most, n):
+    """Small and big items: 4096 additions of 16 keys to a sum at most, as above.  Big items round probabilities to bf16: an error of about the
+    last rounding's size with values of both signs; with values of mean 1 the roundings of so many probabilities cancel in the mean."""
+    assert long_sums(r, n, mean) <= most
+
+
+@pytest.mark.parametrize("r", [10, 64])
+@pytest.mark.parametrize("value", [1e37, math.inf])
+def test_pieces_of_long_items_in_a_second_pass(r, value):
+    """148 whole items of three pieces over the same keys, with values near the largest bf16 in one channel and an infinity in another, at keys of
+    the first piece, the last one, and the newest key."""
+    n, B, Hkv, D, page, g = 140000, 37, 4, 64, 64, gen(3)
+    k, v = (torch.randn(-(-n // page), Hkv, page, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    table = torch.arange(k.shape[0], dtype=torch.int32, device=DEV).expand(B, -1).contiguous()
+    Q = torch.randn(B * r, Hkv * 4 * D, generator=g, device=DEV).to(torch.bfloat16)
+    call = lambda: gmlp.kv_attention(Q, gmlp.KvCache(k, v), table, torch.full((B,), n, dtype=torch.int32, device=DEV), 16, q_len=r, checked=True)
+    clean = call().view(B * r, Hkv, 4, D).clone()
+    v[:, 1, :, 6] = 1e37
+    for j, channel in ((77, 9), (n - 5000, 10), (n - 1, 11)):
+        v[j // page, 1, j % page, channel] = value
+    O = call().view(B * r, Hkv, 4, D)
+    assert bool(((O[:, 1, :, 6].double() - 1e37).abs() <= 2.0 ** -7 * 1e37).all())
+    last = torch.zeros(B, r, dtype=torch.bool, device=DEV)
+    last[:, -1] = True
+    if value == math.inf:
+        assert bool((O[:, 1, :, 9:11] == value).all()) and bool((O[last.view(-1), 1, :, 11] == value).all())
+        assert torch.equal(O[~last.view(-1), 1, :, 11], clean[~last.view(-1), 1, :, 11])
+    else:
+        assert bool((O[:, 1, :, 9:11] > 1e28).all())
+    other = torch.ones_like(O, dtype=torch.bool)
+    other[:, 1, :, 6], other[:, 1, :, 9:12] = False, False
+    assert torch.equal(O[other], clean[other])

@@ -460,8 +460,9 @@ uint64_t gmlp_kv4_workspace_bytes(int64_t B, int32_t q_len, int32_t n_q_heads, i
  * Rotary positions.  Pair i of a head's first rotary_dim channels - (2 i, 2 i + 1) if interleaved, else (i, i + rotary_dim / 2) - turns
  * by the angle position * f_i and is multiplied by an amplitude A; the head's other channels stay as they are:
  *     u' = A (u cos t - v sin t),   v' = A (u sin t + v cos t),   t = position * f_i.
- * steps[i] is f_i / (2 pi), turns per position, in units of 2^-64 (modulo one turn): position * step modulo 2^64 is exact, so a far
- * position's angle is as good as a near one's.  The rotation is computed in fp32 and rounded once.  Positions may be negative; the call
+ * steps[i] is f_i / (2 pi), turns per position, in units of 2^-64 (modulo one turn), rounded; position * step modulo 2^64 is exact.  So an
+ * angle is off by position * 1.5 * 2^-64 turns at most, which up to position 2^38 is no more than the rotation's fp32 arithmetic takes anyway
+ * (and grows to whole turns towards 2^63).  The rotation is computed in fp32 and rounded once.  Positions may be negative; the call
  * with negated positions is the transpose, i.e. the gradient.  rotary_dim is a multiple of 4 (4-byte accesses unless it is one of 16, or of
  * 8 if interleaved).
  * gmlp_rope_steps fills the table (on the HOST; pure host arithmetic) from f_i = base^(-2 i / rotary_dim), scaled for contexts longer than

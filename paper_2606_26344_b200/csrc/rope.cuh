@@ -2,8 +2,9 @@
 //
 // Pair i of a head's first `rot` channels turns by position * f_i and is multiplied by an amplitude A:
 //     u' = A (u cos t - v sin t),   v' = A (u sin t + v cos t),   (u, v) = channels (2 i, 2 i + 1) or (i, i + rot / 2).
-// The table holds f_i / (2 pi), turns per position, in units of 2^-64: position * step modulo 2^64 is the angle's place within the
-// turn, exactly, however far the position; its upper 32 bits become the argument of one sincospi.  (In fp32 the angle of position
+// The table holds f_i / (2 pi), turns per position, rounded to units of 2^-64: position * step modulo 2^64, an exact product, is the angle's
+// place within the turn, off by the entry's rounding times the position (no more than fp32 takes anyway up to position 2^38); its upper 32 bits
+// become the argument of one sincospi.  (In fp32 the angle of position
 // 131072 would be off by 2^-8 radians: half a unit in the last place of its 17 bits before the point.)
 //
 // What bounds it: bytes, one read and one write of each row.  A pair's cosine and sine (some 40 instructions) serve all heads of a

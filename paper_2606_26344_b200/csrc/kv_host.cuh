@@ -213,7 +213,7 @@ int launch_kv_attention(DeviceState* dev, const CUtensorMap& tmQ, const CUtensor
     const int ctas = dev->sm_count;
     int rc = launch_block(kernel, dim3((unsigned)ctas), dim3(gmlp::kKvThreads), gmlp::kv_attn_smem(D), st, tmQ, tmQfew, tmK, tmV, k);
     if (rc != GMLP_OK) return rc;
-    prof_mark("kv_attention", st);
+    prof_mark(few ? "kv_attention_few" : "kv_attention", st);
     if (!join) return GMLP_OK;
     rc = launch_block(gmlp::kv_join_kernel<D>, dim3((unsigned)ctas, k.slot_rows > 64 ? 8 : 4), dim3(gmlp::kKvJoinThreads), 0, st, k);
     if (rc != GMLP_OK) return rc;

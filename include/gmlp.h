@@ -552,7 +552,8 @@ int gmlp_kv_append(const gmlp_kv_append_args* args);
  * no request are left as they were.  What the pages hold past a request's end, and table entries past its last page, are never used, and
  * what a row does not see does not reach it, infinities and NaN included.  An infinity or NaN in V reaches every row that sees its key, however
  * small its probability (unless the row is zeros), and finite values of any size give finite results; both may take a second pass over part of
- * the call's work.  Scores, exponentials and sums are fp32; the probabilities are
+ * the call's work.  Finite scores, scale * q.k * log2(e), up to 2^30 in magnitude are told apart as far as fp32 holds them; a row whose largest
+ * one is beyond that may become zeros or NaN.  Scores, exponentials and sums are fp32; the probabilities are
  * rounded to bf16 for the second product, as in gmlp_gqa_attention, in tiles of more than 128 rows (positions times n_q_heads /
  * n_kv_heads), and kept to 16 bits of significand (two bf16 terms) in smaller ones; O is rounded once.
  * A table entry outside of the cache, a negative length, a length past the table, and a q_start that falls or passes T are reported like a

@@ -227,3 +227,31 @@ def test_pieces_of_long_items_in_a_second_pass(r, value):
     other = torch.ones_like(O, dtype=torch.bool)
     other[:, 1, :, 6], other[:, 1, :, 9:12] = False, False
     assert torch.equal(O[other], clean[other])
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("power", [24, 27, 29, 30])
+@pytest.mark.parametrize("r,n", [(1, 300), (1, 9000), (10, 100), (10, 5000), (300, 700)])
+def test_scores_of_large_magnitude(r, n, power, sign):
+    """Up to 2^30 binary orders, the stated range.  Keys that are all the same give the mean of the values that a row sees, although the fp32
+    base is off the score by up to 32 binary orders there; one key that scores twice as much gives its value."""
+    batch = Batch([(r, n)], 8, 2, 128, 64, behind=0)
+    score = 0.99 * 2.0 ** power / (128 ** -0.5 * 1.4426950408889634)
+    batch.Q.zero_()
+    batch.Q[:, ::128] = 2.0 ** (power // 2)
+    k = torch.zeros_like(batch.cache.k)
+    k[..., 0] = sign * score / 2 / 2.0 ** (power // 2)
+    batch.cache.k.copy_(torch.where(torch.isnan(batch.cache.k), batch.cache.k, k))
+    O = batch.run().view(r, 2, 4, 128)
+    _, v = batch.keys(0)
+    seen = n - r + 1 + torch.arange(r, device=DEV)
+    want = (v.double().cumsum(0) / torch.arange(1, n + 1, device=DEV)[:, None, None])[seen - 1][:, :, None]
+    size = (v.double().abs().cumsum(0) / torch.arange(1, n + 1, device=DEV)[:, None, None])[seen - 1][:, :, None]
+    # the last rounding, one of each probability (big items), and a sum of n terms
+    assert bool(((O.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + n * 2.0 ** -23) * size).all())
+    j = n - r                                                                # a key that every row sees
+    batch.cache.k[batch.table[0, j // 64].long(), :, j % 64, 0] *= 2 if sign > 0 else 0.5
+    # Its probability before the division is 2^e, e what the fp32 base is off: no power of two.  Two bf16 terms hold it to 2^-16, which the last
+    # rounding removes (V is a bf16 number); one term (big items) to 2^-8 of the value, and the last rounding may take 2^-8 on top.
+    one_term, value = r * 4 > 128, v[j].double()[None, :, None].expand(r, 2, 4, 128)
+    assert bool(((batch.run().view(r, 2, 4, 128).double() - value).abs() <= (2.0 ** -7 * 1.01 if one_term else 0.0) * value.abs()).all())

@@ -33,6 +33,7 @@
 // from the first pass is written anew; the rest stays.  Parts of cut items are divided by their own sum of p, so that the join weighs means.
 // Calls without a second pass pay for the test, the join's weights and the longer code: 256 requests of 200 keys 90 us, 87 before; one token over
 // 2^20 keys 102 and 99; 64 of 4096 keys 179 and 178; a prompt of 8192 the same.  A second pass takes three to five times as long as a first.
+// Scores: from 2^31 binary orders on, the rounding of the base alone (a product of a score and the scale) passes the exponents of fp32.
 #pragma once
 #include <type_traits>
 #include <cuda.h>
@@ -208,9 +209,6 @@ __device__ __forceinline__ uint32_t bf16_pair_times(uint32_t w, float f) {
 }
 __device__ __forceinline__ bool bf16_pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
-// A bounded wait of a whole warp.  Smaller than wait_bounded (limit in units of 2^32 cycles, reported at the kernel's end): it stands in some
-// thirty places, and the kernel's code has to stay in the instruction cache - at 298 KB, everything inline several times over, each step of
-// a short item cost microseconds.
 // The same number, which the compiler takes for another one each time: conditions on it are not moved out of a loop by doubling the loop.
 __device__ __forceinline__ int opaque(int v) {
     asm volatile("" : "+r"(v));
@@ -221,6 +219,9 @@ __device__ __forceinline__ uint32_t clock_hi() {
     asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(t));
     return t;
 }
+// A bounded wait of a whole warp.  Smaller than wait_bounded (limit in units of 2^32 cycles, reported at the kernel's end): it stands in some
+// thirty places, and the kernel's code has to stay in the instruction cache - at 298 KB, everything inline several times over, each step of
+// a short item cost microseconds.
 __device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
     bool ok = ptx::mbar_try_wait(bar, parity);
     if (!ok) {

@@ -269,6 +269,8 @@ int kv_attention_impl(const gmlp_kv_attention_args* a) {
     const int q_pos = a->T < k.tile_pos ? (int)a->T : k.tile_pos, D = a->cache.head_dim;
     // Where a request has more than 256 rows (a big item's) on average, most belong to big items, and these run better in the kernel that has no
     // code for few ones (a chunk of 2048 237 us with, 226 without; 40 single tokens and three chunks of 500, 143 rows on average, 234 and 246).
+    // The host knows neither the lengths nor which rows belong to a request: padded rows count, and a chunk beside single tokens over many more
+    // keys may take the kernel without few items although most of the work is theirs.
     const bool few = a->T * ratio <= 256 * a->B;
     k.few_pos = few ? gmlp::kKvFew / ratio : 0;                              // 0: none
     const int few_pos = k.few_pos == 0 ? q_pos : (a->T < k.few_pos ? (int)a->T : k.few_pos);

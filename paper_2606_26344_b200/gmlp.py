@@ -1056,7 +1056,8 @@ def rope_steps(rotary_dim: int, base: float = 10000.0, scaling=None):
 
 class Rope:
     """A rotation's table (gmlp_rope): ``rotary_dim`` channels of each head, pairs (i, i + rotary_dim / 2) or, ``interleaved``,
-    (2 i, 2 i + 1).  ``scaling`` as for rope_steps(); ``amplitude`` overrides the scaling's own."""
+    (2 i, 2 i + 1).  ``scaling`` as for rope_steps(); ``amplitude`` overrides the scaling's own.  Built once per model: the table goes to the
+    device with a blocking copy."""
     __slots__ = ("steps", "rotary_dim", "interleaved", "amplitude", "device", "struct")
 
     def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None,

@@ -255,3 +255,34 @@ def test_scores_of_large_magnitude(r, n, power, sign):
     # rounding removes (V is a bf16 number); one term (big items) to 2^-8 of the value, and the last rounding may take 2^-8 on top.
     one_term, value = r * 4 > 128, v[j].double()[None, :, None].expand(r, 2, 4, 128)
     assert bool(((batch.run().view(r, 2, 4, 128).double() - value).abs() <= (2.0 ** -7 * 1.01 if one_term else 0.0) * value.abs()).all())
+
+
+@pytest.mark.parametrize("reqs,Hq,Hkv,D,page", [KINDS[1], KINDS[4], KINDS[6], KINDS[7], KINDS[9]])
+@pytest.mark.parametrize("size", [1.0, 3.38e38])
+def test_a_second_pass_without_a_mask_and_with_bad_pages(reqs, Hq, Hkv, D, page, size):
+    """Without a causal mask; then with a page outside of the cache in the first request, whose keys are left out, beside an infinity in the next
+    page of each key head."""
+    batch = Batch(reqs, Hq, Hkv, D, page)
+    v, some = batch.cache.v, range(0, len(reqs), max(1, len(reqs) // 20))
+    v.copy_(torch.where(torch.isnan(v), v, size * (2 * torch.rand(v.shape, generator=gen(2), device=DEV) - 1).to(torch.bfloat16)))
+    assert bool(torch.isfinite(batch.check(causal=False, only=some)).all())
+    (r, n), ratio = reqs[0], Hq // Hkv
+    v[batch.table[0, 2].long(), :, 1, 4] = math.inf
+    batch.table[0, 1] = batch.cache.n_pages
+    O = torch.full_like(batch.Q, 7.0)
+    gmlp.kv_attention(batch.Q, batch.cache, batch.table, batch.lengths, Hq, q_start=batch.start, causal=False, O=O)
+    assert gmlp.device_status() >> 16 == 200
+    batch.check_rows(O, causal=False, only=[b for b in some if b > 0])
+    got = O[:r].view(r, Hkv, ratio, D)
+    assert bool((got[..., 4] == math.inf).all())
+    j = torch.arange(n, device=DEV)
+    j = j[j // page != 1]
+    k, x = (c[batch.table[0, j // page].long(), :, j % page].double() for c in (batch.cache.k, v))
+    q = batch.Q[:r].double().view(r, Hkv, ratio, D)
+    p = (torch.einsum("rghd,ngd->rghn", q, k) * D ** -0.5).softmax(-1)
+    x[..., 4] = 0.0
+    want, A = torch.einsum("rghn,ngd->rghd", p, x), torch.einsum("rghn,ngd->rghd", p, x.abs())
+    # rounding of O and of each probability, 2^-8; scores and sums as in the others' bound, far below
+    ok = (got.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -9) * A
+    ok[..., 4] = True
+    assert bool(ok.all())

@@ -31,3 +31,9 @@ def test_rows_over_many_keys(case):
                                                 ([(200, 2500), (1, 5000), (3, 900)] * 4, 8, 2, 64, 48)])
 def test_rows_of_items_cut_between_ctas(reqs, Hq, Hkv, D, page):
     check(reqs, Hq, Hkv, D, page, only=range(0, len(reqs), max(1, len(reqs) // 24)))
+
+
+@pytest.mark.parametrize("r", [1, 20, 64])
+def test_parts_of_more_than_one_piece(r):
+    """24 items of 400000 to 600000 keys over the SMs: parts of some 600 blocks of 128 keys, more than are summed at a time."""
+    check([(r, 400001), (r, 500000), (r, 599999)], 32, 8, 64, 64, only=(0, 2))
